@@ -18,7 +18,7 @@ CODES = {"fp32": 0, "bf16": 1, "fp16": 2}
 PARAM = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
 ACT = {"fp32": torch.float64, "bf16": torch.bfloat16, "fp16": torch.float16}
 RESID = {"fp32": torch.float64, "bf16": torch.float32, "fp16": torch.float32}
-EPS = 1e-5
+EPS = float(torch.tensor(1e-5, dtype=torch.float32))      # calls take it, and the loss's scale, as an fp32 number
 
 
 def listed():
@@ -120,7 +120,7 @@ def prepare(case, seed):
         target.view(case["batch"], case["seq"])[:, -1] = -1          # the last position of a prompt has no next token
         s["target"] = target.to(torch.int32)
         # the mean over the positions that count; fp16 gradients are scaled up as fp16 training does
-        s["scale"] = (16384.0 if dt == "fp16" else 1.0) / (case["batch"] * (case["seq"] - 1))
+        s["scale"] = float(torch.tensor((16384.0 if dt == "fp16" else 1.0) / (case["batch"] * (case["seq"] - 1)), dtype=torch.float32))
         s["row_loss"] = torch.empty(rows, device=DEV, dtype=RESID[dt])
         s["dx"] = torch.empty((rows, d), device=DEV, dtype=ACT[dt])
         s["de"] = torch.empty((vocab, d), device=DEV, dtype=PARAM[dt])
