@@ -343,6 +343,57 @@ int zo_kernel_lmhead_ce(const void *x, const void *e_plus, const void *e_minus, 
 int zo_kernel_lmhead_ce_noalloc(const void *x, const void *e_plus, const void *e_minus, const int32_t *target,
                                 double *row_loss, int dtype, int m_half, int d, int vocab, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Gradient of the last module.  The final LayerNorm and the tied LM head are the
+ * one module whose exact gradient needs no other module's: these calls give it,
+ * for programs that train that module by its gradient and the blocks by Eq. 2, or
+ * that hold g against z . grad L.  One copy of the parameters, rows in any number;
+ * bare buffers, as above.  Types go with dtype as everywhere: activations (x, y
+ * and their gradients dx, dy) are 16-bit, or double for ZO_FP32; the residual
+ * stream, its gradient, mean, rstd and row losses fp32, or double for ZO_FP32; a
+ * parameter's gradient has the parameter's type.  Every sum is taken in fp32 (fp64
+ * for ZO_FP32) and rounded once.  All results are the same bits every time.
+ * Scratch: device memory of the size the _scratch_bytes call says, 256-byte
+ * aligned; a call writes what it reads there, so nothing has to start at zero, and
+ * calls whose kernels may overlap (other streams, graphs that replay at the same
+ * time) need one each.
+ * ---------------------------------------------------------------------- */
+
+/* LayerNorm of resid [rows, d] with its statistics kept: mean[r] = sum h / d, rstd[r] = (sum (h - mean)^2 / d + ln_eps)^-1/2,
+ * y = gain (h - mean) rstd + bias. */
+int zo_kernel_layernorm(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype,
+                        int rows, int d, float ln_eps, void *stream);
+
+/* Its backward pass.  With xh = (h - mean) rstd and a = dy gain, per row:
+ *     dresid = rstd (a - mean_c(a) - xh mean_c(a xh)),    dgain = sum_r dy xh,    dbias = sum_r dy.
+ * accumulate non-zero: dresid is added to what the buffer holds (the gradient that passes the LayerNorm by on the residual
+ * stream).  dresid may be NULL (gain may be, then), or dgain and dbias both (scratch may be, then).  dresid may not overlap
+ * the inputs. */
+size_t zo_kernel_layernorm_grad_scratch_bytes(int dtype, int rows, int d);
+int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid,
+                             void *dgain, void *dbias, void *scratch, int dtype, int rows, int d, int accumulate, void *stream);
+
+/* Tied LM head and cross entropy, forward and backward: for x [rows, d] and e [vocab, d], logits l = x e^T,
+ *     row_loss[r] = logsumexp(l[r]) - l[r, target[r]],    G = scale (softmax(l) - onehot(target)),    dx = G e,    de = G^T x.
+ * A row with target[r] < 0 does not count: row_loss, its row of G and its row of dx are 0 whatever x[r] holds, NaN included.  A
+ * target >= vocab makes the row's loss NaN, and dx[r] and de with it.  scale: 1 / (rows that count) for the mean loss, times
+ * whatever keeps ZO_FP16 gradients in range.  de is the head's share of the tied embedding's gradient alone.  2-byte
+ * dtypes: d and vocab multiples of 8, buffers 16-byte aligned (ZO_EINVAL otherwise). */
+size_t zo_kernel_lmhead_grad_scratch_bytes(int dtype, int rows, int d, int vocab);
+int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch,
+                          int dtype, int rows, int d, int vocab, float scale, void *stream);
+
+/* Global norm of n_tensors gradients and clipping by it: norm[0] = sqrt(sum of all squares), norm[1] = c = max_norm / norm[0] where
+ * norm[0] > max_norm, else 1; dst[t] = rn(c src[t]) for every tensor t of numel[t] elements.  A norm that is not a finite number makes c 0 and
+ * every dst zeros, as a g that is not finite leaves theta alone.  The sums are taken in fp64.
+ *   src, dst, numel  host arrays of n_tensors device pointers and counts, read before the call returns; tensors of dtype's storage
+ *                    type, 16-byte aligned.  dst[t] may be src[t], and otherwise overlaps no tensor.  numel 0: skipped.
+ *   max_norm         > 0; infinity for the norm alone (dst[t] = src[t] is then not touched)
+ *   norm             device, double[2] */
+size_t zo_kernel_grad_clip_scratch_bytes(void);
+int zo_kernel_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm,
+                        double *norm, void *scratch, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

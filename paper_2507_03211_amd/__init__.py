@@ -26,6 +26,8 @@ EXPORTS = (
     "zo_kernel_z", "zo_kernel_normal_pairs", "zo_kernel_axpy_z", "zo_kernel_axpy_z_sr", "zo_kernel_stage_pm", "zo_kernel_stage_update_pm", "zo_kernel_linear_pm", "zo_kernel_linear_tile",
     "zo_kernel_layernorm_pm", "zo_kernel_attention", "zo_kernel_lmhead_scratch_bytes", "zo_kernel_lmhead_ce",
     "zo_kernel_lmhead_ce_noalloc",
+    "zo_kernel_layernorm", "zo_kernel_layernorm_grad_scratch_bytes", "zo_kernel_layernorm_grad", "zo_kernel_lmhead_grad_scratch_bytes",
+    "zo_kernel_lmhead_grad", "zo_kernel_grad_clip_scratch_bytes", "zo_kernel_grad_clip",
 )
 
 
@@ -89,6 +91,16 @@ def lib():
         L.zo_kernel_lmhead_scratch_bytes.argtypes = [i32, i32, i32]
         L.zo_kernel_lmhead_ce.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
         L.zo_kernel_lmhead_ce_noalloc.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
+        L.zo_kernel_layernorm.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, f32, vp]
+        L.zo_kernel_layernorm_grad_scratch_bytes.restype = sz
+        L.zo_kernel_layernorm_grad_scratch_bytes.argtypes = [i32, i32, i32]
+        L.zo_kernel_layernorm_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
+        L.zo_kernel_lmhead_grad_scratch_bytes.restype = sz
+        L.zo_kernel_lmhead_grad_scratch_bytes.argtypes = [i32, i32, i32, i32]
+        L.zo_kernel_lmhead_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, f32, vp]
+        L.zo_kernel_grad_clip_scratch_bytes.restype = sz
+        L.zo_kernel_grad_clip_scratch_bytes.argtypes = []
+        L.zo_kernel_grad_clip.argtypes = [vp, vp, vp, i32, i32, f32, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -294,3 +306,48 @@ ZO_NOALLOC_SCRATCH_BYTES = 32 << 20
 def zo_kernel_lmhead_ce_noalloc(x, e_plus, e_minus, target, row_loss, dtype, m_half, d, vocab, stream=None):
     _check(lib().zo_kernel_lmhead_ce_noalloc(_ptr(x), _ptr(e_plus), _ptr(e_minus), _ptr(target), _ptr(row_loss),
                                              dtype, m_half, d, vocab, _stream(stream)))
+
+
+def zo_kernel_layernorm(resid, gain, bias, y, mean, rstd, dtype, rows, d, ln_eps, stream=None):
+    _check(lib().zo_kernel_layernorm(_ptr(resid), _ptr(gain), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), dtype, rows, d, ln_eps,
+                                     _stream(stream)))
+
+
+def zo_kernel_layernorm_grad_scratch_bytes(dtype, rows, d):
+    return int(lib().zo_kernel_layernorm_grad_scratch_bytes(dtype, rows, d))
+
+
+def zo_kernel_layernorm_grad(dy, resid, gain, mean, rstd, dresid, dgain, dbias, scratch, dtype, rows, d, accumulate=False, stream=None):
+    _check(lib().zo_kernel_layernorm_grad(_ptr(dy), _ptr(resid), _ptr(gain), _ptr(mean), _ptr(rstd), _ptr(dresid), _ptr(dgain), _ptr(dbias),
+                                          _ptr(scratch), dtype, rows, d, int(accumulate), _stream(stream)))
+
+
+def zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab):
+    return int(lib().zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab))
+
+
+def zo_kernel_lmhead_grad(x, e, target, row_loss, dx, de, scratch, dtype, rows, d, vocab, scale, stream=None):
+    _check(lib().zo_kernel_lmhead_grad(_ptr(x), _ptr(e), _ptr(target), _ptr(row_loss), _ptr(dx), _ptr(de), _ptr(scratch), dtype, rows, d,
+                                       vocab, scale, _stream(stream)))
+
+
+def zo_kernel_grad_clip_scratch_bytes():
+    return int(lib().zo_kernel_grad_clip_scratch_bytes())
+
+
+def _table(items, ctype):
+    """A host array of addresses or counts: a ctypes array as it is (a program that clips the same tensors every step keeps one), else
+    built from the list's tensors, addresses or numbers."""
+    if isinstance(items, ctypes.Array):
+        if items._type_ is not ctype:
+            raise TypeError("expected an array of %s, got one of %s" % (ctype.__name__, items._type_.__name__))
+        return items
+    return (ctype * len(items))(*[_ptr(t) for t in items])
+
+
+def zo_kernel_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, norm, scratch, stream=None):
+    """`src`, `dst`: lists of tensors or addresses, `numel`: list of counts; or ctypes arrays of them (c_void_p, c_uint64)."""
+    src, dst, numel = _table(src, ctypes.c_void_p), _table(dst, ctypes.c_void_p), _table(numel, ctypes.c_uint64)
+    if min(len(src), len(dst), len(numel)) < n_tensors:
+        raise ValueError("n_tensors is %d, the tables hold %d, %d and %d" % (n_tensors, len(src), len(dst), len(numel)))
+    _check(lib().zo_kernel_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, _ptr(norm), _ptr(scratch), _stream(stream)))

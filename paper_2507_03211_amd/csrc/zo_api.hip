@@ -1339,3 +1339,76 @@ extern "C" int zo_kernel_lmhead_ce_noalloc(const void *x, const void *e_plus, co
     // and target logits by the GEMM epilogue, the logits chunk by the GEMM): nothing has to start at zero
     return lmhead_ce(nullptr, (hipStream_t)stream, x, e_plus, e_minus, target, row_loss, buf, chunk_rows, dtype, 2, m_half, d, vocab, true);
 }
+
+// ------------------------------------------------------------------ gradient of the last module
+extern "C" int zo_kernel_layernorm(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype, int rows, int d,
+                                   float ln_eps, void *stream)
+{
+    ZO_TRY(check_dtype(dtype));
+    if (!resid || !gain || !bias || !y || !mean || !rstd) return fail(ZO_EINVAL, "NULL argument");
+    if (rows < 1 || d < 1) return fail(ZO_EINVAL, "bad shape %d x %d", rows, d);
+    if (!(ln_eps > 0.0f)) return fail(ZO_EINVAL, "ln_eps must be positive");
+    ZO_HIP(launch_layernorm_stats(resid, gain, bias, y, mean, rstd, dtype, rows, d, ln_eps, (hipStream_t)stream));
+    return ZO_OK;
+}
+
+extern "C" size_t zo_kernel_layernorm_grad_scratch_bytes(int dtype, int rows, int d)
+{
+    return dtype < 0 || dtype > 2 || rows < 1 || d < 1 ? 0 : layernorm_grad_scratch(dtype, rows, d);
+}
+
+extern "C" int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid, void *dgain,
+                                        void *dbias, void *scratch_mem, int dtype, int rows, int d, int accumulate, void *stream)
+{
+    ZO_TRY(check_dtype(dtype));
+    if (!dy || !resid || !mean || !rstd) return fail(ZO_EINVAL, "NULL argument");
+    if (rows < 1 || d < 1) return fail(ZO_EINVAL, "bad shape %d x %d", rows, d);
+    if (!dgain != !dbias) return fail(ZO_EINVAL, "dgain and dbias go together: one of them is NULL");
+    if (!dresid && !dgain) return fail(ZO_EINVAL, "no output asked for");
+    if (dresid && !gain) return fail(ZO_EINVAL, "gain is NULL");
+    if (dgain && !scratch_mem) return fail(ZO_EINVAL, "scratch is NULL");
+    if (dgain && (uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");
+    ZO_HIP(launch_layernorm_grad(dy, resid, gain, mean, rstd, dresid, dgain, dbias, scratch_mem, dtype, rows, d, accumulate != 0, (hipStream_t)stream));
+    return ZO_OK;
+}
+
+extern "C" size_t zo_kernel_lmhead_grad_scratch_bytes(int dtype, int rows, int d, int vocab)
+{
+    return dtype < 0 || dtype > 2 || rows < 1 || d < 1 || vocab < 2 ? 0 : head_grad_scratch(dtype, rows, d, vocab);
+}
+
+extern "C" int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch_mem, int dtype,
+                                     int rows, int d, int vocab, float scale, void *stream)
+{
+    ZO_TRY(check_dtype(dtype));
+    if (!x || !e || !target || !row_loss || !dx || !de || !scratch_mem) return fail(ZO_EINVAL, "NULL argument");
+    if (rows < 1 || d < 1 || vocab < 2) return fail(ZO_EINVAL, "bad shape: %d rows, d %d, vocab %d", rows, d, vocab);
+    if (dtype != ZO_FP32 && (d % 8 || vocab % 8)) return fail(ZO_EINVAL, "d and vocab must be multiples of 8 for 2-byte types");
+    if (dtype != ZO_FP32 && ((uintptr_t)x % 16 || (uintptr_t)e % 16 || (uintptr_t)dx % 16 || (uintptr_t)de % 16))
+        return fail(ZO_EINVAL, "buffers must be 16-byte aligned");
+    if ((uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");
+    if (!(scale - scale == 0.0f)) return fail(ZO_EINVAL, "scale must be a finite number");
+    ZO_HIP(launch_head_grad(x, e, target, row_loss, dx, de, scratch_mem, dtype, rows, d, vocab, scale, (hipStream_t)stream));
+    return ZO_OK;
+}
+
+extern "C" size_t zo_kernel_grad_clip_scratch_bytes(void) { return kClipSlots * sizeof(double); }
+
+extern "C" int zo_kernel_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm, double *norm,
+                                   void *scratch_mem, void *stream)
+{
+    ZO_TRY(check_dtype(dtype));
+    if (n_tensors < 0) return fail(ZO_EINVAL, "n_tensors %d is negative", n_tensors);
+    if (n_tensors && (!src || !dst || !numel)) return fail(ZO_EINVAL, "NULL argument");
+    if (!norm || !scratch_mem) return fail(ZO_EINVAL, "NULL argument");
+    if ((uintptr_t)scratch_mem % 256 || (uintptr_t)norm % 8) return fail(ZO_EINVAL, "scratch must be 256-byte aligned, norm 8-byte");
+    if (!(max_norm > 0.0f)) return fail(ZO_EINVAL, "max_norm must be positive");
+    for (int i = 0; i < n_tensors; ++i) {
+        if (numel[i] == 0) continue;
+        if (!src[i] || !dst[i]) return fail(ZO_EINVAL, "tensor %d is NULL", i);
+        if ((uintptr_t)src[i] % 16 || (uintptr_t)dst[i] % 16) return fail(ZO_EINVAL, "tensor %d is not 16-byte aligned", i);
+        if (numel[i] >= 1ull << 44) return fail(ZO_EINVAL, "tensor %d has %llu elements", i, (unsigned long long)numel[i]);
+    }
+    ZO_HIP(launch_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, norm, scratch_mem, (hipStream_t)stream));
+    return ZO_OK;
+}

@@ -109,4 +109,35 @@ bool mfma_attention_supported(int seq, int n_heads, int d_head);
 hipError_t launch_attention_mfma(const void *qkv, void *out, int dtype, int n_seq, int seq, int n_heads,
                                  int d_head, hipStream_t s);
 
+// ---- gradient of the last module (zo_grad_kernels.hip) ----
+hipError_t launch_layernorm_stats(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype, int rows,
+                                  int d, float eps, hipStream_t s);
+// `dresid` may be null, and `dgain` with `dbias`.  `scratch`: layernorm_grad_scratch bytes
+size_t layernorm_grad_scratch(int dtype, int rows, int d);
+hipError_t launch_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid, void *dgain,
+                                 void *dbias, void *scratch, int dtype, int rows, int d, bool accumulate, hipStream_t s);
+size_t head_grad_scratch(int dtype, int rows, int d, int vocab);
+hipError_t launch_head_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype,
+                            int rows, int d, int vocab, float scale, hipStream_t s);
+
+struct ClipDesc {            // one tensor of a pass over gradients
+    const void *src;
+    void *dst;
+    uint32_t first, chunks;  // its first chunk in the launch, and how many it has
+    uint32_t last;           // elements of the last one
+    uint32_t pad;
+};
+constexpr uint32_t kClipChunk = 16384;     // elements per chunk
+constexpr uint32_t kClipSlots = 1024;      // workgroups of a pass at most, each with a partial sum of its own
+constexpr int kClipMax = 124;
+struct ClipBatch {
+    int n;
+    uint32_t chunks;
+    ClipDesc d[kClipMax];
+};
+static_assert(sizeof(ClipBatch) + 64 <= 4096, "passed by value: a kernel takes 4 KiB of arguments");
+// dst may be src, tensor by tensor.  `scratch`: kClipSlots doubles; `norm`: the norm and the coefficient
+hipError_t launch_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm, double *norm,
+                            void *scratch, hipStream_t s);
+
 }  // namespace zo

@@ -1,0 +1,199 @@
+"""LayerNorm with its statistics and its backward pass against the formulas in 64 bits, element by element.
+
+Tolerances.  A sum over a row of d elements, or over `rows` rows, goes through chains of at most K(n) = 128 + n / 64 additions
+(a lane's share, then a tree), each off by u of the sum of magnitudes at most; every other operation by u of its result.
+Results are then rounded to their type: half a step.
+"""
+import pytest
+import torch
+
+import paper_2507_03211_amd as zo_amd
+import zo_inputs as zi
+from gpu_util import DEV, act_dtype, resid_dtype
+from grad_util import Out, generator, half, least, normal, param_dtype, unit
+
+pytestmark = pytest.mark.gpu
+EPS = float(torch.tensor(1e-5, dtype=torch.float32))            # as the call gets it
+DTYPES = [zi.FP32, zi.BF16, zi.FP16]
+SHAPES = [(1, 1), (5, 7), (3, 64), (67, 64), (64, 200), (9, 768), (1003, 768), (2, 1100), (70, 1536), (4, 1792), (7, 2048), (6, 2052), (13, 3001), (5, 4096),
+          (300, 5120), (9, 6000), (3, 8192), (3, 12288), (5, 12292), (2, 13001), (3000, 16), (2500, 130), (1, 5120)]
+
+
+def K(n):
+    return 128 + n / 64
+
+
+def rows_of(dtype, rows, d, seed=0):
+    g = generator(1000 * rows + d + seed)
+    h = (normal((rows, d), torch.float64, g) * (0.5 + 2.0 * torch.rand((rows, 1), device=DEV, generator=g, dtype=torch.float64))
+         + normal((rows, 1), torch.float64, g)).to(resid_dtype(dtype))
+    gain = (1.0 + normal((d,), torch.float64, g, 0.3)).to(param_dtype(dtype))
+    return g, h, gain
+
+
+def stats64(h):
+    h = h.double()
+    mean = h.mean(1)
+    return mean, ((h - mean[:, None]).square().mean(1) + EPS).rsqrt()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,d", SHAPES)
+def test_forward(dtype, rows, d):
+    g, h, gain = rows_of(dtype, rows, d)
+    bias = normal((d,), param_dtype(dtype), g, 0.3)
+    y, mean, rstd = Out((rows, d), act_dtype(dtype)), Out((rows,), resid_dtype(dtype)), Out((rows,), resid_dtype(dtype))
+    zo_amd.zo_kernel_layernorm(h, gain, bias, y.t, mean.t, rstd.t, dtype, rows, d, EPS)
+    m, r = stats64(h)
+    u, k = unit(dtype), K(d)
+    hd, gd, bd = h.double(), gain.double(), bias.double()
+    size = hd.abs().mean(1)
+    off_mean = 1.1 * (k + 1) * u * size
+    # of the variance: every difference carries the mean's error and a rounding, the sum its chain; rstd takes half of it
+    centred = (hd - m[:, None]).abs()
+    off_var = 2 * centred.mean(1) * off_mean + off_mean**2 + (k + 6) * u * centred.square().mean(1)
+    off_rstd = r * (0.6 * off_var * r * r + 4 * u)
+    assert ((mean.t.double() - m).abs() <= off_mean).all()
+    assert ((rstd.t.double() - r).abs() <= off_rstd).all()
+    xh = (hd - m[:, None]) * r[:, None]
+    want = xh * gd + bd
+    off = gd.abs() * (xh.abs() * (off_rstd / r)[:, None] + r[:, None] * (off_mean[:, None] + u * centred)) + 3 * u * ((xh * gd).abs() + bd.abs())
+    t = act_dtype(dtype)
+    tol = half(t) * want.abs() + 1.01 * off + least(t)
+    assert ((y.t.double() - want).abs() <= tol).all()
+    assert y.whole() and mean.whole() and rstd.whole()
+
+
+def backward(dtype, rows, d, dy, h, gain, mean, rstd, dresid=True, weights=True, before=None):
+    dh = Out((rows, d), resid_dtype(dtype), fill=None) if dresid else None
+    if before is not None:
+        dh.t.copy_(before)
+    dg, db = (Out((d,), param_dtype(dtype)) for _ in range(2)) if weights else (None, None)
+    scratch = Out((zo_amd.zo_kernel_layernorm_grad_scratch_bytes(dtype, rows, d),), torch.uint8)
+    zo_amd.zo_kernel_layernorm_grad(dy, h, gain, mean, rstd, dh.t if dh else None, dg.t if dg else None, db.t if db else None, scratch.t, dtype,
+                                    rows, d, before is not None)
+    torch.cuda.synchronize()
+    assert scratch.whole()
+    for o in (dh, dg, db):
+        assert o is None or o.whole()
+    return [o.t if o else None for o in (dh, dg, db)]
+
+
+def check_backward(dtype, rows, d, dy, h, gain, mean, rstd, got, before=None):
+    u = unit(dtype)
+    dyd, hd, gd, m, r = dy.double(), h.double(), gain.double(), mean.double()[:, None], rstd.double()[:, None]
+    xh = (hd - m) * r
+    off_xh = 2 * u * xh.abs()                                          # the difference and the product
+    a = dyd * gd
+    ma, mx = a.mean(1, keepdim=True), (a * xh).mean(1, keepdim=True)
+    off_ma = (K(d) + 3) * u * a.abs().mean(1, keepdim=True)
+    off_mx = (K(d) + 6) * u * (a * xh).abs().mean(1, keepdim=True)
+    dh, dg, db = got
+    if dh is not None:
+        want = r * (a - ma - xh * mx)
+        off = r * (off_ma + xh.abs() * off_mx + off_xh * mx.abs() + 5 * u * (a.abs() + ma.abs() + (xh * mx).abs()))
+        if before is not None:
+            want = want + before.double()
+            off = off + u * want.abs()
+        assert ((dh.double() - want).abs() <= 1.01 * off).all()
+    if dg is not None:
+        t = param_dtype(dtype)
+        for have, want, size in ((dg, (dyd * xh).sum(0), (dyd * xh).abs().sum(0)), (db, dyd.sum(0), dyd.abs().sum(0))):
+            # (fp32 gradients of 64-bit sums: the rounding through fp32 is theirs)
+            tol = (half(t) * want.abs() * 1.01 + 1.01 * (K(rows) + 4) * u * size + least(t))
+            assert ((have.double() - want).abs() <= tol).all()
+
+
+def case(dtype, rows, d, seed=0):
+    g, h, gain = rows_of(dtype, rows, d, seed)
+    m, r = stats64(h)
+    dy = normal((rows, d), act_dtype(dtype), g, 0.1)
+    return dy, h, gain, m.to(resid_dtype(dtype)), r.to(resid_dtype(dtype))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,d", SHAPES)
+def test_backward(dtype, rows, d):
+    c = case(dtype, rows, d)
+    check_backward(dtype, rows, d, *c, backward(dtype, rows, d, *c))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,d", [(37, 768), (12, 2052), (5, 333)])
+def test_accumulates_and_leaves_out(dtype, rows, d):
+    c = case(dtype, rows, d, 5)
+    before = normal((rows, d), resid_dtype(dtype), generator(3), 0.2)
+    check_backward(dtype, rows, d, *c, backward(dtype, rows, d, *c, before=before), before=before)
+    both = backward(dtype, rows, d, *c)
+    only_dh = backward(dtype, rows, d, *c, weights=False)
+    only_w = backward(dtype, rows, d, *c, dresid=False)
+    assert torch.equal(both[0], only_dh[0]) and torch.equal(both[1], only_w[1]) and torch.equal(both[2], only_w[2])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 768, 5120, 1001])
+def test_against_differences(dtype, d):
+    """sum(dy . y) along a direction of (h, gain, bias), by the formulas in 64 bits at two steps, against the gradient: the error of a
+    central difference falls by four when its step is halved, so that of the finer one is a third of what the two differ by."""
+    rows = 6
+    g, h, gain = rows_of(dtype, rows, d, 9)
+    m, r = stats64(h)
+    dy = normal((rows, d), act_dtype(dtype), g, 0.1)
+    dh, dg, db = backward(dtype, rows, d, dy, h, gain, m.to(resid_dtype(dtype)), r.to(resid_dtype(dtype)))
+    vh, vg, vb = (normal(s, torch.float64, g) for s in ((rows, d), (d,), (d,)))
+
+    def f(t):
+        hh = h.double() + t * vh
+        mm, rr = stats64(hh)
+        return (dy.double() * ((hh - mm[:, None]) * rr[:, None] * (gain.double() + t * vg) + t * vb)).sum()
+
+    step = 1e-3
+    coarse, fine = ((f(s) - f(-s)) / (2 * s) for s in (step, step / 2))
+    got = (dh.double() * vh).sum() + (dg.double() * vg).sum() + (db.double() * vb).sum()
+    t = param_dtype(dtype)
+    # the weights' roundings are independent: seven standard deviations of at most half a step each; fp32 statistics and dresid: 2^-18 of the sum's size
+    size = (dh.double() * vh).abs().sum()
+    off = 7 * half(t) * torch.sqrt((dg.double() * vg).square().sum() + (db.double() * vb).square().sum()) + (2.0**-18 if dtype != zi.FP32 else 2.0**-40) * size
+    assert (got - fine).abs() <= (coarse - fine).abs() + off + 1e-9 * size
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,d", [(5, 768), (4, 5120), (3, 77)])
+def test_constant_rows_and_what_is_not_finite(dtype, rows, d):
+    """A row of equal elements has xh = 0 and rstd = eps^-1/2; a row that holds a NaN or an infinity spoils itself and nobody else."""
+    g, h, gain = rows_of(dtype, rows, d, 2)
+    h[0] = 3.0
+    h[1, d // 2] = float("nan")
+    h[2, d - 1] = float("inf")
+    bias = normal((d,), param_dtype(dtype), g, 0.3)
+    y, mean, rstd = Out((rows, d), act_dtype(dtype)), Out((rows,), resid_dtype(dtype)), Out((rows,), resid_dtype(dtype))
+    zo_amd.zo_kernel_layernorm(h, gain, bias, y.t, mean.t, rstd.t, dtype, rows, d, EPS)
+    assert torch.equal(y.t[0], bias.to(y.t.dtype)) and mean.t[0] == 3.0
+    assert not torch.isfinite(y.t[1]).any() and not torch.isfinite(y.t[2]).all()
+    assert torch.isfinite(y.t[3:]).all()
+    dy = normal((rows, d), act_dtype(dtype), g)
+    dh, dg, db = backward(dtype, rows, d, dy, h, gain, mean.t, rstd.t)
+    assert torch.isfinite(dh[0]).all() and torch.isfinite(dh[3:]).all() and torch.isfinite(db).all()
+    assert not torch.isfinite(dh[1]).any() and not torch.isfinite(dg).all()
+
+
+@pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
+@pytest.mark.parametrize("d", [768, 5120])
+def test_buffers_off_their_alignment(dtype, d):
+    """Elements are all a buffer need be aligned to: rows that start anywhere give the same numbers to their tolerance."""
+    rows = 11
+    dy, h, gain, m, r = case(dtype, rows, d, 4)
+
+    def shifted(t):
+        raw = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+        raw[1:] = t.reshape(-1)
+        return raw[1:].view(t.shape)
+
+    check_backward(dtype, rows, d, dy, h, gain, m, r, backward(dtype, rows, d, shifted(dy), shifted(h), shifted(gain), m, r))
+    bias = normal((d,), param_dtype(dtype), generator(8), 0.3)
+    outs = []
+    for move in (lambda t: t, shifted):
+        y, mean, rstd = move(torch.zeros((rows, d), dtype=act_dtype(dtype), device=DEV)), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        zo_amd.zo_kernel_layernorm(move(h), move(gain), move(bias), y, mean, rstd, dtype, rows, d, EPS)
+        outs.append(y.double())
+    assert ((outs[0] - outs[1]).abs() <= 2 * half(act_dtype(dtype)) * outs[0].abs() + 2.0**-16).all()

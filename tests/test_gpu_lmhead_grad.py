@@ -1,0 +1,224 @@
+"""Cross entropy of the tied LM head with its gradient against the formulas in 64 bits, element by element.
+
+Tolerances (16-bit types).  A logit is a sum of d products in fp32: off by A u sum |x e|, A = 16 + d / 8 (the matrix
+instructions add sixteen products at a time; the row's largest such error is `dl`).  A probability is off by 2 dl + 2^-21 of itself: its
+own logit, the row's logsumexp, and exponential, sums and roundings of 32 bits.  It enters the products rounded to the 16-bit type, by half
+a step `h` at most.  These roundings are independent, so a sum of n such terms is off by 7 h sqrt(sum of squares) (bounded
+independent terms pass that once in 10^10), everything else by its worst case; then the result is rounded, half a step.
+fp32 parameters: all in fp64, results of the parameters' type rounded once.
+"""
+import pytest
+import torch
+
+import paper_2507_03211_amd as zo_amd
+import zo_inputs as zi
+from gpu_util import DEV, act_dtype, resid_dtype
+from grad_util import Out, generator, half, least, normal, param_dtype, unit
+
+pytestmark = pytest.mark.gpu
+HALVES = [zi.BF16, zi.FP16]
+
+
+def inputs(dtype, rows, d, vocab, seed=0, lean=12.0, std=0.05):
+    g = generator(seed + 7 * rows + 13 * d + vocab)
+    e = normal((vocab, d), param_dtype(dtype), g, std)
+    target = torch.randint(0, vocab, (rows,), device=DEV, generator=g)
+    x = normal((rows, d), torch.float64, g)
+    x = (x + lean / (std * std * d) * torch.rand((rows, 1), device=DEV, generator=g, dtype=torch.float64) * e[target].double()).to(act_dtype(dtype))
+    if rows > 2:
+        target[torch.randperm(rows, device=DEV, generator=g)[:max(1, rows // 7)]] = -1
+    return x, e, target.to(torch.int32)
+
+
+def call(dtype, x, e, target, scale, stream=None):
+    (rows, d), vocab = x.shape, e.shape[0]
+    loss, dx, de = Out((rows,), resid_dtype(dtype)), Out((rows, d), act_dtype(dtype)), Out((vocab, d), param_dtype(dtype))
+    scratch = Out((zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab),), torch.uint8)
+    zo_amd.zo_kernel_lmhead_grad(x, e, target, loss.t, dx.t, de.t, scratch.t, dtype, rows, d, vocab, scale, stream)
+    torch.cuda.synchronize()
+    assert loss.whole() and dx.whole() and de.whole() and scratch.whole()
+    return loss.t, dx.t, de.t
+
+
+def check(dtype, x, e, target, scale, got):
+    """x's rows of targets < 0 are taken as zeros; the scale is an fp32 number, as the call gets it."""
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    loss, dx, de = got
+    (rows, d), vocab = x.shape, e.shape[0]
+    live = target >= 0
+    xd, ed = torch.where(live[:, None], x.double(), 0.0), e.double()
+    at = target.clamp(min=0).long()[:, None]
+    logits = xd @ ed.t()
+    lse = torch.logsumexp(logits, 1, keepdim=True)
+    p = torch.exp(logits - lse)
+    hit = logits.gather(1, at)
+    G = p.clone()
+    G.scatter_(1, at, torch.expm1(hit - lse))
+    G[~live] = 0.0
+    want_loss = torch.where(live, (lse - hit).squeeze(1), 0.0)
+    u = unit(dtype)
+    dl = ((16 + d / 8) * u * (xd.abs() @ ed.abs().t()).amax(1, keepdim=True))
+    rel = 2 * dl + (2.0**-21 if dtype != zi.FP32 else 2.0**-48)
+    # beside the roundings to 16 bits, in absolute size: every probability by `rel` of itself, the target's by that of p
+    off_G = 1.1 * rel * p
+    off_G[~live] = 0.0
+    assert ((loss.double() - want_loss).abs() <= 2 * dl.squeeze(1) + 8 * u * (1.0 + lse.abs() + hit.abs()).squeeze(1)).all()
+    assert (loss[~live] == 0).all() and (dx[~live] == 0).all()
+    h = 0.0 if dtype == zi.FP32 else half(act_dtype(dtype))
+    tiny = 2.0**-39 if dtype == zi.FP16 else 0.0                     # half the step of probabilities below fp16's normal numbers, 2^15 times enlarged
+    for out, A, B, n in ((dx, G, ed, vocab), (de, G.t().contiguous(), xd, rows)):
+        off = off_G if out is dx else off_G.t().contiguous()
+        want = scale * (A @ B)
+        t = out.dtype
+        tol = half(t) * want.abs() + abs(scale) * (
+            7 * h * torch.sqrt(A.square() @ B.square()) + (off + tiny * (A != 0)) @ B.abs() + (24 + n / 8) * u * (A.abs() @ B.abs()))
+        assert ((out.double() - want).abs() <= 1.02 * tol + least(t)).all(), "dx" if out is dx else "de"
+
+
+SHAPES = [
+    (1, 64, 8), (1, 768, 50272), (2, 8, 16), (5, 72, 200), (20, 768, 50272), (33, 64, 520), (62, 128, 512), (64, 64, 64), (65, 200, 1000),
+    (130, 192, 4104), (257, 320, 2600), (300, 384, 8008), (513, 1024, 3000), (700, 264, 5000), (1048, 640, 6824), (2100, 128, 2056), (2049, 576, 4160),
+]
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows,d,vocab", SHAPES)
+def test_sixteen_bits(dtype, rows, d, vocab):
+    x, e, target = inputs(dtype, rows, d, vocab)
+    scale = (4096.0 if dtype == zi.FP16 else 1.0) / rows
+    check(dtype, x, e, target, scale, call(dtype, x, e, target, scale))
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(1, 1, 2), (3, 7, 11), (62, 64, 512), (65, 130, 517), (300, 96, 1001)])
+def test_fp32_parameters(rows, d, vocab):
+    x, e, target = inputs(zi.FP32, rows, d, vocab)
+    check(zi.FP32, x, e, target, 1.0 / rows, call(zi.FP32, x, e, target, 1.0 / rows))
+
+
+def test_fp32_parameters_in_pieces():
+    """More logits than a piece holds: 2^25 of them are worked at a time."""
+    rows, d, vocab = 2100, 16, 17000
+    x, e, target = inputs(zi.FP32, rows, d, vocab)
+    check(zi.FP32, x, e, target, 0.5, call(zi.FP32, x, e, target, 0.5))
+
+
+@pytest.mark.parametrize("dtype", [zi.FP32, zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows", [40, 600])
+def test_rows_that_do_not_count(dtype, rows):
+    """Whatever such a row holds, all else is as if it held zeros."""
+    d, vocab = 128, 1000
+    x, e, target = inputs(dtype, rows, d, vocab, 3)
+    target[rows // 3:rows // 2] = -1
+    target[rows - 1] = -7
+    x[target < 0] = 0.0
+    a = call(dtype, x, e, target, 0.25)
+    x[target < 0] = float("nan")
+    x[rows // 3] = float("inf")
+    b = call(dtype, x, e, target, 0.25)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    check(dtype, x, e, target, 0.25, b)
+    target[:] = -1
+    assert all((t == 0).all() for t in call(dtype, x, e, target, 0.25))
+
+
+@pytest.mark.parametrize("dtype", [zi.FP32, zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows", [9, 400])
+def test_targets_beyond_the_vocabulary(dtype, rows):
+    d, vocab = 64, 520
+    x, e, target = inputs(dtype, rows, d, vocab, 4)
+    target[4], target[5] = vocab, 5
+    loss, dx, de = call(dtype, x, e, target, 1.0)
+    assert torch.isnan(loss[4]) and torch.isnan(dx[4]).all() and torch.isnan(de).all()
+    keep = torch.arange(rows, device=DEV) != 4
+    assert torch.isfinite(loss[keep]).all() and torch.isfinite(dx[keep]).all()
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows", [12, 384])
+@pytest.mark.parametrize("size", [1.0, 50.0, 3000.0])
+def test_logits_of_all_sizes(dtype, rows, size):
+    """Rows of one word's embedding times `size`: from soft answers to ones that are certain, and certainly wrong."""
+    d, vocab = 128, 776
+    x, e, target = inputs(dtype, rows, d, vocab, 5, std=0.3)
+    word = torch.arange(rows, device=DEV) * 3 % vocab
+    x = (e[word].double() * size).to(act_dtype(dtype))
+    target[::2] = word[::2].int()                              # half the rows answer with the target
+    target[3] = -1
+    check(dtype, x, e, target, 1.0 / rows, call(dtype, x, e, target, 1.0 / rows))
+
+
+@pytest.mark.parametrize("dtype", [zi.FP32, zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows", [10, 300])
+def test_numbers_that_are_not_finite(dtype, rows):
+    """A NaN or infinite row that counts spoils its loss, its dx and de; the other rows' losses and dx stay."""
+    d, vocab = 64, 304
+    for bad in (float("nan"), float("inf")):
+        x, e, target = inputs(dtype, rows, d, vocab, 6)
+        target[2], target[3] = 17, 18
+        x[2, 5] = bad
+        loss, dx, de = call(dtype, x, e, target, 1.0)
+        keep = torch.arange(rows, device=DEV) != 2
+        assert torch.isnan(loss[2]) and torch.isnan(dx[2]).all() and torch.isnan(de).any()
+        assert torch.isfinite(loss[keep]).all() and torch.isfinite(dx[keep]).all()
+
+
+@pytest.mark.parametrize("dtype", [zi.FP32, zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows,d,vocab", [(16, 256, 4096), (520, 256, 4096)])
+def test_same_bits_every_time_on_any_stream(dtype, rows, d, vocab):
+    x, e, target = inputs(dtype, rows, d, vocab, 8)
+    first = call(dtype, x, e, target, 0.01)
+    streams = [torch.cuda.Stream(device=DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    # two calls under way at once, each with a workspace of its own, other bytes in it
+    outs = []
+    for i, s in enumerate(streams):
+        o = [Out((rows,), resid_dtype(dtype)), Out((rows, d), act_dtype(dtype)), Out((vocab, d), param_dtype(dtype))]
+        scratch = torch.full((zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab),), 0xFF * i, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        outs.append((o, scratch))
+    for s, (o, scratch) in zip(streams, outs):
+        zo_amd.zo_kernel_lmhead_grad(x, e, target, o[0].t, o[1].t, o[2].t, scratch, dtype, rows, d, vocab, 0.01, s)
+    torch.cuda.synchronize()
+    for o, _ in outs:
+        assert all(torch.equal(a.t, b) for a, b in zip(o, first))
+
+
+def test_same_word_many_times():
+    """All rows ask for one word, and all rows are alike: its gradient is the sum of as many equal shares."""
+    dtype, rows, d, vocab = zi.BF16, 333, 192, 1024
+    x, e, target = inputs(dtype, rows, d, vocab, 9)
+    target[:] = 1021
+    check(dtype, x, e, target, 1.0 / rows, call(dtype, x, e, target, 1.0 / rows))
+
+
+@pytest.mark.parametrize("dtype", [zi.FP32, zi.BF16])
+def test_against_differences(dtype):
+    """The mean loss by its own row losses in 64 bits along a direction of (x, e), at two steps: the finer central difference is off by a
+    third of what the two differ by."""
+    rows, d, vocab = 24, 64, 304
+    x, e, target = inputs(dtype, rows, d, vocab, 10)
+    live = int((target >= 0).sum())
+    _, dx, de = call(dtype, x, e, target, 1.0 / live)
+    g = generator(77)
+    vx, ve = normal((rows, d), torch.float64, g), normal((vocab, d), torch.float64, g, 0.1)
+
+    def f(t):
+        xx, ee = x.double() + t * vx, e.double() + t * ve
+        if dtype == zi.FP32:                                     # the call's own losses, at parameters of its type
+            ee32 = ee.float()
+            return call(dtype, xx, ee32, target, 1.0)[0].sum() / live
+        l = xx @ ee.t()
+        at = target.clamp(min=0).long()[:, None]
+        return torch.where(target >= 0, torch.logsumexp(l, 1) - l.gather(1, at).squeeze(1), 0.0).sum() / live
+
+    step = 2.0**-6
+    coarse, fine = ((f(s) - f(-s)) / (2 * s) for s in (step, step / 2))
+    got = (dx.double() * vx).sum() + (de.double() * ve).sum()
+    # 16-bit: the gradient's own rounding and its probabilities', two independent half steps a term; fp32: the parameters the
+    # losses were taken at are off by 2^-24 of 0.05 + step ve, a loss by as much of its slope, and that over the step
+    h = half(act_dtype(dtype)) if dtype != zi.FP32 else 2.0**-24
+    terms = torch.sqrt((dx.double() * vx).square().sum() + (de.double() * ve).square().sum())
+    off = 7 * 1.5 * h * terms
+    if dtype == zi.FP32:
+        off = off + 7 * 2.0**-24 * (e.abs().max().double() + step * ve.abs().max()) * torch.sqrt(de.double().square().sum()) / step
+    assert (got - fine).abs() <= (coarse - fine).abs() + off

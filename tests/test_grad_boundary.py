@@ -1,0 +1,72 @@
+"""The gradient calls' argument checks, on the host: nothing below touches a device."""
+import ctypes
+
+import pytest
+
+import paper_2507_03211_amd as zo_amd
+from paper_2507_03211_amd import ZO_BF16, ZO_FP16, ZO_FP32
+
+P = 4096            # an address that is aligned and never followed
+INF, NAN = float("inf"), float("nan")
+
+
+def refused(f, *args):
+    with pytest.raises(zo_amd.ZoError) as e:
+        f(*args)
+    assert e.value.status == zo_amd.ZO_EINVAL
+    return str(e.value)
+
+
+def test_layernorm():
+    good = [P, P, P, P, P, P, ZO_BF16, 4, 64, 1e-5]
+    for i in range(6):
+        assert "NULL" in refused(zo_amd.zo_kernel_layernorm, *(good[:i] + [None] + good[i + 1:]))
+    for at, value in ((6, 3), (6, -1), (7, 0), (7, -5), (8, 0), (9, 0.0), (9, -1.0), (9, NAN)):
+        refused(zo_amd.zo_kernel_layernorm, *(good[:at] + [value] + good[at + 1:]))
+
+
+def test_layernorm_grad():
+    #       dy resid gain mean rstd dresid dgain dbias scratch dtype rows d accumulate
+    good = [P, P, P, P, P, P, P, P, P, ZO_FP16, 4, 64, False]
+    f = zo_amd.zo_kernel_layernorm_grad
+    for i in (0, 1, 2, 3, 4, 8):
+        assert "NULL" in refused(f, *(good[:i] + [None] + good[i + 1:]))
+    assert "go together" in refused(f, *(good[:6] + [None] + good[7:]))
+    assert "go together" in refused(f, *(good[:7] + [None] + good[8:]))
+    assert "no output" in refused(f, P, P, P, P, P, None, None, None, P, ZO_FP16, 4, 64, False)
+    assert "aligned" in refused(f, *(good[:8] + [P + 16] + good[9:]))
+    for at, value in ((9, 5), (10, 0), (11, 0), (11, -64)):
+        refused(f, *(good[:at] + [value] + good[at + 1:]))
+    assert zo_amd.zo_kernel_layernorm_grad_scratch_bytes(ZO_BF16, 1, 1) > 0
+    for bad in ((3, 4, 64), (-1, 4, 64), (ZO_BF16, 0, 64), (ZO_BF16, 4, 0)):
+        assert zo_amd.zo_kernel_layernorm_grad_scratch_bytes(*bad) == 0
+
+
+def test_lmhead_grad():
+    #       x e target row_loss dx de scratch dtype rows d vocab scale
+    good = [P, P, P, P, P, P, P, ZO_BF16, 4, 64, 512, 1.0]
+    f = zo_amd.zo_kernel_lmhead_grad
+    for i in range(7):
+        assert "NULL" in refused(f, *(good[:i] + [None] + good[i + 1:]))
+    for at, value in ((7, 3), (8, 0), (9, 0), (10, 1), (9, 60), (10, 500), (11, INF), (11, NAN), (0, P + 2), (1, P + 8), (4, P + 2), (5, P + 8),
+                      (6, P + 128)):
+        refused(f, *(good[:at] + [value] + good[at + 1:]))
+    assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(ZO_FP32, 1, 1, 2) > 0
+    for bad in ((3, 4, 64, 512), (ZO_BF16, 0, 64, 512), (ZO_BF16, 4, 0, 512), (ZO_BF16, 4, 64, 1)):
+        assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(*bad) == 0
+
+
+def test_grad_clip():
+    #       src dst numel n dtype max_norm norm scratch
+    good = [[P, P], [P, P], [4, 4], 2, ZO_BF16, 1.0, P, P]
+    f = zo_amd.zo_kernel_grad_clip
+    for at, value in ((0, [P, None]), (1, [None, P]), (0, [P + 8, P]), (1, [P, P + 2]), (2, [4, 1 << 60]), (3, -1), (4, 3), (5, 0.0), (5, -1.0),
+                      (5, NAN), (6, None), (7, None), (6, P + 4), (7, P + 16)):
+        refused(f, *(good[:at] + [value] + good[at + 1:]))
+    L = zo_amd.lib()
+    for tables in ((None, None, None), (None, (ctypes.c_void_p * 1)(P), (ctypes.c_uint64 * 1)(4))):
+        assert L.zo_kernel_grad_clip(*tables, 1, ZO_BF16, 1.0, P, P, None) == zo_amd.ZO_EINVAL
+    with pytest.raises(ValueError):
+        f([P], [P, P], [4, 4], 2, ZO_BF16, 1.0, P, P)                       # a table shorter than n_tensors
+    with pytest.raises(TypeError):
+        f((ctypes.c_uint64 * 1)(P), [P], [4], 1, ZO_BF16, 1.0, P, P)         # an array of another type
