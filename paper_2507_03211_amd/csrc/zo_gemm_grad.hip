@@ -1,0 +1,229 @@
+// Gradient of the tied LM head and its cross entropy on the matrix cores (bf16 / fp16 parameters).
+//
+//   l = x e^T,  lse_r = log sum_v exp(l_rv),  G = exp(l - lse) - onehot(target),  dx = scale G e,  de = scale G^T x
+//
+// Four products of 2 rows vocab d flop: the logits twice, first for lse alone (the fused cross entropy of the forward pass, which leaves
+// (maximum, sum) pairs and no logits), then for G, and the two with G.  G exists one piece of the vocabulary at a time, rounded to the
+// parameters' 16-bit type because that is what the matrix instructions take: each element is off by half a step, a product's
+// sum by about as much as its own final rounding (the largest element, that of the target, is p - 1 formed in fp32).  Operands stay as
+// they lie: G, e and x are read with the contraction as the outer index where a product wants it so (zo_gemm_tiles.hip.h).
+#include "zo_gemm_tiles.hip.h"
+
+namespace zo {
+
+namespace {
+
+// ------------------------------------------------------------------ around the products
+// Rows as the products take them: x [rows, d] -> [rows_p, dp], zeros in rows that do not count (so that whatever these hold meets
+// no sum), in rows beyond the last and in columns beyond d.  Eight elements a thread.
+__global__ __launch_bounds__(256) void head_rows_kernel(const uint16_t *__restrict__ x, const int32_t *__restrict__ target, uint4 *__restrict__ out, int rows,
+                                                        int rows_p, int d, int dp)
+{
+    const int per_row = dp / 8;
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < (size_t)rows_p * per_row; i += (size_t)gridDim.x * blockDim.x) {
+        const int r = (int)(i / per_row), c = (int)(i % per_row) * 8;
+        uint4 v{0, 0, 0, 0};
+        if (r < rows && c < d && (!target || target[r] >= 0)) v = *(const uint4 *)(x + (size_t)r * d + c);
+        out[i] = v;
+    }
+}
+
+// A row's (maximum, sum) pairs -> its loss and what G takes of it: logsumexp rounded to fp32 and the exponent's share on top, which is
+// the rest of it in units of log 2 and, in fp16, the factor 2^15.  Rows that do not count: loss 0, infinity (G = 0).  One wavefront a row.
+__global__ __launch_bounds__(256) void head_lse_kernel(const float2 *__restrict__ partials, int n_partial, const float *__restrict__ target_logit,
+                                                       const int32_t *__restrict__ target, float *__restrict__ row_loss, float2 *__restrict__ stats, int rows,
+                                                       int vocab, float shift)
+{
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (r >= rows) return;
+    const int tg = target[r];
+    if (tg < 0) {
+        if (lane == 0) { row_loss[r] = 0.0f; stats[r] = float2{INFINITY, 0.0f}; }
+        return;
+    }
+    const float2 *p = partials + (size_t)r * n_partial;
+    constexpr int KEEP = 8;                                     // in registers, all under way together; the rest is read twice
+    float2 v[KEEP];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) v[i] = lane + 64 * i < n_partial ? p[lane + 64 * i] : float2{-INFINITY, 0.0f};
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) mx = v[i].x > mx ? v[i].x : mx;
+    for (int i = lane + 64 * KEEP; i < n_partial; i += 64) mx = p[i].x > mx ? p[i].x : mx;
+    mx = wave_max(mx);
+    double s = 0.0;
+    auto add = [&](float2 q) {
+        if (q.x > -INFINITY) s += (double)q.y * (double)__expf(q.x - mx);
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (64 * i < n_partial) add(v[i]);
+    for (int i = lane + 64 * KEEP; i < n_partial; i += 64) add(p[i]);
+    s = wave_sum(s);
+    if (lane != 0) return;
+    const double lse = tg < vocab ? log(s) + (double)mx : (double)__builtin_nan("");
+    const float hi = (float)lse;
+    row_loss[r] = (float)(lse - (double)target_logit[r]);
+    stats[r] = float2{hi, (float)(((double)hi - lse) * 1.4426950408889634) + shift};
+}
+
+// dx = rn(alpha sum_z part[z]): the shares of the contraction over the vocabulary, in order.  Eight elements a thread.
+template <int DT>
+__global__ __launch_bounds__(256) void head_dx_kernel(const float4 *__restrict__ part, int shares, size_t n8, float alpha, uint4 *__restrict__ dx)
+{
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n8; i += (size_t)gridDim.x * blockDim.x) {
+        float4 a = part[2 * i], b = part[2 * i + 1];
+        for (int z = 1; z < shares; ++z) {
+            const float4 p = part[2 * (z * n8 + i)], q = part[2 * (z * n8 + i) + 1];
+            a = float4{a.x + p.x, a.y + p.y, a.z + p.z, a.w + p.w};
+            b = float4{b.x + q.x, b.y + q.y, b.z + q.z, b.w + q.w};
+        }
+        auto two = [&](float lo, float hi) { return (uint32_t)Prec<DT>::acc2a(alpha * lo) | ((uint32_t)Prec<DT>::acc2a(alpha * hi) << 16); };
+        dx[i] = uint4{two(a.x, a.y), two(a.z, a.w), two(b.x, b.y), two(b.z, b.w)};
+    }
+}
+
+// ------------------------------------------------------------------ the products
+template <int DT, int EPI, class OP> hipError_t launch_product(Tile t, const Args &a, const typename OP::Arg &op)
+{
+    switch (t) {
+    case T256x256: return launch_pipe<DT, EPI, Shape<4, 4, 2>, OP>(a, op);
+    case T256x192: return launch_pipe<DT, EPI, Shape<4, 3, 2>, OP>(a, op);
+    case T256x128: return launch_pipe<DT, EPI, Shape<4, 2, 2>, OP>(a, op);
+    case T128x128: return launch_pipe<DT, EPI, Shape<2, 2, 4>, OP>(a, op);
+    default: return launch_small_t<DT, EPI, 1, false, OP>(a, op);
+    }
+}
+using Logits = Product<false, false>;       // x rows, words: both with k inside
+using ByRows = Product<true, true>;         // G^T x: contraction over the rows, outside in both
+using ByWords = Product<false, true>;       // G e: contraction over the words, outside in e
+
+constexpr Tile kProductTiles[] = {T256x256, T256x192, T256x128, T128x128, T64x64};
+Tile pick_product(int shares, int m, int n, int slabs, int epi, float *us = nullptr)
+{
+    Tile best = T64x64;
+    float best_us = 0.0f;
+    for (Tile t : kProductTiles) {
+        if (!tile_fits(t, slabs)) continue;
+        const float v = tile_us(t, shares, m, n, slabs, epi);
+        if (best_us == 0.0f || v < best_us) { best = t; best_us = v; }
+    }
+    if (us) *us = best_us;
+    return best;
+}
+
+size_t up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
+size_t larger(size_t a, size_t b) { return a > b ? a : b; }
+
+// G is held for `width` words at a time: as many as kPieceBytes hold (8192 rows: the whole of 50272 words), in `shares` shares of
+// share_words for the product with e, whose outputs [rows, d] are few tiles where rows are few.
+constexpr size_t kPieceBytes = 1u << 30;
+struct HeadPlan {
+    int rows_p, dp, width, pieces, shares, share_words, pairs;
+    Tile by_words;
+    size_t xs, es, g, stats, part, total;
+};
+HeadPlan head_plan(int rows, int d, int vocab)
+{
+    HeadPlan p{};
+    p.rows_p = (rows + BK - 1) / BK * BK;
+    p.dp = (d + BK - 1) / BK * BK;
+    const size_t fit = kPieceBytes / (2 * (size_t)p.rows_p) / BK * BK;
+    const int most = (int)(fit < (size_t)BK ? BK : fit > (size_t)vocab ? (size_t)vocab : fit);
+    const int whole = (vocab + BK - 1) / BK;                     // slabs of words
+    p.pieces = (vocab + most - 1) / most;
+    const int slabs = (whole + p.pieces - 1) / p.pieces;
+    float best = 0.0f;
+    for (int z = 1; z <= 64 && z <= slabs; z += z < 8 ? 1 : z < 16 ? 2 : 4) {
+        float us;
+        const Tile t = pick_product(z, rows, d, (slabs + z - 1) / z, 3, &us);
+        us += 4.0f + (float)z * (float)rows * (float)d * 8.0f / 4.0e6f;
+        if (best == 0.0f || us < best) { best = us; p.shares = z; p.by_words = t; }
+    }
+    p.share_words = (slabs + p.shares - 1) / p.shares * BK;
+    p.width = p.share_words * p.shares;
+    p.pieces = (vocab + p.width - 1) / p.width;
+    p.pairs = mfma_ce_partials(1, rows, vocab, p.dp);
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o = up(o + bytes); return at; };
+    p.xs = take(2 * (size_t)p.rows_p * p.dp);
+    p.es = p.dp == d ? 0 : take(2 * (size_t)vocab * p.dp);
+    p.stats = take((size_t)rows * sizeof(float2));
+    // the pairs and target logits are done with when G begins
+    p.g = take(larger(2 * (size_t)p.rows_p * p.width, up((size_t)rows * p.pairs * 8) + 4 * (size_t)rows));
+    p.part = take(4 * (size_t)p.shares * rows * d);
+    p.total = o;
+    return p;
+}
+
+template <int DT>
+hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target, float *row_loss, uint16_t *dx, uint16_t *de, char *ws, int rows, int d,
+                     int vocab, float scale, hipStream_t s)
+{
+    const HeadPlan p = head_plan(rows, d, vocab);
+    uint16_t *xs = (uint16_t *)(ws + p.xs), *g = (uint16_t *)(ws + p.g);
+    float2 *stats = (float2 *)(ws + p.stats);
+    float *part = (float *)(ws + p.part);
+    const float alpha = DT == kFP16 ? scale * 0x1p-15f : scale;
+    hipError_t err = hipSuccess;
+    auto copy = [&](const uint16_t *from, const int32_t *tg, uint16_t *to, int n, int n_p) {
+        const size_t blocks = ((size_t)n_p * (p.dp / 8) + 255) / 256;
+        head_rows_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s>>>(from, tg, (uint4 *)to, n, n_p, d, p.dp);
+        return hipGetLastError();
+    };
+    if ((err = copy(x, target, xs, rows, p.rows_p)) != hipSuccess) return err;
+    const uint16_t *w = e;                                       // words with rows of dp
+    if (p.dp != d) {
+        if ((err = copy(e, nullptr, (uint16_t *)(ws + p.es), vocab, vocab)) != hipSuccess) return err;
+        w = (const uint16_t *)(ws + p.es);
+    }
+    float *hit = (float *)(ws + p.g + up((size_t)rows * p.pairs * 8));
+    if ((err = launch_linear_mfma(xs, w, w, target, hit, g, DT, 1, rows, vocab, p.dp, 4, s)) != hipSuccess) return err;
+    head_lse_kernel<<<dim3((rows + 3) / 4), dim3(256), 0, s>>>((const float2 *)g, p.pairs, hit, target, row_loss, stats, rows, vocab,
+                                                               DT == kFP16 ? 15.0f : 0.0f);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+    for (int v0 = 0; v0 < vocab; v0 += p.width) {
+        const int words = vocab - v0 < p.width ? vocab - v0 : p.width;
+        {
+            Logits::Arg op{};
+            op.ldx = op.ldw = p.dp;
+            op.stats = stats; op.target = target; op.rows = rows; op.words = words; op.first_word = v0;
+            const Args a{xs, w + (size_t)v0 * p.dp, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
+            if ((err = launch_product<DT, 5, Logits>(pick_product(1, p.rows_p, p.width, p.dp / BK, 0), a, op)) != hipSuccess) return err;
+        }
+        {
+            ByRows::Arg op{};
+            op.ldx = p.width; op.ldw = p.dp;
+            op.x_end = (uint64_t)(uintptr_t)(g + (size_t)p.rows_p * p.width);
+            op.w_end = (uint64_t)(uintptr_t)(xs + (size_t)p.rows_p * p.dp);
+            op.alpha = alpha;
+            const Args a{g, xs, nullptr, nullptr, nullptr, de + (size_t)v0 * d, 1, words, d, p.rows_p, s};
+            if ((err = launch_product<DT, 6, ByRows>(pick_product(1, words, d, p.rows_p / BK, 0), a, op)) != hipSuccess) return err;
+        }
+        {
+            ByWords::Arg op{};
+            op.ldx = p.width; op.ldw = d;
+            op.xz = p.share_words; op.wz = (uint64_t)p.share_words * d;
+            op.w_end = (uint64_t)(uintptr_t)(e + (size_t)vocab * d);
+            const Args a{g, e + (size_t)v0 * d, nullptr, nullptr, nullptr, part, p.shares, rows, d, p.share_words, s};
+            err = v0 == 0 ? launch_product<DT, 7, ByWords>(p.by_words, a, op) : launch_product<DT, 8, ByWords>(p.by_words, a, op);
+            if (err != hipSuccess) return err;
+        }
+    }
+    const size_t n8 = (size_t)rows * d / 8, blocks = (n8 + 255) / 256;
+    head_dx_kernel<DT><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s>>>((const float4 *)part, p.shares, n8, alpha, (uint4 *)dx);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t head_grad_mfma_scratch(int rows, int d, int vocab) { return head_plan(rows, d, vocab).total; }
+
+hipError_t launch_head_grad_mfma(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype, int rows,
+                                 int d, int vocab, float scale, hipStream_t s)
+{
+    auto f = dtype == kBF16 ? head_grad<kBF16> : head_grad<kFP16>;
+    return f((const uint16_t *)x, (const uint16_t *)e, target, (float *)row_loss, (uint16_t *)dx, (uint16_t *)de, (char *)scratch, rows, d, vocab, scale, s);
+}
+
+}  // namespace zo

@@ -137,23 +137,23 @@ int dweight_run(int rows, int d)
 }
 
 // ------------------------------------------------------------------ LM head: cross entropy's gradient
-// The vocabulary is worked in pieces of `width` words whose logits [rows, width] are the only ones in memory.  RowState: per row
+// Of fp32 parameters, with fp64 activations and sums (16-bit types: zo_gemm_grad.hip).  The vocabulary is worked in pieces of
+// `width` words whose logits [rows, width] are the only ones in memory.  RowState: per row
 // the running maximum and sum of exponentials over the pieces so far, and the target's logit.
 struct RowState { double max, sum, hit; };
 
 // Takes a piece's logits into the rows' states.  `words`: how many words the piece has.
-template <typename Acc>
-__global__ __launch_bounds__(256) void head_stats_kernel(const Acc *__restrict__ logits, const int32_t *__restrict__ target, RowState *__restrict__ state,
+__global__ __launch_bounds__(256) void head_stats_kernel(const double *__restrict__ logits, const int32_t *__restrict__ target, RowState *__restrict__ state,
                                                          int words, int first_word)
 {
     __shared__ double red[16];
     const size_t r = blockIdx.x;
-    const Acc *lg = logits + r * words;
+    const double *lg = logits + r * words;
     double mx = -INFINITY;
-    for (int c = threadIdx.x; c < words; c += blockDim.x) mx = lg[c] > mx ? (double)lg[c] : mx;
+    for (int c = threadIdx.x; c < words; c += blockDim.x) mx = lg[c] > mx ? lg[c] : mx;
     mx = block_max(mx, red);
     double s = 0.0;
-    for (int c = threadIdx.x; c < words; c += blockDim.x) s += exp((double)lg[c] - mx);
+    for (int c = threadIdx.x; c < words; c += blockDim.x) s += exp(lg[c] - mx);
     s = block_sum(s, red);
     if (threadIdx.x != 0) return;
     RowState st = first_word ? state[r] : RowState{-INFINITY, 0.0, 0.0};
@@ -167,57 +167,46 @@ __global__ __launch_bounds__(256) void head_stats_kernel(const Acc *__restrict__
 
 // Logits of a piece -> G = exp(l - lse) - [word is the target], 0 in rows that do not count, NaN in those whose target lies
 // beyond the vocabulary.  `row_loss`: with one of the pieces, else null.
-template <typename Acc>
-__global__ __launch_bounds__(256) void head_probs_kernel(Acc *__restrict__ logits, const int32_t *__restrict__ target, const RowState *__restrict__ state,
-                                                         Acc *__restrict__ row_loss, int words, int first_word, int vocab)
+__global__ __launch_bounds__(256) void head_probs_kernel(double *__restrict__ logits, const int32_t *__restrict__ target, const RowState *__restrict__ state,
+                                                         double *__restrict__ row_loss, int words, int first_word, int vocab)
 {
     const size_t r = blockIdx.x;
     const int tg = target[r];
     const RowState st = state[r];
     const double nan = __builtin_nan(""), lse = tg >= vocab ? nan : st.max + log(st.sum);
-    if (row_loss && threadIdx.x == 0 && blockIdx.y == 0) row_loss[r] = (Acc)(tg < 0 ? 0.0 : lse - st.hit);
+    if (row_loss && threadIdx.x == 0 && blockIdx.y == 0) row_loss[r] = tg < 0 ? 0.0 : lse - st.hit;
     const int at = tg - first_word, c = blockIdx.y * blockDim.x + threadIdx.x;
     if (c >= words) return;
-    Acc *lg = logits + r * words + c;
-    *lg = (Acc)(tg < 0 ? 0.0 : c == at ? expm1((double)*lg - lse) : exp((double)*lg - lse));
+    double *lg = logits + r * words + c;
+    *lg = tg < 0 ? 0.0 : c == at ? expm1(*lg - lse) : exp(*lg - lse);
 }
 
-// c[i, j] (+)= scale sum_k a(i, k) b(k, j): a's element at a[i ai + k ak], b's row k at b[k ldb].  64 x 64 outputs a workgroup, 16
+// c[i, j] (+)= scale sum_k a(i, k) b(k, j): a's element at a[i ai + k ak], b's row k at b[k n].  64 x 64 outputs a workgroup, 16
 // terms a slab.  Rows of b (`live_k`) or of c (`live_i`) whose target does not count are taken as zeros, whatever they hold.
-template <int DT, bool BW, bool CW>
-__global__ __launch_bounds__(256) void head_product_kernel(const typename Prec<DT>::Acc *__restrict__ a, size_t ai, size_t ak, const void *b_, size_t ldb, void *c_,
-                                                           int m, int n, int k, float scale, int accumulate, const int32_t *__restrict__ live_k,
+template <typename TB, typename TC>
+__global__ __launch_bounds__(256) void head_product_kernel(const double *__restrict__ a, size_t ai, size_t ak, const TB *__restrict__ b, TC *__restrict__ c, int m,
+                                                           int n, int k, double scale, int accumulate, const int32_t *__restrict__ live_k,
                                                            const int32_t *__restrict__ live_i)
 {
-    using P = Prec<DT>;
-    using Acc = typename P::Acc;
-    using TB = std::conditional_t<BW, typename P::W, typename P::A>;
-    using TC = std::conditional_t<CW, typename P::W, typename P::A>;
-    const TB *b = (const TB *)b_;
     constexpr int B = 64, S = 16;
-    __shared__ Acc as[S][B + 1], bs[S][B + 1];
+    __shared__ double as[S][B + 1], bs[S][B + 1];
     const int i0 = blockIdx.y * B, j0 = blockIdx.x * B, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    Acc acc[4][4] = {};
+    double acc[4][4] = {};
     for (int k0 = 0; k0 < k; k0 += S) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int idx = threadIdx.x + 256 * e;
             // neighbouring threads along whichever index is contiguous
             const int ar = ak == 1 ? idx / S : idx % B, akk = ak == 1 ? idx % S : idx / B;
-            as[akk][ar] = k0 + akk < k && i0 + ar < m ? a[(size_t)(i0 + ar) * ai + (size_t)(k0 + akk) * ak] : (Acc)0;
+            as[akk][ar] = k0 + akk < k && i0 + ar < m ? a[(size_t)(i0 + ar) * ai + (size_t)(k0 + akk) * ak] : 0.0;
             const int bc = idx % B, bkk = idx / B;
-            Acc v = 0;
-            if (k0 + bkk < k && j0 + bc < n && (!live_k || live_k[k0 + bkk] >= 0)) {
-                const TB raw = b[(size_t)(k0 + bkk) * ldb + (j0 + bc)];
-                if constexpr (BW) v = (Acc)P::w2f(raw);
-                else v = P::a2acc(raw);
-            }
-            bs[bkk][bc] = v;
+            const bool in = k0 + bkk < k && j0 + bc < n && (!live_k || live_k[k0 + bkk] >= 0);
+            bs[bkk][bc] = in ? (double)b[(size_t)(k0 + bkk) * n + (j0 + bc)] : 0.0;
         }
         __syncthreads();
 #pragma unroll
         for (int kk = 0; kk < S; ++kk) {
-            Acc x[4], y[4];
+            double x[4], y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) { x[e] = as[kk][ty + 16 * e]; y[e] = bs[kk][tx + 16 * e]; }
 #pragma unroll
@@ -233,11 +222,9 @@ __global__ __launch_bounds__(256) void head_product_kernel(const typename Prec<D
         for (int q = 0; q < 4; ++q) {
             const int i = i0 + ty + 16 * p, j = j0 + tx + 16 * q;
             if (i >= m || j >= n) continue;
-            const size_t at = (size_t)i * n + j;
-            const Acc v = live_i && live_i[i] < 0 ? (Acc)0 : (Acc)scale * acc[p][q];
-            TC *c = (TC *)c_;
-            if constexpr (CW) c[at] = P::f2w((float)v);
-            else c[at] = accumulate ? P::acc2a(P::a2acc(c[at]) + v) : P::acc2a(v);
+            TC *at = c + (size_t)i * n + j;
+            const double v = live_i && live_i[i] < 0 ? 0.0 : scale * acc[p][q];
+            *at = (TC)(accumulate ? (double)*at + v : v);
         }
 }
 
@@ -365,44 +352,42 @@ hipError_t launch_layernorm_grad(const void *dy, const void *resid, const void *
 }
 
 namespace {
-// The fp64 head's pieces: logits of 2^25 words and rows (256 MiB) at most, 64 words at least.  16-bit types: one piece.
-int head_width(int dtype, int rows, int vocab)
+// Words of a piece: logits of 2^25 words and rows (256 MiB) at most, 64 words at least.
+int head_f64_width(int rows, int vocab)
 {
     const long w = (1l << 25) / rows / 64 * 64;
-    return dtype != kFP32 || w >= vocab ? vocab : (int)(w < 64 ? 64 : w);
+    return w >= vocab ? vocab : (int)(w < 64 ? 64 : w);
 }
+size_t head_f64_state(int rows) { return ((size_t)rows * sizeof(RowState) + 255) / 256 * 256; }
 
-template <int DT>
-hipError_t head_grad_plain(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int rows, int d,
-                           int vocab, float scale, hipStream_t s)
+hipError_t head_grad_f64(const double *x, const float *e, const int32_t *target, double *row_loss, double *dx, float *de, void *scratch, int rows, int d,
+                         int vocab, double scale, hipStream_t s)
 {
-    using P = Prec<DT>;
-    using Acc = typename P::Acc;
     RowState *state = (RowState *)scratch;
-    Acc *logits = (Acc *)((char *)scratch + ((size_t)rows * sizeof(RowState) + 255) / 256 * 256);
-    const int width = head_width(DT, rows, vocab);
+    double *logits = (double *)((char *)scratch + head_f64_state(rows));
+    const int width = head_f64_width(rows, vocab);
     auto piece = [&](int v0) { return vocab - v0 < width ? vocab - v0 : width; };
-    auto words = [&](const void *w, int v0) { return (typename P::W *)w + (size_t)v0 * d; };
     auto make_logits = [&](int v0) {
-        return launch_linear(x, words(e, v0), words(e, v0), nullptr, nullptr, logits, DT, 1, rows, piece(v0), d, 3, true, s);
+        const float *w = e + (size_t)v0 * d;
+        return launch_linear(x, w, w, nullptr, nullptr, logits, kFP32, 1, rows, piece(v0), d, 3, true, s);
     };
     hipError_t err = hipSuccess;
     for (int v0 = 0; v0 < vocab; v0 += width) {
         if ((err = make_logits(v0)) != hipSuccess) return err;
-        head_stats_kernel<Acc><<<dim3(rows), dim3(256), 0, s>>>(logits, target, state, piece(v0), v0);
+        head_stats_kernel<<<dim3(rows), dim3(256), 0, s>>>(logits, target, state, piece(v0), v0);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     for (int v0 = 0; v0 < vocab; v0 += width) {
         // (a single piece's logits are still there)
         if (width < vocab && (err = make_logits(v0)) != hipSuccess) return err;
         const int n = piece(v0);
-        head_probs_kernel<Acc><<<dim3(rows, (n + 255) / 256), dim3(256), 0, s>>>(logits, target, state, v0 == 0 ? (Acc *)row_loss : nullptr, n, v0, vocab);
+        head_probs_kernel<<<dim3(rows, (n + 255) / 256), dim3(256), 0, s>>>(logits, target, state, v0 == 0 ? row_loss : nullptr, n, v0, vocab);
         if ((err = hipGetLastError()) != hipSuccess) return err;
-        head_product_kernel<DT, true, false><<<dim3((d + 63) / 64, (rows + 63) / 64), dim3(256), 0, s>>>(
-            logits, (size_t)n, 1, words(e, v0), (size_t)d, dx, rows, d, n, scale, v0 > 0, nullptr, target);
+        head_product_kernel<float, double><<<dim3((d + 63) / 64, (rows + 63) / 64), dim3(256), 0, s>>>(
+            logits, (size_t)n, 1, e + (size_t)v0 * d, dx, rows, d, n, scale, v0 > 0, nullptr, target);
         if ((err = hipGetLastError()) != hipSuccess) return err;
-        head_product_kernel<DT, false, true><<<dim3((d + 63) / 64, (n + 63) / 64), dim3(256), 0, s>>>(
-            logits, 1, (size_t)n, x, (size_t)d, words(de, v0), n, d, rows, scale, 0, target, nullptr);
+        head_product_kernel<double, float><<<dim3((d + 63) / 64, (n + 63) / 64), dim3(256), 0, s>>>(
+            logits, 1, (size_t)n, x, de + (size_t)v0 * d, n, d, rows, scale, 0, target, nullptr);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     return hipSuccess;
@@ -411,15 +396,15 @@ hipError_t head_grad_plain(const void *x, const void *e, const int32_t *target, 
 
 size_t head_grad_scratch(int dtype, int rows, int d, int vocab)
 {
-    (void)d;
-    return ((size_t)rows * sizeof(RowState) + 255) / 256 * 256 + (size_t)rows * head_width(dtype, rows, vocab) * acc_bytes(dtype);
+    if (dtype != kFP32) return head_grad_mfma_scratch(rows, d, vocab);
+    return head_f64_state(rows) + (size_t)rows * head_f64_width(rows, vocab) * sizeof(double);
 }
 
 hipError_t launch_head_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype, int rows,
                             int d, int vocab, float scale, hipStream_t s)
 {
-    ZO_DISPATCH_DT(dtype, return (head_grad_plain<DT>(x, e, target, row_loss, dx, de, scratch, rows, d, vocab, scale, s)));
-    return hipErrorInvalidValue;
+    if (dtype != kFP32) return launch_head_grad_mfma(x, e, target, row_loss, dx, de, scratch, dtype, rows, d, vocab, scale, s);
+    return head_grad_f64((const double *)x, (const float *)e, target, (double *)row_loss, (double *)dx, (float *)de, scratch, rows, d, vocab, (double)scale, s);
 }
 
 namespace {

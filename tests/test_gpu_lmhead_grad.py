@@ -222,3 +222,11 @@ def test_against_differences(dtype):
     if dtype == zi.FP32:
         off = off + 7 * 2.0**-24 * (e.abs().max().double() + step * ve.abs().max()) * torch.sqrt(de.double().square().sum()) / step
     assert (got - fine).abs() <= (coarse - fine).abs() + off
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_sixteen_bits_in_pieces(dtype):
+    """More words than the workspace holds probabilities for at once (2^30 bytes): the later pieces' share of dx is added to the first's."""
+    rows, d, vocab = 8300, 64, 66008
+    x, e, target = inputs(dtype, rows, d, vocab, 12)
+    check(dtype, x, e, target, 1.0 / 64, call(dtype, x, e, target, 1.0 / 64))
