@@ -1407,6 +1407,7 @@ extern "C" int zo_kernel_grad_clip(const void *const *src, void *const *dst, con
         if (numel[i] == 0) continue;
         if (!src[i] || !dst[i]) return fail(ZO_EINVAL, "tensor %d is NULL", i);
         if ((uintptr_t)src[i] % 16 || (uintptr_t)dst[i] % 16) return fail(ZO_EINVAL, "tensor %d is not 16-byte aligned", i);
+        if ((uint64_t)(uintptr_t)src[i] >> 48 || (uint64_t)(uintptr_t)dst[i] >> 48) return fail(ZO_EINVAL, "tensor %d: not a device address", i);
         if (numel[i] >= 1ull << 44) return fail(ZO_EINVAL, "tensor %d has %llu elements", i, (unsigned long long)numel[i]);
     }
     ZO_HIP(launch_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, norm, scratch_mem, (hipStream_t)stream));

@@ -57,11 +57,13 @@ __global__ __launch_bounds__(256) void embed_kernel(const int32_t *__restrict__ 
 }
 
 // ------------------------------------------------------------------ LayerNorm
-// One workgroup per row; mean and (biased) variance by two passes over the row.
+// One workgroup per row; mean and (biased) variance by two passes over the row.  `stats`, if its pointers are not null (all kernels
+// here), keeps both for a backward pass.
+struct NormStats { void *mean, *rstd; };
 template <int DT>
 __global__ __launch_bounds__(256) void layernorm_kernel(const void *resid, const void *g_p, const void *g_m,
                                                         const void *b_p, const void *b_m, void *y, int m_half, int d,
-                                                        float eps)
+                                                        float eps, NormStats stats)
 {
     using P = Prec<DT>;
     using Acc = typename P::Acc;
@@ -81,6 +83,7 @@ __global__ __launch_bounds__(256) void layernorm_kernel(const void *resid, const
     Acc rstd;
     if constexpr (sizeof(Acc) == 8) rstd = 1.0 / __builtin_sqrt(var + (double)eps);
     else rstd = 1.0f / __builtin_sqrtf(var + eps);
+    if (stats.mean && threadIdx.x == 0) { ((Acc *)stats.mean)[row] = mean; ((Acc *)stats.rstd)[row] = rstd; }
     for (int c = threadIdx.x; c < d; c += blockDim.x) {
         const Acc t = ((Acc)h[c] - mean) * rstd * (Acc)P::w2f(g[c]) + (Acc)P::w2f(b[c]);
         out[c] = P::acc2a(t);
@@ -94,11 +97,11 @@ __global__ __launch_bounds__(256) void layernorm_kernel(const void *resid, const
 // gain and bias loaded with the row, 16384 rows, us before / here: d 768 14.0 / 13.3, 1024 17.9 / 15.9 (6.3 TB/s), 2048 37.0 /
 // 34.4.  As many pieces as the row has: with eight for all rows above 1024, 88 registers a lane (5 waves per SIMD) and loads of
 // pieces that are not there, 4096 rows of 1280 8.7 us / 7.5 with five, of 1536 9.8 / 8.3 with six, of 1792 10.4 / 9.5 with seven.
-template <int DT, int NV>
+template <int DT, int NV, bool STATS = false>
 __global__ __launch_bounds__(256) void layernorm_wave_kernel(const float *__restrict__ resid, const uint16_t *__restrict__ g_p,
                                                              const uint16_t *__restrict__ g_m, const uint16_t *__restrict__ b_p,
                                                              const uint16_t *__restrict__ b_m, uint16_t *__restrict__ y, int rows,
-                                                             int m_half, int d, float eps)
+                                                             int m_half, int d, float eps, NormStats stats)
 {
     using P = Prec<DT>;
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -134,6 +137,7 @@ __global__ __launch_bounds__(256) void layernorm_wave_kernel(const float *__rest
         }
     }
     const float rstd = 1.0f / __builtin_sqrtf(wave_sum(q) / (float)d + eps);
+    if (STATS && lane == 0) { ((float *)stats.mean)[row] = mean; ((float *)stats.rstd)[row] = rstd; }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = lane + 64 * i;
@@ -157,11 +161,11 @@ __global__ __launch_bounds__(256) void layernorm_wave_kernel(const float *__rest
 // wavefronts through LDS.  d % 4 == 0, d <= 1024 NV.  Measured against the wavefront-per-row kernel (8192 rows):
 // 5.4 against 4.7 TB/s at d = 4096 and 5120, 5.5 against 2.7 at 12288 (48 float4 per lane leave a SIMD two waves),
 // 5.5 against 5.9 at 2048, 4.3 against 5.6 at 1280: hence the switch at 2048.
-template <int DT, int NV>
+template <int DT, int NV, bool STATS = false>
 __global__ __launch_bounds__(256) void layernorm_block_kernel(const float *__restrict__ resid, const uint16_t *__restrict__ g_p,
                                                               const uint16_t *__restrict__ g_m, const uint16_t *__restrict__ b_p,
                                                               const uint16_t *__restrict__ b_m, uint16_t *__restrict__ y, int m_half,
-                                                              int d, float eps)
+                                                              int d, float eps, NormStats stats)
 {
     using P = Prec<DT>;
     __shared__ float red[16];
@@ -189,6 +193,7 @@ __global__ __launch_bounds__(256) void layernorm_block_kernel(const float *__res
         }
     }
     const float rstd = 1.0f / __builtin_sqrtf(block_sum(q, red) / (float)d + eps);
+    if (STATS && tid == 0) { ((float *)stats.mean)[row] = mean; ((float *)stats.rstd)[row] = rstd; }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = tid + 256 * i;
@@ -582,42 +587,63 @@ hipError_t launch_embed(const int32_t *tokens, const void *e_p, const void *e_m,
     return hipGetLastError();
 }
 
+namespace {
+template <int DT, bool STATS>
+hipError_t launch_layernorm_fast(const void *resid, const void *g_p, const void *g_m, const void *b_p, const void *b_m, void *y, int rows, int m_half,
+                                 int d, float eps, const NormStats &st, hipStream_t s)
+{
+    const dim3 wgrid((rows + 3) / 4), wblock(256);
+#define ZO_LNW(NV)                                                                                                                 \
+    layernorm_wave_kernel<DT, NV, STATS><<<wgrid, wblock, 0, s>>>((const float *)resid, (const uint16_t *)g_p, (const uint16_t *)g_m, \
+                                                                  (const uint16_t *)b_p, (const uint16_t *)b_m, (uint16_t *)y, rows,   \
+                                                                  m_half, d, eps, st)
+#define ZO_LNB(NV)                                                                                                              \
+    layernorm_block_kernel<DT, NV, STATS><<<dim3(rows), dim3(256), 0, s>>>((const float *)resid, (const uint16_t *)g_p,        \
+                                                                           (const uint16_t *)g_m, (const uint16_t *)b_p,       \
+                                                                           (const uint16_t *)b_m, (uint16_t *)y, m_half, d, eps, st)
+    switch (layernorm_pieces(d)) {
+    case 3: ZO_LNW(3); break;
+    case 4: ZO_LNW(4); break;
+    case 5: ZO_LNW(5); break;
+    case 6: ZO_LNW(6); break;
+    case 7: ZO_LNW(7); break;
+    case 8: ZO_LNW(8); break;
+    default:
+        if (d <= 4096) ZO_LNB(4);
+        else if (d <= 5120) ZO_LNB(5);
+        else if (d <= 8192) ZO_LNB(8);
+        else ZO_LNB(12);
+    }
+#undef ZO_LNB
+#undef ZO_LNW
+    return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_layernorm(const void *resid, const void *g_p, const void *g_m, const void *b_p, const void *b_m,
                             void *y, int dtype, int n_sign, int m_half, int d, float eps, hipStream_t s)
 {
     const int rows = n_sign * m_half;
     if (dtype != kFP32 && d % 4 == 0 && d <= 12288) {
-        const dim3 wgrid((rows + 3) / 4), wblock(256);
-#define ZO_LNW(DT, NV)                                                                                                        \
-    layernorm_wave_kernel<DT, NV><<<wgrid, wblock, 0, s>>>((const float *)resid, (const uint16_t *)g_p, (const uint16_t *)g_m, \
-                                                           (const uint16_t *)b_p, (const uint16_t *)b_m, (uint16_t *)y, rows,   \
-                                                           m_half, d, eps)
-#define ZO_LNB(DT, NV)                                                                                                        \
-    layernorm_block_kernel<DT, NV><<<dim3(rows), dim3(256), 0, s>>>((const float *)resid, (const uint16_t *)g_p,              \
-                                                                    (const uint16_t *)g_m, (const uint16_t *)b_p,             \
-                                                                    (const uint16_t *)b_m, (uint16_t *)y, m_half, d, eps)
-#define ZO_LNW_D(DT)                          \
-    switch (layernorm_pieces(d)) {            \
-    case 3: ZO_LNW(DT, 3); break;             \
-    case 4: ZO_LNW(DT, 4); break;             \
-    case 5: ZO_LNW(DT, 5); break;             \
-    case 6: ZO_LNW(DT, 6); break;             \
-    case 7: ZO_LNW(DT, 7); break;             \
-    case 8: ZO_LNW(DT, 8); break;             \
-    default:                                  \
-        if (d <= 4096) ZO_LNB(DT, 4);         \
-        else if (d <= 5120) ZO_LNB(DT, 5);    \
-        else if (d <= 8192) ZO_LNB(DT, 8);    \
-        else ZO_LNB(DT, 12);                  \
-    }
-        if (dtype == kBF16) { ZO_LNW_D(kBF16) } else { ZO_LNW_D(kFP16) }
-#undef ZO_LNB
-#undef ZO_LNW_D
-#undef ZO_LNW
-        return hipGetLastError();
+        auto f = dtype == kBF16 ? launch_layernorm_fast<kBF16, false> : launch_layernorm_fast<kFP16, false>;
+        return f(resid, g_p, g_m, b_p, b_m, y, rows, m_half, d, eps, NormStats{}, s);
     }
     const dim3 grid(rows), block(256);
-    ZO_DISPATCH_DT(dtype, (layernorm_kernel<DT><<<grid, block, 0, s>>>(resid, g_p, g_m, b_p, b_m, y, m_half, d, eps)));
+    ZO_DISPATCH_DT(dtype, (layernorm_kernel<DT><<<grid, block, 0, s>>>(resid, g_p, g_m, b_p, b_m, y, m_half, d, eps, NormStats{})));
+    return hipGetLastError();
+}
+
+hipError_t launch_layernorm_stats(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype, int rows, int d,
+                                  float eps, hipStream_t s)
+{
+    const NormStats st{mean, rstd};
+    // the fast kernels take rows four elements at a time
+    const bool fours = d % 4 == 0 && (uintptr_t)resid % 16 == 0 && ((uintptr_t)gain | (uintptr_t)bias | (uintptr_t)y) % 8 == 0;
+    if (dtype != kFP32 && fours && d <= 12288) {
+        auto f = dtype == kBF16 ? launch_layernorm_fast<kBF16, true> : launch_layernorm_fast<kFP16, true>;
+        return f(resid, gain, gain, bias, bias, y, rows, rows, d, eps, st, s);
+    }
+    ZO_DISPATCH_DT(dtype, (layernorm_kernel<DT><<<dim3(rows), dim3(256), 0, s>>>(resid, gain, gain, bias, bias, y, rows, d, eps, st)));
     return hipGetLastError();
 }
 

@@ -9,6 +9,8 @@ namespace zo {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 #define ZO_DISPATCH_DT(dtype, CALL)                  \
     switch (dtype) {                                 \
     case kFP32: { constexpr int DT = kFP32; CALL; } break; \
@@ -17,123 +19,275 @@ namespace {
     default: return hipErrorInvalidValue;            \
     }
 
-// ------------------------------------------------------------------ LayerNorm forward, statistics kept
-// mean = sum h / d, rstd = 1 / sqrt(sum (h - mean)^2 / d + eps), y = g (h - mean) rstd + b.  One workgroup per row.
-template <int DT>
-__global__ __launch_bounds__(256) void layernorm_stats_kernel(const void *resid, const void *gain, const void *bias, void *y, void *mean_out,
-                                                              void *rstd_out, int d, float eps)
-{
-    using P = Prec<DT>;
-    using Acc = typename P::Acc;
-    __shared__ Acc red[16];
-    const size_t row = blockIdx.x;
-    const typename P::R *h = (const typename P::R *)resid + row * d;
-    const typename P::W *g = (const typename P::W *)gain, *b = (const typename P::W *)bias;
-    typename P::A *out = (typename P::A *)y + row * d;
-    Acc s = 0;
-    for (int c = threadIdx.x; c < d; c += blockDim.x) s += (Acc)h[c];
-    const Acc mean = block_sum(s, red) / (Acc)d;
-    Acc v = 0;
-    for (int c = threadIdx.x; c < d; c += blockDim.x) { const Acc t = (Acc)h[c] - mean; v += t * t; }
-    const Acc var = block_sum(v, red) / (Acc)d;
-    Acc rstd;
-    if constexpr (sizeof(Acc) == 8) rstd = 1.0 / __builtin_sqrt(var + (double)eps);
-    else rstd = 1.0f / __builtin_sqrtf(var + eps);
-    if (threadIdx.x == 0) {
-        ((Acc *)mean_out)[row] = mean;
-        ((Acc *)rstd_out)[row] = rstd;
-    }
-    for (int c = threadIdx.x; c < d; c += blockDim.x) out[c] = P::acc2a(((Acc)h[c] - mean) * rstd * (Acc)P::w2f(g[c]) + (Acc)P::w2f(b[c]));
-}
-
 // ------------------------------------------------------------------ LayerNorm backward
 // With xh = (h - mean) rstd and a = dy g:   dh = rstd (a - mean_c(a) - xh mean_c(a xh)),
 //                                           dg = sum_r dy xh,  db = sum_r dy.
-// One workgroup per row for dh.
+// One pass over dy and h: a workgroup takes every gridDim-th row (or group of four), works dh row by row and adds up its rows' share
+// of dg and db, which it leaves in part[workgroup][2][d]; layernorm_dweight_kernel adds the workgroups' shares in order.  Bound by memory:
+// 10 bytes an element of 16-bit types.
+
+// Rows of any length and type: one workgroup a row, its share of the weights' gradient added up in `part` itself (each thread its own columns).
 template <int DT>
-__global__ __launch_bounds__(256) void layernorm_dresid_kernel(const void *dy_, const void *resid, const void *gain, const void *mean_, const void *rstd_,
-                                                               void *dresid, int d, int accumulate)
+__global__ __launch_bounds__(256) void layernorm_grad_kernel(const void *dy_, const void *resid, const void *gain, const void *mean_, const void *rstd_,
+                                                             void *dresid, void *part_, int rows, int d, bool accumulate, bool weights)
 {
     using P = Prec<DT>;
     using Acc = typename P::Acc;
     __shared__ Acc red[16];
-    const size_t row = blockIdx.x;
-    const typename P::A *dy = (const typename P::A *)dy_ + row * d;
-    const typename P::R *h = (const typename P::R *)resid + row * d;
     const typename P::W *g = (const typename P::W *)gain;
-    typename P::R *out = (typename P::R *)dresid + row * d;
-    const Acc mean = ((const Acc *)mean_)[row], rstd = ((const Acc *)rstd_)[row];
-    Acc sa = 0, sx = 0;
-    for (int c = threadIdx.x; c < d; c += blockDim.x) {
-        const Acc a = P::a2acc(dy[c]) * (Acc)P::w2f(g[c]);
-        sa += a;
-        sx += a * (((Acc)h[c] - mean) * rstd);
-    }
-    sa = block_sum(sa, red) / (Acc)d;
-    sx = block_sum(sx, red) / (Acc)d;
-    for (int c = threadIdx.x; c < d; c += blockDim.x) {
-        const Acc a = P::a2acc(dy[c]) * (Acc)P::w2f(g[c]), xh = ((Acc)h[c] - mean) * rstd;
-        const Acc v = rstd * (a - sa - xh * sx);
-        out[c] = accumulate ? out[c] + (typename P::R)v : (typename P::R)v;
+    Acc *part = (Acc *)part_ + (size_t)blockIdx.x * 2 * d;
+    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
+        const typename P::A *dy = (const typename P::A *)dy_ + (size_t)row * d;
+        const typename P::R *h = (const typename P::R *)resid + (size_t)row * d;
+        const Acc mean = ((const Acc *)mean_)[row], rstd = ((const Acc *)rstd_)[row];
+        Acc sa = 0, sx = 0;
+        for (int c = threadIdx.x; c < d; c += blockDim.x) {
+            const Acc v = P::a2acc(dy[c]), xh = ((Acc)h[c] - mean) * rstd;
+            if (dresid) {
+                const Acc a = v * (Acc)P::w2f(g[c]);
+                sa += a;
+                sx += a * xh;
+            }
+            if (weights) {
+                const bool first = row == (int)blockIdx.x;
+                part[c] = first ? v * xh : part[c] + v * xh;
+                part[d + c] = first ? v : part[d + c] + v;
+            }
+        }
+        if (!dresid) continue;
+        sa = block_sum(sa, red) / (Acc)d;
+        sx = block_sum(sx, red) / (Acc)d;
+        typename P::R *out = (typename P::R *)dresid + (size_t)row * d;
+        for (int c = threadIdx.x; c < d; c += blockDim.x) {
+            const Acc a = P::a2acc(dy[c]) * (Acc)P::w2f(g[c]), xh = ((Acc)h[c] - mean) * rstd;
+            const Acc v = rstd * (a - sa - xh * sx);
+            out[c] = (typename P::R)(accumulate ? out[c] + v : v);
+        }
     }
 }
 
-// Gain's and bias's gradient: workgroup (x, y) adds up 64 columns over the y-th run of `run` rows, four rows at a time, and
-// leaves its two sums in part[y]; layernorm_dweight_finish_kernel adds the runs in order.
+__device__ __forceinline__ float fused(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ __forceinline__ double fused(double a, double b, double c) { return __builtin_fma(a, b, c); }
+
+// Rows in registers: NV pieces of VW elements a lane, WPR wavefronts a row (one: four rows at a time).  VW = 4 where rows of 16-bit types
+// are a multiple of four elements long and buffers aligned, else 1.  The next row is on its way while one is worked; gain and the weights'
+// sums stay in registers throughout.  One workgroup a CU is enough: us with 256 / 512 of them, bf16, launch of the sums below included,
+// 8192 rows of 768 19.3 / 19.3, of 1536 30.0 / 31.9, 4096 60.8 / 69, 5120 79.2 / 86 (floor 81.9 at the copy rate, which leaves the
+// memory-side cache out), 12288 195 / 204; 2048 is the exception, 39.5 / 37.6.  Wavefronts a row, the best number of pieces of each: 1536
+// columns 30.0 (1) / 32.6 (2) / 32.4 (4), 2048 37.6 / 37.1 / 37.6, where 8 pieces and one wavefront take 314 registers, and 1003 rows
+// 12.0 / 11.8 / 11.4; 5120 79.2 (4) / 84.8 (8).  Element by element, 4096 rows of 1101 25 us, of 2603 39.8, of 4802 52.6 (46 - 102 - 178 with
+// the kernel for any length).
+template <int DT, int NV, int WPR, int VW>
+__global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void layernorm_grad_rows_kernel(
+    const typename Prec<DT>::A *__restrict__ dy, const typename Prec<DT>::R *__restrict__ resid, const typename Prec<DT>::W *__restrict__ gain,
+    const typename Prec<DT>::Acc *__restrict__ mean_, const typename Prec<DT>::Acc *__restrict__ rstd_, typename Prec<DT>::R *__restrict__ dresid,
+    typename Prec<DT>::Acc *__restrict__ part, int rows, int d, bool accumulate, bool weights)
+{
+    using P = Prec<DT>;
+    using Acc = typename P::Acc;                                // the residual stream's type too
+    static_assert(std::is_same_v<Acc, typename P::R>, "");
+    typedef typename P::A act_t __attribute__((ext_vector_type(VW)));
+    typedef typename P::W gain_t __attribute__((ext_vector_type(VW)));
+    typedef Acc acc_t __attribute__((ext_vector_type(VW)));
+    struct Pair { Acc a, x; };
+    constexpr int LANES = 64 * WPR, RPB = WPR == 1 ? 4 : 1;     // lanes a row, rows at a time
+    __shared__ Pair sums[2][WPR];
+    extern __shared__ __attribute__((aligned(16))) char shared_raw[];   // WPR == 1: [2][d], the four wavefronts' sums
+    const int tid = threadIdx.x, lane = tid % LANES, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int nvec = d / VW, step = (int)gridDim.x * RPB;
+    const Acc inv_d = (Acc)1 / (Acc)d;
+    auto inside = [&](int i) { return lane + LANES * i < nvec; };
+    auto col = [&](int i) { return inside(i) ? lane + LANES * i : nvec - 1; };
+    gain_t gv[NV];
+    acc_t dg[NV] = {}, db[NV] = {};
+    if (dresid) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) gv[i] = ((const gain_t *)gain)[col(i)];
+    }
+    struct Row { acc_t h[NV]; act_t dy[NV]; Acc mean, rstd; };
+    auto load = [&](int row, Row &r) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) r.dy[i] = ((const act_t *)(dy + (size_t)row * d))[col(i)];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) r.h[i] = ((const acc_t *)(resid + (size_t)row * d))[col(i)];
+        r.mean = mean_[row];
+        r.rstd = rstd_[row];
+    };
+    int row = (int)blockIdx.x * RPB + (WPR == 1 ? wave : 0);
+    Row cur, nxt;
+    if (row < rows) load(row, cur);
+    for (int turn = 0; row < rows; row += step, turn ^= 1) {
+        const int next = row + step;
+        if (next < rows) load(next, nxt);
+        Acc sa = 0, sx = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+                const Acc v = inside(i) ? P::a2acc(cur.dy[i][e]) : (Acc)0;
+                const Acc xh = (cur.h[i][e] - cur.mean) * cur.rstd, a = v * (Acc)P::w2f(gv[i][e]);
+                sa += a;
+                sx = fused(a, xh, sx);
+                dg[i][e] = fused(v, xh, dg[i][e]);
+                db[i][e] += v;
+            }
+        }
+        if (dresid) {
+            sa = wave_sum(sa);
+            sx = wave_sum(sx);
+            if constexpr (WPR > 1) {                            // two sets of slots: a wavefront may be a row ahead of its neighbours
+                if ((tid & 63) == 0) sums[turn][wave] = Pair{sa, sx};
+                __syncthreads();
+                sa = sx = 0;
+#pragma unroll
+                for (int w = 0; w < WPR; ++w) { sa += sums[turn][w].a; sx += sums[turn][w].x; }
+            }
+            sa *= inv_d;
+            sx *= inv_d;
+            acc_t *out = (acc_t *)(dresid + (size_t)row * d);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                acc_t o;
+#pragma unroll
+                for (int e = 0; e < VW; ++e)
+                    o[e] = cur.rstd * (fused(P::a2acc(cur.dy[i][e]), (Acc)P::w2f(gv[i][e]), -sa) - (cur.h[i][e] - cur.mean) * cur.rstd * sx);
+                if (inside(i)) {
+                    acc_t *at = out + lane + LANES * i;
+                    if (accumulate) {
+                        const acc_t before = *at;
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) o[e] += before[e];
+                    }
+                    *at = o;
+                }
+            }
+        }
+        cur = nxt;
+    }
+    if (!weights) return;
+    part += (size_t)blockIdx.x * 2 * d;
+    acc_t *pg = (acc_t *)part, *pb = (acc_t *)(part + d);
+    if constexpr (WPR > 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (inside(i)) { pg[lane + LANES * i] = dg[i]; pb[lane + LANES * i] = db[i]; }
+    } else {
+        // the wavefronts add theirs one after the other, the last one writes
+        acc_t *sg = (acc_t *)shared_raw, *sb = (acc_t *)((Acc *)shared_raw + d);
+        for (int w = 0; w < 4; ++w) {
+            if (wave == w) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (!inside(i)) continue;
+                    const int c = lane + LANES * i;
+                    acc_t a = dg[i], b = db[i];
+                    if (w > 0) {
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) { a[e] += sg[c][e]; b[e] += sb[c][e]; }
+                    }
+                    (w < 3 ? sg : pg)[c] = a;
+                    (w < 3 ? sb : pb)[c] = b;
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Few rows, of any length and type, in one launch: the first `rows` workgroups work a row's dh each, the others 32 columns of dg and db
+// each, eight rows at a time.  dy and h are read twice, which is nothing next to a second launch.
 template <int DT>
-__global__ __launch_bounds__(256) void layernorm_dweight_kernel(const void *dy_, const void *resid, const void *mean_, const void *rstd_, void *part_,
-                                                                int rows, int d, int run)
+__global__ __launch_bounds__(256) void layernorm_grad_few_kernel(const void *dy_, const void *resid, const void *gain, const void *mean_, const void *rstd_,
+                                                                 void *dresid, void *dgain, void *dbias, int rows, int d, bool accumulate, int row_blocks)
 {
     using P = Prec<DT>;
     using Acc = typename P::Acc;
-    __shared__ Acc red[2][4][64];
-    const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-    const int first = blockIdx.y * run, last = first + run < rows ? first + run : rows;
+    __shared__ Acc red[16];
+    __shared__ Acc cols[2][8][32];
+    if ((int)blockIdx.x < row_blocks) {
+        const size_t row = blockIdx.x;
+        const typename P::A *dy = (const typename P::A *)dy_ + row * d;
+        const typename P::R *h = (const typename P::R *)resid + row * d;
+        const typename P::W *g = (const typename P::W *)gain;
+        const Acc mean = ((const Acc *)mean_)[row], rstd = ((const Acc *)rstd_)[row];
+        Acc sa = 0, sx = 0;
+#pragma unroll 4
+        for (int c = threadIdx.x; c < d; c += 256) {
+            const Acc a = P::a2acc(dy[c]) * (Acc)P::w2f(g[c]);
+            sa += a;
+            sx += a * (((Acc)h[c] - mean) * rstd);
+        }
+        sa = block_sum(sa, red) / (Acc)d;
+        sx = block_sum(sx, red) / (Acc)d;
+        typename P::R *out = (typename P::R *)dresid + row * d;
+#pragma unroll 4
+        for (int c = threadIdx.x; c < d; c += 256) {
+            const Acc a = P::a2acc(dy[c]) * (Acc)P::w2f(g[c]), xh = ((Acc)h[c] - mean) * rstd;
+            const Acc v = rstd * (a - sa - xh * sx);
+            out[c] = (typename P::R)(accumulate ? out[c] + v : v);
+        }
+        return;
+    }
+    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5, c = ((int)blockIdx.x - row_blocks) * 32 + lane;
     Acc dg = 0, db = 0;
     if (c < d) {
-        for (int r = first + sub; r < last; r += 4) {
+#pragma unroll 4
+        for (int r = sub; r < rows; r += 8) {
             const Acc v = P::a2acc(((const typename P::A *)dy_)[(size_t)r * d + c]);
             const Acc xh = ((Acc)((const typename P::R *)resid)[(size_t)r * d + c] - ((const Acc *)mean_)[r]) * ((const Acc *)rstd_)[r];
             dg += v * xh;
             db += v;
         }
     }
-    red[0][sub][lane] = dg;
-    red[1][sub][lane] = db;
+    cols[0][sub][lane] = dg;
+    cols[1][sub][lane] = db;
     __syncthreads();
-    if (sub == 0 && c < d) {
-        Acc *part = (Acc *)part_ + (size_t)blockIdx.y * 2 * d;
-        part[c] = (red[0][0][lane] + red[0][1][lane]) + (red[0][2][lane] + red[0][3][lane]);
-        part[d + c] = (red[1][0][lane] + red[1][1][lane]) + (red[1][2][lane] + red[1][3][lane]);
+    if (sub < 2 && c < d) {
+        Acc v = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += cols[sub][k][lane];
+        ((typename P::W *)(sub ? dbias : dgain))[c] = P::f2w((float)v);
     }
 }
 
+// The workgroups' shares -> dg and db.  64 columns a workgroup, its sixteen wavefronts every sixteenth share each.
 template <int DT>
-__global__ __launch_bounds__(256) void layernorm_dweight_finish_kernel(const void *part_, void *dgain, void *dbias, int d, int runs)
+__global__ __launch_bounds__(1024) void layernorm_dweight_kernel(const void *part_, void *dgain, void *dbias, int d, int shares)
 {
     using P = Prec<DT>;
     using Acc = typename P::Acc;
-    __shared__ Acc red[4][64];
+    __shared__ Acc red[16][64];
     const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     Acc s = 0;
-    if (c < 2 * d)
-        for (int r = sub; r < runs; r += 4) s += ((const Acc *)part_)[(size_t)r * 2 * d + c];
+    if (c < 2 * d) {
+#pragma unroll 4
+        for (int r = sub; r < shares; r += 16) s += ((const Acc *)part_)[(size_t)r * 2 * d + c];
+    }
     red[sub][lane] = s;
     __syncthreads();
     if (sub == 0 && c < 2 * d) {
-        const Acc v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+        Acc v = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v += red[k][lane];
         ((typename P::W *)(c < d ? dgain : dbias))[c < d ? c : c - d] = P::f2w((float)v);
     }
 }
 
-// Rows per run of the weights' sums: so many runs that their workgroups fill the chip, 64 rows at least.
-int dweight_run(int rows, int d)
+// Which rows go through registers: up to 12288 elements by fours, 8192 (24 elements a lane spill) 16-bit ones and 4096 fp64 ones one by one.
+bool norm_grad_in_registers(int dtype, int d, bool fours) { return d <= (dtype == kFP32 ? 4096 : fours ? 12288 : 8192); }
+
+// Few rows take one launch.  us, one launch / two: 256 rows of 768 5.2 / 7.7, of 5120 8.8 / 10.2, 400 rows of 2048 8.6 / 8.4; rows of 12288
+// are slow one by one, 64 of them 14.6 / 10.1, 256 23.8 / 16.2, of 8101 18.3 / 14.7.
+bool norm_grad_few(int dtype, int rows, int d) { return rows <= 256 && (d <= 5120 || !norm_grad_in_registers(dtype, d, d % 4 == 0)); }
+
+// How many workgroups a backward pass over many rows has, each with a share of the weights' gradient: one a CU, and two rows (eight, where
+// wavefronts have rows of their own) for each at least.  The kernel for any length, where a row is a workgroup's whole latency: one row, 1024
+// at most (4096 rows of 2603, 256 / 512 / 1024 workgroups 205 / 143 / 102 us).
+int norm_grad_shares(int dtype, int rows, int d)
 {
-    const int columns = (d + 63) / 64;
-    int runs = (2048 + columns - 1) / columns;
-    runs = runs < 1 ? 1 : runs;
-    const int run = (rows + runs - 1) / runs;
-    return run < 64 ? 64 : run;
+    const bool registers = norm_grad_in_registers(dtype, d, d % 4 == 0);
+    const int each = !registers ? 1 : d <= 1536 ? 8 : 2, most = registers ? 256 : 1024, n = (rows + each - 1) / each;
+    return n < most ? n : most;
 }
 
 // ------------------------------------------------------------------ LM head: cross entropy's gradient
@@ -229,29 +383,50 @@ __global__ __launch_bounds__(256) void head_product_kernel(const double *__restr
 }
 
 // ------------------------------------------------------------------ global norm and clipping
-// The tensor of chunk `c`: lanes compare the table's first chunks side by side.  All lanes return the same.
-__device__ __forceinline__ int clip_tensor(const ClipBatch &b, uint32_t c)
+// Chunk c of a batch: its tensor (found by the lanes side by side), where it starts and its elements.
+struct ClipPlace { uint64_t src, dst; size_t at; uint32_t n; };
+template <typename W> __device__ __forceinline__ ClipPlace clip_place(const ClipBatch &b, uint32_t c)
 {
     const int lane = threadIdx.x & 63;
-    int t = 0;
-    for (int i = 0; i < b.n; i += 64) t += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < b.n && b.d[i + lane].first <= c));
-    return __builtin_amdgcn_readfirstlane(t - 1);
+    int t = -1;
+    for (int i = 0; i < b.n; i += 64) t += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < b.n && b.first[i + lane] <= c));
+    t = __builtin_amdgcn_readfirstlane(t);
+    const uint64_t src = b.src[t];
+    const uint32_t end = t + 1 < b.n ? b.first[t + 1] : b.chunks;
+    return {src & 0xffffffffffffull, b.dst[t], (size_t)(c - b.first[t]) * kClipChunk, c + 1 == end ? (uint32_t)(src >> 48) + 1 : kClipChunk};
 }
 
-template <int DT> __device__ __forceinline__ void clip_load(const void *src, uint32_t n, uint32_t i, float (&v)[16 / sizeof(typename Prec<DT>::W)])
+// f(element, the 16 bytes that start there) over a chunk of n elements, what lies past its end as zeros; in a whole chunk kClipAhead pieces a
+// thread are under way together.
+constexpr int kClipAhead = 8;
+template <typename W, class F> __device__ __forceinline__ void clip_chunk(const W *src, uint32_t n, F &&f)
 {
-    using W = typename Prec<DT>::W;
-    constexpr int E = 16 / sizeof(W);
-    const W *p = (const W *)src + i;
-    if (i + E <= n) {
-        W w[E];
-        *(uint4 *)w = *(const uint4 *)p;
+    constexpr uint32_t E = 16 / sizeof(W), STEP = 256 * E;
+    static_assert(kClipChunk % (kClipAhead * STEP) == 0, "a chunk is whole bursts");
+    if (n == kClipChunk) {
+        for (uint32_t i0 = 0; i0 < kClipChunk; i0 += kClipAhead * STEP) {
+            uint4 v[kClipAhead];
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = Prec<DT>::w2f(w[e]);
-    } else {
+            for (int k = 0; k < kClipAhead; ++k) v[k] = *(const uint4 *)(src + i0 + k * STEP + threadIdx.x * E);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = i + e < n ? Prec<DT>::w2f(p[e]) : 0.0f;
+            for (int k = 0; k < kClipAhead; ++k) f(i0 + k * STEP + threadIdx.x * E, v[k]);
+        }
+        return;
     }
+    for (uint32_t i = threadIdx.x * E; i < n; i += STEP) {
+        union { uint4 v; W w[E]; } u;
+        if (i + E <= n) u.v = *(const uint4 *)(src + i);
+        else
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) u.w[e] = i + e < n ? src[i + e] : (W)0;
+        f(i, u.v);
+    }
+}
+template <typename W> __device__ __forceinline__ W clip_element(const uint4 &v, int e)
+{
+    const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (sizeof(W) == 4) return __uint_as_float(words[e]);
+    else return (W)(e & 1 ? words[e / 2] >> 16 : words[e / 2] & 0xffff);
 }
 
 // sum g^2 of a batch of tensors, one partial sum per workgroup, in fp64: no square of an fp32 number leaves its range, and the
@@ -259,27 +434,28 @@ template <int DT> __device__ __forceinline__ void clip_load(const void *src, uin
 template <int DT>
 __global__ __launch_bounds__(256) void grad_norm_kernel(ClipBatch b, double *__restrict__ part, int seen)
 {
+    using W = typename Prec<DT>::W;
     __shared__ double red[16];
-    constexpr int E = 16 / sizeof(typename Prec<DT>::W);
-    double s = 0.0;
+    constexpr int E = 16 / sizeof(W);
+    double s[4] = {0.0, 0.0, 0.0, 0.0};                         // side by side: a chain of one would wait for each fma
     for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
-        const ClipDesc &t = b.d[clip_tensor(b, c)];
-        const uint32_t local = c - t.first, n = local + 1 == t.chunks ? t.last : kClipChunk;
-        const void *src = (const typename Prec<DT>::W *)t.src + (size_t)local * kClipChunk;
-        for (uint32_t i = threadIdx.x * E; i < n; i += blockDim.x * E) {
-            float v[E];
-            clip_load<DT>(src, n, i, v);
+        const ClipPlace t = clip_place<W>(b, c);
+        clip_chunk((const W *)t.src + t.at, t.n, [&](uint32_t, const uint4 &v) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
-        }
+            for (int e = 0; e < E; ++e) {
+                const double g = (double)Prec<DT>::w2f(clip_element<W>(v, e));
+                s[e & 3] = __builtin_fma(g, g, s[e & 3]);
+            }
+        });
     }
-    s = block_sum(s, red);
-    if (threadIdx.x == 0) part[blockIdx.x] = (int)blockIdx.x < seen ? part[blockIdx.x] + s : s;
+    const double sum = block_sum((s[0] + s[1]) + (s[2] + s[3]), red);
+    if (threadIdx.x == 0) part[blockIdx.x] = (int)blockIdx.x < seen ? part[blockIdx.x] + sum : sum;
 }
 
 // dst = rn(c src), c = max / norm where norm exceeds max, else 1; where the norm is not a finite number, zeros.  Every workgroup adds up the
-// partial sums itself, in the same order.  The chunks are taken from the last one down: those read last are the ones still in the
-// memory-side cache.
+// partial sums itself, in the same order.  Gradients of up to the memory-side cache's 256 MiB are found there the second time: stores past it
+// leave them there (125 M bf16 gradients into another buffer 122 us, 150 with plain stores; from the last chunk down 122).  117 us with
+// one launch a pass (501 MB that must move, 98 us at the copy rate), where tables of 124 tensors took two.
 template <int DT>
 __global__ __launch_bounds__(256) void grad_scale_kernel(ClipBatch b, const double *__restrict__ part, int n_part, float max_norm, double *__restrict__ out, bool write_norm)
 {
@@ -293,61 +469,106 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(ClipBatch b, const doub
     const bool finite = norm - norm == 0.0;
     const double coef = !finite ? 0.0 : norm > (double)max_norm ? (double)max_norm / norm : 1.0;
     if (write_norm && blockIdx.x == 0 && threadIdx.x == 0) { out[0] = norm; out[1] = coef; }
-    for (uint32_t c0 = blockIdx.x; c0 < b.chunks; c0 += gridDim.x) {
-        const uint32_t c = b.chunks - 1 - c0;
-        const ClipDesc &t = b.d[clip_tensor(b, c)];
+    for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
+        const ClipPlace t = clip_place<W>(b, c);
         if (coef == 1.0 && t.dst == t.src) continue;
-        const uint32_t local = c - t.first, n = local + 1 == t.chunks ? t.last : kClipChunk;
-        const void *src = (const W *)t.src + (size_t)local * kClipChunk;
-        W *dst = (W *)t.dst + (size_t)local * kClipChunk;
-        for (uint32_t i = threadIdx.x * E; i < n; i += blockDim.x * E) {
-            float v[E];
-            clip_load<DT>(src, n, i, v);
-            W w[E];
+        const uint32_t n = t.n;
+        W *dst = (W *)t.dst + t.at;
+        clip_chunk((const W *)t.src + t.at, n, [&](uint32_t i, const uint4 &v) {
+            union { u32x4 v; W w[E]; } o;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
+                const float g = P::w2f(clip_element<W>(v, e));
                 // fp32: the product in fp64, rounded once.  16-bit types: the fp32 product's rounding is 2^-13 of theirs and less
-                if constexpr (DT == kFP32) w[e] = finite ? (float)(coef * (double)v[e]) : 0.0f;
-                else w[e] = P::f2w(finite ? (float)coef * v[e] : 0.0f);
+                if constexpr (DT == kFP32) o.w[e] = finite ? (float)(coef * (double)g) : 0.0f;
+                else o.w[e] = P::f2w(finite ? (float)coef * g : 0.0f);
             }
-            if (i + E <= n) *(uint4 *)(dst + i) = *(uint4 *)w;
+            if (i + E <= n) __builtin_nontemporal_store(o.v, (u32x4 *)(dst + i));
             else
                 for (int e = 0; e < E; ++e)
-                    if (i + e < n) dst[i + e] = w[e];
-        }
+                    if (i + e < n) dst[i + e] = o.w[e];
+        });
     }
 }
 
 }  // namespace
 
 // ------------------------------------------------------------------ launchers
-hipError_t launch_layernorm_stats(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype, int rows, int d,
-                                  float eps, hipStream_t s)
+
+namespace {
+struct NormGrad {
+    const void *dy, *resid, *gain, *mean, *rstd;
+    void *dresid, *part;
+    int rows, d;
+    bool accumulate, weights;
+};
+template <int DT, int NV, int WPR, int VW = 4> void norm_grad_rows(const NormGrad &a, int shares, hipStream_t s)
 {
-    ZO_DISPATCH_DT(dtype, (layernorm_stats_kernel<DT><<<dim3(rows), dim3(256), 0, s>>>(resid, gain, bias, y, mean, rstd, d, eps)));
-    return hipGetLastError();
+    using P = Prec<DT>;
+    using Acc = typename P::Acc;
+    layernorm_grad_rows_kernel<DT, NV, WPR, VW><<<dim3(shares), dim3(WPR == 1 ? 256 : 64 * WPR), WPR == 1 ? 2 * a.d * sizeof(Acc) : 0, s>>>(
+        (const typename P::A *)a.dy, (const typename P::R *)a.resid, (const typename P::W *)a.gain, (const Acc *)a.mean, (const Acc *)a.rstd,
+        (typename P::R *)a.dresid, (Acc *)a.part, a.rows, a.d, a.accumulate, a.weights);
 }
+template <int DT> void norm_grad(const NormGrad &a, int shares, hipStream_t s)
+{
+    const bool fours = DT != kFP32 && a.d % 4 == 0 && ((uintptr_t)a.resid | (uintptr_t)a.dresid) % 16 == 0 && ((uintptr_t)a.dy | (uintptr_t)a.gain) % 8 == 0;
+    if (!norm_grad_in_registers(DT, a.d, fours)) {
+        layernorm_grad_kernel<DT><<<dim3(shares), dim3(256), 0, s>>>(a.dy, a.resid, a.gain, a.mean, a.rstd, a.dresid, a.part, a.rows, a.d, a.accumulate,
+                                                                    a.weights);
+        return;
+    }
+    if constexpr (DT != kFP32) {
+        if (fours && a.d <= 1536) {
+            switch ((a.d + 255) / 256) {
+            case 1: return norm_grad_rows<DT, 1, 1>(a, shares, s);
+            case 2: return norm_grad_rows<DT, 2, 1>(a, shares, s);
+            case 3: return norm_grad_rows<DT, 3, 1>(a, shares, s);
+            case 4: return norm_grad_rows<DT, 4, 1>(a, shares, s);
+            case 5: return norm_grad_rows<DT, 5, 1>(a, shares, s);
+            default: return norm_grad_rows<DT, 6, 1>(a, shares, s);
+            }
+        }
+        if (fours && a.d <= 5120) {
+            switch ((a.d + 1023) / 1024) {
+            case 2: return norm_grad_rows<DT, 2, 4>(a, shares, s);
+            case 3: return norm_grad_rows<DT, 3, 4>(a, shares, s);
+            case 4: return norm_grad_rows<DT, 4, 4>(a, shares, s);
+            default: return norm_grad_rows<DT, 5, 4>(a, shares, s);
+            }
+        }
+        if (fours && a.d <= 8192) return norm_grad_rows<DT, 4, 8>(a, shares, s);
+        if (fours) return norm_grad_rows<DT, 6, 8>(a, shares, s);
+        if (a.d > 4096) return norm_grad_rows<DT, 16, 8, 1>(a, shares, s);
+        if (a.d > 2048) return norm_grad_rows<DT, 16, 4, 1>(a, shares, s);
+    } else if (a.d > 2048) {
+        return norm_grad_rows<DT, 8, 8, 1>(a, shares, s);
+    }
+    if (a.d > 512) return norm_grad_rows<DT, 8, 4, 1>(a, shares, s);
+    norm_grad_rows<DT, 8, 1, 1>(a, shares, s);
+}
+}  // namespace
 
 size_t layernorm_grad_scratch(int dtype, int rows, int d)
 {
-    const int run = dweight_run(rows, d);
-    return (size_t)((rows + run - 1) / run) * 2 * d * acc_bytes(dtype);
+    return norm_grad_few(dtype, rows, d) ? 256 : (size_t)norm_grad_shares(dtype, rows, d) * 2 * d * acc_bytes(dtype);
 }
 
 hipError_t launch_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid, void *dgain,
                                  void *dbias, void *scratch, int dtype, int rows, int d, bool accumulate, hipStream_t s)
 {
-    if (dresid) {
-        ZO_DISPATCH_DT(dtype, (layernorm_dresid_kernel<DT><<<dim3(rows), dim3(256), 0, s>>>(dy, resid, gain, mean, rstd, dresid, d, accumulate)));
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    if (norm_grad_few(dtype, rows, d)) {
+        const int row_blocks = dresid ? rows : 0, blocks = row_blocks + (dgain ? (d + 31) / 32 : 0);
+        ZO_DISPATCH_DT(dtype, (layernorm_grad_few_kernel<DT><<<dim3(blocks), dim3(256), 0, s>>>(dy, resid, gain, mean, rstd, dresid, dgain, dbias, rows, d,
+                                                                                               accumulate, row_blocks)));
+        return hipGetLastError();
     }
-    if (!dgain) return hipSuccess;
-    const int run = dweight_run(rows, d), runs = (rows + run - 1) / run;
-    ZO_DISPATCH_DT(dtype, (layernorm_dweight_kernel<DT><<<dim3((d + 63) / 64, runs), dim3(256), 0, s>>>(dy, resid, mean, rstd, scratch, rows, d, run)));
+    const NormGrad a{dy, resid, gain, mean, rstd, dresid, scratch, rows, d, accumulate, dgain != nullptr};
+    const int shares = norm_grad_shares(dtype, rows, d);
+    ZO_DISPATCH_DT(dtype, norm_grad<DT>(a, shares, s));
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    ZO_DISPATCH_DT(dtype, (layernorm_dweight_finish_kernel<DT><<<dim3((2 * d + 63) / 64), dim3(256), 0, s>>>(scratch, dgain, dbias, d, runs)));
+    if (e != hipSuccess || !dgain) return e;
+    ZO_DISPATCH_DT(dtype, (layernorm_dweight_kernel<DT><<<dim3((2 * d + 63) / 64), dim3(1024), 0, s>>>(scratch, dgain, dbias, d, shares)));
     return hipGetLastError();
 }
 
@@ -408,27 +629,29 @@ hipError_t launch_head_grad(const void *x, const void *e, const int32_t *target,
 }
 
 namespace {
-template <class F> hipError_t clip_batches(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, bool backwards, F &&f)
+template <class F> hipError_t clip_batches(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, F &&f)
 {
     // tensors of a batch: as many as its table holds, and chunk numbers of 31 bits
     ClipBatch b{};
-    hipError_t err = hipSuccess;
-    bool any = false;
+    bool first = true;
     auto flush = [&] {
         if (b.n == 0) return hipSuccess;
-        const hipError_t e = f(b, any);
-        any = true;
+        const hipError_t e = f(b, first);
+        first = false;
         b.n = 0;
         b.chunks = 0;
         return e;
     };
-    for (int j = 0; j < n_tensors; ++j) {
-        const int i = backwards ? n_tensors - 1 - j : j;
+    for (int i = 0; i < n_tensors; ++i) {
         if (numel[i] == 0) continue;
         const uint64_t chunks = (numel[i] + kClipChunk - 1) / kClipChunk;
-        if (b.n == kClipMax || b.chunks + chunks >= (1ull << 31))
-            if ((err = flush()) != hipSuccess) return err;
-        b.d[b.n++] = ClipDesc{src[i], dst ? dst[i] : nullptr, b.chunks, (uint32_t)chunks, (uint32_t)(numel[i] - (chunks - 1) * kClipChunk), 0};
+        if (b.n == kClipMax || b.chunks + chunks >= (1ull << 31)) {
+            const hipError_t e = flush();
+            if (e != hipSuccess) return e;
+        }
+        b.src[b.n] = (uint64_t)(uintptr_t)src[i] | (numel[i] - (chunks - 1) * kClipChunk - 1) << 48;
+        b.dst[b.n] = (uint64_t)(uintptr_t)dst[i];
+        b.first[b.n++] = b.chunks;
         b.chunks += (uint32_t)chunks;
     }
     return flush();
@@ -440,7 +663,7 @@ hipError_t launch_grad_clip(const void *const *src, void *const *dst, const uint
 {
     double *part = (double *)scratch;
     int slots = 0;
-    hipError_t err = clip_batches(src, nullptr, numel, n_tensors, false, [&](const ClipBatch &b, bool) {
+    hipError_t err = clip_batches(src, dst, numel, n_tensors, [&](const ClipBatch &b, bool) {
         const int grid = (int)(b.chunks < kClipSlots ? b.chunks : kClipSlots);
         ZO_DISPATCH_DT(dtype, (grad_norm_kernel<DT><<<dim3(grid), dim3(256), 0, s>>>(b, part, slots)));
         slots = grid > slots ? grid : slots;
@@ -448,9 +671,9 @@ hipError_t launch_grad_clip(const void *const *src, void *const *dst, const uint
     });
     if (err != hipSuccess) return err;
     bool done = false;
-    err = clip_batches(src, dst, numel, n_tensors, true, [&](const ClipBatch &b, bool later) {
+    err = clip_batches(src, dst, numel, n_tensors, [&](const ClipBatch &b, bool first) {
         const int grid = (int)(b.chunks < kClipSlots ? b.chunks : kClipSlots);
-        ZO_DISPATCH_DT(dtype, (grad_scale_kernel<DT><<<dim3(grid), dim3(256), 0, s>>>(b, part, slots, max_norm, norm, !later)));
+        ZO_DISPATCH_DT(dtype, (grad_scale_kernel<DT><<<dim3(grid), dim3(256), 0, s>>>(b, part, slots, max_norm, norm, first)));
         done = true;
         return hipGetLastError();
     });

@@ -124,21 +124,18 @@ size_t head_grad_mfma_scratch(int rows, int d, int vocab);
 hipError_t launch_head_grad_mfma(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype,
                                  int rows, int d, int vocab, float scale, hipStream_t s);
 
-struct ClipDesc {            // one tensor of a pass over gradients
-    const void *src;
-    void *dst;
-    uint32_t first, chunks;  // its first chunk in the launch, and how many it has
-    uint32_t last;           // elements of the last one
-    uint32_t pad;
-};
 constexpr uint32_t kClipChunk = 16384;     // elements per chunk
 constexpr uint32_t kClipSlots = 1024;      // workgroups of a pass at most, each with a partial sum of its own
-constexpr int kClipMax = 124;
+// Tensors of a pass over gradients, twenty bytes each: those of a 12-layer model go into one launch.
+constexpr int kClipMax = 201;
 struct ClipBatch {
+    uint64_t src[kClipMax];                // address, 48 bits; above it the elements of the last chunk less one
+    uint64_t dst[kClipMax];
+    uint32_t first[kClipMax];              // first chunk
     int n;
     uint32_t chunks;
-    ClipDesc d[kClipMax];
 };
+static_assert(kClipChunk <= 1 << 16, "the last chunk's elements less one are a 16-bit number");
 static_assert(sizeof(ClipBatch) + 64 <= 4096, "passed by value: a kernel takes 4 KiB of arguments");
 // dst may be src, tensor by tensor.  `scratch`: kClipSlots doubles; `norm`: the norm and the coefficient
 hipError_t launch_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm, double *norm,
