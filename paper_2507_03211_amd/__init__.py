@@ -106,12 +106,11 @@ def lib():
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    address = getattr(x, "data_ptr", None)       # tensors first: a call has up to nine of them
+    if address is not None:
+        return address()
+    if x is None or isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     raise TypeError("expected a tensor, an address or None, got %r" % type(x))
 
 

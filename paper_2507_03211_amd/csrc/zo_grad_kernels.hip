@@ -335,51 +335,101 @@ __global__ __launch_bounds__(256) void head_probs_kernel(double *__restrict__ lo
     *lg = tg < 0 ? 0.0 : c == at ? expm1(*lg - lse) : exp(*lg - lse);
 }
 
-// c[i, j] (+)= scale sum_k a(i, k) b(k, j): a's element at a[i ai + k ak], b's row k at b[k n].  64 x 64 outputs a workgroup, 16
-// terms a slab.  Rows of b (`live_k`) or of c (`live_i`) whose target does not count are taken as zeros, whatever they hold.
-template <typename TB, typename TC>
-__global__ __launch_bounds__(256) void head_product_kernel(const double *__restrict__ a, size_t ai, size_t ak, const TB *__restrict__ b, TC *__restrict__ c, int m,
-                                                           int n, int k, double scale, int accumulate, const int32_t *__restrict__ live_k,
-                                                           const int32_t *__restrict__ live_i)
+// Both of the above in one launch, for a vocabulary in one piece of up to kSoftmaxWords: a row's logits stay in registers between.
+constexpr int kSoftmaxWords = 4096;
+__global__ __launch_bounds__(256) void head_softmax_kernel(double *__restrict__ logits, const int32_t *__restrict__ target, double *__restrict__ row_loss, int vocab)
 {
-    constexpr int B = 64, S = 16;
-    __shared__ double as[S][B + 1], bs[S][B + 1];
-    const int i0 = blockIdx.y * B, j0 = blockIdx.x * B, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    double acc[4][4] = {};
-    for (int k0 = 0; k0 < k; k0 += S) {
+    __shared__ double red[16];
+    constexpr int NE = kSoftmaxWords / 256;
+    const size_t r = blockIdx.x;
+    const int tg = target[r];
+    double *lg = logits + r * vocab;
+    double v[NE], mx = -INFINITY, s = 0.0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int idx = threadIdx.x + 256 * e;
-            // neighbouring threads along whichever index is contiguous
-            const int ar = ak == 1 ? idx / S : idx % B, akk = ak == 1 ? idx % S : idx / B;
-            as[akk][ar] = k0 + akk < k && i0 + ar < m ? a[(size_t)(i0 + ar) * ai + (size_t)(k0 + akk) * ak] : 0.0;
-            const int bc = idx % B, bkk = idx / B;
-            const bool in = k0 + bkk < k && j0 + bc < n && (!live_k || live_k[k0 + bkk] >= 0);
-            bs[bkk][bc] = in ? (double)b[(size_t)(k0 + bkk) * n + (j0 + bc)] : 0.0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < S; ++kk) {
-            double x[4], y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { x[e] = as[kk][ty + 16 * e]; y[e] = bs[kk][tx + 16 * e]; }
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[p][q] += x[p] * y[q];
-        }
-        __syncthreads();
+    for (int i = 0; i < NE; ++i) {
+        const int c = threadIdx.x + 256 * i;
+        v[i] = c < vocab ? lg[c] : -INFINITY;
     }
+    const double hit = tg >= 0 && tg < vocab ? lg[tg] : 0.0;
 #pragma unroll
-    for (int p = 0; p < 4; ++p)
+    for (int i = 0; i < NE; ++i) mx = v[i] > mx ? v[i] : mx;
+    mx = block_max(mx, red);
+#pragma unroll
+    for (int i = 0; i < NE; ++i)
+        if (256 * i < vocab) s += exp(v[i] - mx);
+    s = block_sum(s, red);
+    const double lse = tg >= vocab ? __builtin_nan("") : mx + log(s);
+    if (threadIdx.x == 0) row_loss[r] = tg < 0 ? 0.0 : lse - hit;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+        const int c = threadIdx.x + 256 * i;
+        if (c < vocab) lg[c] = tg < 0 ? 0.0 : c == tg ? expm1(v[i] - lse) : exp(v[i] - lse);
+    }
+}
+
+// dx = scale G e (rows of G and dx: `rows`; added to what is there with `accumulate`) and de = scale G^T x, one launch: the first dx_tiles
+// workgroups have tiles of dx, the others of de.  A workgroup owns 16 TB x 16 TB outputs, its W wavefronts take every W-th 16-deep piece
+// of the contraction straight from memory into v_mfma_f64_16x16x4 operands, and the partial sums meet in LDS, in a fixed order (as in the
+// layers of this precision).  x's rows whose target does not count are taken as zeros, whatever they hold, and dx's are zeros.
+template <int TB, int W>
+__global__ __launch_bounds__(64 * W) void head_products_kernel(const double *__restrict__ grad, const float *__restrict__ e, const double *__restrict__ x,
+                                                               const int32_t *__restrict__ target, double *__restrict__ dx, float *__restrict__ de,
+                                                               int rows, int words, int d, double scale, bool accumulate, int dx_tiles)
+{
+    typedef double f64x4 __attribute__((ext_vector_type(4)));
+    constexpr int BT = 16 * TB;
+    __shared__ double part[W][BT][BT + 1];
+    const bool by_words = (int)blockIdx.x < dx_tiles;           // of dx, the contraction over the words
+    const int tile = by_words ? (int)blockIdx.x : (int)blockIdx.x - dx_tiles;
+    const int tiles_d = (d + BT - 1) / BT, i0 = tile / tiles_d * BT, j0 = tile % tiles_d * BT;
+    const int m = by_words ? rows : words, k = by_words ? words : rows;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+    f64x4 acc[TB][TB] = {};
+#pragma unroll 2
+    for (int k0 = 16 * wave; k0 < k; k0 += 16 * W) {
+        f64x4 av[TB], bv[TB];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int i = i0 + ty + 16 * p, j = j0 + tx + 16 * q;
-            if (i >= m || j >= n) continue;
-            TC *at = c + (size_t)i * n + j;
-            const double v = live_i && live_i[i] < 0 ? 0.0 : scale * acc[p][q];
-            *at = (TC)(accumulate ? (double)*at + v : v);
+            const int kk = k0 + 4 * g + q, kc = kk < k ? kk : k - 1;
+            const bool live = kk < k && (by_words || target[kc] >= 0);
+#pragma unroll
+            for (int t = 0; t < TB; ++t) {
+                const int i = i0 + 16 * t + r16 < m ? i0 + 16 * t + r16 : m - 1, j = j0 + 16 * t + r16 < d ? j0 + 16 * t + r16 : d - 1;   // clamped: never stored
+                const double a = by_words ? grad[(size_t)i * words + kc] : grad[(size_t)kc * words + i];
+                const double b = by_words ? (double)e[(size_t)kc * d + j] : x[(size_t)kc * d + j];
+                av[t][q] = live ? a : 0.0;
+                bv[t][q] = live ? b : 0.0;
+            }
         }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < TB; ++i)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f64_16x16x4f64(av[i][q], bv[j][q], acc[i][j], 0, 0, 0);
+    }
+    // element e of a lane's result: row 4 e + lane / 16, column lane % 16 of the 16 x 16 block
+#pragma unroll
+    for (int i = 0; i < TB; ++i)
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) part[wave][16 * i + 4 * q + g][16 * j + r16] = acc[i][j][q];
+    __syncthreads();
+    for (int o = threadIdx.x; o < BT * BT; o += 64 * W) {
+        const int i = i0 + o / BT, j = j0 + o % BT;
+        if (i >= m || j >= d) continue;
+        double v = 0.0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v += part[w][o / BT][o % BT];
+        v *= scale;
+        if (by_words) {
+            double *at = dx + (size_t)i * d + j;
+            *at = target[i] < 0 ? 0.0 : accumulate ? *at + v : v;
+        } else {
+            de[(size_t)i * d + j] = (float)v;
+        }
+    }
 }
 
 // ------------------------------------------------------------------ global norm and clipping
@@ -593,7 +643,13 @@ hipError_t head_grad_f64(const double *x, const float *e, const int32_t *target,
         return launch_linear(x, w, w, nullptr, nullptr, logits, kFP32, 1, rows, piece(v0), d, 3, true, s);
     };
     hipError_t err = hipSuccess;
-    for (int v0 = 0; v0 < vocab; v0 += width) {
+    const bool together = width == vocab && vocab <= kSoftmaxWords;
+    if (together) {
+        if ((err = make_logits(0)) != hipSuccess) return err;
+        head_softmax_kernel<<<dim3(rows), dim3(256), 0, s>>>(logits, target, row_loss, vocab);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
+    for (int v0 = 0; v0 < vocab && !together; v0 += width) {
         if ((err = make_logits(v0)) != hipSuccess) return err;
         head_stats_kernel<<<dim3(rows), dim3(256), 0, s>>>(logits, target, state, piece(v0), v0);
         if ((err = hipGetLastError()) != hipSuccess) return err;
@@ -602,14 +658,18 @@ hipError_t head_grad_f64(const double *x, const float *e, const int32_t *target,
         // (a single piece's logits are still there)
         if (width < vocab && (err = make_logits(v0)) != hipSuccess) return err;
         const int n = piece(v0);
-        head_probs_kernel<<<dim3(rows, (n + 255) / 256), dim3(256), 0, s>>>(logits, target, state, v0 == 0 ? row_loss : nullptr, n, v0, vocab);
-        if ((err = hipGetLastError()) != hipSuccess) return err;
-        head_product_kernel<float, double><<<dim3((d + 63) / 64, (rows + 63) / 64), dim3(256), 0, s>>>(
-            logits, (size_t)n, 1, e + (size_t)v0 * d, dx, rows, d, n, scale, v0 > 0, nullptr, target);
-        if ((err = hipGetLastError()) != hipSuccess) return err;
-        head_product_kernel<double, float><<<dim3((d + 63) / 64, (n + 63) / 64), dim3(256), 0, s>>>(
-            logits, 1, (size_t)n, x, de + (size_t)v0 * d, n, d, rows, scale, 0, target, nullptr);
-        if ((err = hipGetLastError()) != hipSuccess) return err;
+        if (!together) {
+            head_probs_kernel<<<dim3(rows, (n + 255) / 256), dim3(256), 0, s>>>(logits, target, state, v0 == 0 ? row_loss : nullptr, n, v0, vocab);
+            if ((err = hipGetLastError()) != hipSuccess) return err;
+        }
+        auto products = [&](auto kern, int bt, int waves) {
+            const long tiles_d = (d + bt - 1) / bt, dx_tiles = (rows + bt - 1) / bt * tiles_d, de_tiles = (n + bt - 1) / bt * tiles_d;
+            kern<<<dim3((unsigned)(dx_tiles + de_tiles)), dim3(64 * waves), 0, s>>>(logits, e + (size_t)v0 * d, x, target, dx, de + (size_t)v0 * d, rows, n, d,
+                                                                                   scale, v0 > 0, (int)dx_tiles);
+            return hipGetLastError();
+        };
+        const bool many = (long)((rows + 31) / 32) * ((d + 31) / 32) >= 256;
+        if ((err = many ? products(head_products_kernel<2, 4>, 32, 4) : products(head_products_kernel<1, 8>, 16, 8)) != hipSuccess) return err;
     }
     return hipSuccess;
 }
