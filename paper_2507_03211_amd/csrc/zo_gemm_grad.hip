@@ -2,11 +2,13 @@
 //
 //   l = x e^T,  lse_r = log sum_v exp(l_rv),  G = exp(l - lse) - onehot(target),  dx = scale G e,  de = scale G^T x
 //
-// Four products of 2 rows vocab d flop: the logits twice, first for lse alone (the fused cross entropy of the forward pass, which leaves
-// (maximum, sum) pairs and no logits), then for G, and the two with G.  G exists one piece of the vocabulary at a time, rounded to the
-// parameters' 16-bit type because that is what the matrix instructions take: each element is off by half a step, a product's
-// sum by about as much as its own final rounding (the largest element, that of the target, is p - 1 formed in fp32).  Operands stay as
-// they lie: G, e and x are read with the contraction as the outer index where a product wants it so (zo_gemm_tiles.hip.h).
+// G exists one piece of the vocabulary at a time, rounded to the parameters' 16-bit type because that is what the matrix instructions
+// take: each element is off by half a step, a product's sum by about as much as its own final rounding (the largest element, that of the
+// target, is p - 1 formed in fp32).  Where one piece holds the whole vocabulary there are three products of 2 rows vocab d flop: the logits
+// leave 16-bit distances from their strip's maximum where G will lie, with the strips' (maximum, sum) pairs, and a pass over these makes G.
+// Where it takes more, four: the logits for lse alone (the fused cross entropy of the forward pass, which leaves pairs and no logits), then
+// again, piece by piece, for G.  Operands stay as they lie: G, e and x are read with the contraction as the outer index where a
+// product wants it so (zo_gemm_tiles.hip.h).
 #include "zo_gemm_tiles.hip.h"
 
 namespace zo {
@@ -67,6 +69,55 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float2 *__restrict_
     stats[r] = float2{hi, (float)(((double)hi - lse) * 1.4426950408889634) + shift};
 }
 
+// Distances and pairs of a row -> its loss and, in place, its G (as in epilogue 5); zeros in rows that do not count, past the last row and past
+// the last word.  One workgroup a row, so that logsumexp is worked once.  Bound by memory: 4 bytes a word.
+template <int DT>
+__global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ grad, const float2 *__restrict__ pairs, int n_pairs, int strip,
+                                                            const float *__restrict__ hit, const int32_t *__restrict__ target, float *__restrict__ row_loss,
+                                                            int rows, int vocab, int width)
+{
+    __shared__ float red_f[16];
+    __shared__ double red_d[16];
+    constexpr float kOne = DT == kFP16 ? 32768.0f : 1.0f, kShift = DT == kFP16 ? 15.0f : 0.0f;
+    const int r = blockIdx.x, tg = r < rows ? target[r] : -1;
+    uint4 *out = grad + (size_t)r * (width / 8);
+    if (tg < 0) {
+        if (r < rows && threadIdx.x == 0) row_loss[r] = 0.0f;
+        for (int c = threadIdx.x; c < width / 8; c += 512) out[c] = uint4{0, 0, 0, 0};
+        return;
+    }
+    const float2 *p = pairs + (size_t)r * n_pairs;
+    float mx = -INFINITY;
+    for (int i = threadIdx.x; i < n_pairs; i += 512) mx = p[i].x > mx ? p[i].x : mx;
+    mx = block_max(mx, red_f);
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n_pairs; i += 512)
+        if (p[i].x > -INFINITY) s += (double)p[i].y * (double)__expf(p[i].x - mx);
+    s = block_sum(s, red_d);
+    const double lse = tg < vocab ? log(s) + (double)mx : (double)__builtin_nan("");
+    if (threadIdx.x == 0) row_loss[r] = (float)(lse - (double)hit[r]);
+    const float hi = (float)lse, rest = (float)(((double)hi - lse) * 1.4426950408889634) + kShift;
+    const float at_target = tg < vocab ? __builtin_amdgcn_exp2f(__builtin_fmaf(hit[r] - hi, 1.44269504f, rest)) - kOne : 0.0f;
+    for (int c = threadIdx.x; c < width / 8; c += 512) {
+        uint4 q = out[c];
+        const int w0 = 8 * c;
+        const float base = __builtin_fmaf(p[w0 / strip].x - hi, 1.44269504f, rest);
+        uint32_t *words = &q.x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = words[e] & 0xffff, up = words[e] >> 16;
+            auto value = [&](uint32_t steps, int w) {
+                float v = __builtin_amdgcn_exp2f(__builtin_fmaf((float)steps, -1.44269504f * 32.0f / 65535.0f, steps == 65535 ? -INFINITY : base));
+                v = base == base ? v : base;                   // (a row that is not a number, whatever its steps)
+                v = w == tg ? at_target : v;
+                return w < vocab ? v : 0.0f;
+            };
+            words[e] = (uint32_t)Prec<DT>::acc2a(value(lo, w0 + 2 * e)) | ((uint32_t)Prec<DT>::acc2a(value(up, w0 + 2 * e + 1)) << 16);
+        }
+        out[c] = q;
+    }
+}
+
 // dx = rn(alpha sum_z part[z]): the shares of the contraction over the vocabulary, in order.  Eight elements a thread.
 template <int DT>
 __global__ __launch_bounds__(256) void head_dx_kernel(const float4 *__restrict__ part, int shares, size_t n8, float alpha, uint4 *__restrict__ dx)
@@ -113,15 +164,14 @@ Tile pick_product(int shares, int m, int n, int slabs, int epi, float *us = null
 }
 
 size_t up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
-size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 
 // G is held for `width` words at a time: as many as kPieceBytes hold (8192 rows: the whole of 50272 words), in `shares` shares of
 // share_words for the product with e, whose outputs [rows, d] are few tiles where rows are few.
 constexpr size_t kPieceBytes = 1u << 30;
 struct HeadPlan {
-    int rows_p, dp, width, pieces, shares, share_words, pairs;
-    Tile by_words;
-    size_t xs, es, g, stats, part, total;
+    int rows_p, dp, width, pieces, shares, share_words, pairs, strip;
+    Tile logits, by_words;
+    size_t xs, es, g, stats, pair, hit, part, total;
 };
 HeadPlan head_plan(int rows, int d, int vocab)
 {
@@ -143,14 +193,21 @@ HeadPlan head_plan(int rows, int d, int vocab)
     p.share_words = (slabs + p.shares - 1) / p.shares * BK;
     p.width = p.share_words * p.shares;
     p.pieces = (vocab + p.width - 1) / p.width;
-    p.pairs = mfma_ce_partials(1, rows, vocab, p.dp);
+    if (p.pieces == 1) {
+        p.logits = pick_product(1, p.rows_p, p.width, p.dp / BK, 0);
+        p.strip = kTileColumns[p.logits] / 2;                    // a wavefront's columns of the tile
+        p.pairs = 2 * ((p.width + kTileColumns[p.logits] - 1) / kTileColumns[p.logits]);
+    } else {
+        p.pairs = mfma_ce_partials(1, rows, vocab, p.dp);
+    }
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up(o + bytes); return at; };
     p.xs = take(2 * (size_t)p.rows_p * p.dp);
     p.es = p.dp == d ? 0 : take(2 * (size_t)vocab * p.dp);
-    p.stats = take((size_t)rows * sizeof(float2));
-    // the pairs and target logits are done with when G begins
-    p.g = take(larger(2 * (size_t)p.rows_p * p.width, up((size_t)rows * p.pairs * 8) + 4 * (size_t)rows));
+    p.stats = p.pieces == 1 ? 0 : take((size_t)rows * sizeof(float2));
+    p.pair = take((size_t)rows * p.pairs * 8);
+    p.hit = take(4 * (size_t)rows);
+    p.g = take(2 * (size_t)p.rows_p * p.width);
     p.part = take(4 * (size_t)p.shares * rows * d);
     p.total = o;
     return p;
@@ -177,14 +234,23 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
         if ((err = copy(e, nullptr, (uint16_t *)(ws + p.es), vocab, vocab)) != hipSuccess) return err;
         w = (const uint16_t *)(ws + p.es);
     }
-    float *hit = (float *)(ws + p.g + up((size_t)rows * p.pairs * 8));
-    if ((err = launch_linear_mfma(xs, w, w, target, hit, g, DT, 1, rows, vocab, p.dp, 4, s)) != hipSuccess) return err;
-    head_lse_kernel<<<dim3((rows + 3) / 4), dim3(256), 0, s>>>((const float2 *)g, p.pairs, hit, target, row_loss, stats, rows, vocab,
-                                                               DT == kFP16 ? 15.0f : 0.0f);
+    float2 *pair = (float2 *)(ws + p.pair);
+    float *hit = (float *)(ws + p.hit);
+    if (p.pieces == 1) {
+        Logits::Arg op{};
+        op.ldx = op.ldw = p.dp;
+        op.pairs = pair; op.hit = hit; op.target = target; op.rows = rows; op.words = vocab;
+        const Args a{xs, w, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
+        if ((err = launch_product<DT, 9, Logits>(p.logits, a, op)) != hipSuccess) return err;
+        head_gradient_kernel<DT><<<dim3(p.rows_p), dim3(512), 0, s>>>((uint4 *)g, pair, p.pairs, p.strip, hit, target, row_loss, rows, vocab, p.width);
+    } else {
+        if ((err = launch_linear_mfma(xs, w, w, target, hit, pair, DT, 1, rows, vocab, p.dp, 4, s)) != hipSuccess) return err;
+        head_lse_kernel<<<dim3((rows + 3) / 4), dim3(256), 0, s>>>(pair, p.pairs, hit, target, row_loss, stats, rows, vocab, DT == kFP16 ? 15.0f : 0.0f);
+    }
     if ((err = hipGetLastError()) != hipSuccess) return err;
     for (int v0 = 0; v0 < vocab; v0 += p.width) {
         const int words = vocab - v0 < p.width ? vocab - v0 : p.width;
-        {
+        if (p.pieces > 1) {
             Logits::Arg op{};
             op.ldx = op.ldw = p.dp;
             op.stats = stats; op.target = target; op.rows = rows; op.words = words; op.first_word = v0;

@@ -34,8 +34,10 @@ template <bool XK, bool WK> struct Product {
     struct Arg {
         uint64_t ldx, ldw, xz, wz, x_end, w_end;
         float alpha;                        // epilogue 6: factor of the result
-        // epilogue 5
-        const float2 *stats;                // per row: logsumexp (rounded; infinity in rows that do not count) and what goes on top of the exponent
+        // epilogues 5 and 9
+        const float2 *stats;                // 5: per row, logsumexp (rounded; infinity in rows that do not count) and what goes on top of the exponent
+        float2 *pairs;                      // 9: per row and strip
+        float *hit;                         // 9: the target's logit
         const int32_t *target;
         int rows, words, first_word;        // rows and words that exist; the first word's number
     };
@@ -54,13 +56,13 @@ template <int DT> __device__ __forceinline__ f32x16 mfma32(const uint4 &a, const
 // Epilogue 4 (tied LM head fused with the cross-entropy reduction): nothing of the logits is stored.  A lane
 // holds TN * 16 logits of one row (4 runs of 4 consecutive columns per MFMA tile); it reduces them to a
 // (maximum, sum of exp) pair, merges with the other lane half (the remaining columns of the wave's range)
-// and the wave writes one pair per row and per wave-column-range; the lane that holds the target column
+// and the wave writes one pair per row and per wave-column-range (the row's maximum there is also returned); the lane that holds the target column
 // stores that logit.  A last small kernel merges the pairs of a row into logsumexp - target logit.
 // Argument reuse for this epilogue: bias_p -> int32 target[rows], bias_m -> float target_logit[rows],
 // y -> float2 partial[rows][n_partial].
 template <int TN>
-__device__ __forceinline__ void ce_partial_row(const f32x16 (&a)[TN], int col0, int fh, int n, bool live, int tg,
-                                               float *tgt_logit_row, float2 *partial_slot)
+__device__ __forceinline__ float ce_partial_row(f32x16 (&a)[TN], int col0, int fh, int n, bool live, int tg,
+                                                float *tgt_logit_row, float2 *partial_slot)
 {
     // `live` false: a row past the ragged end of the tile.  It takes part (the two halves of the wave exchange their
     // results below) and stores nothing; its pointers are those of the last valid row.
@@ -89,6 +91,8 @@ __device__ __forceinline__ void ce_partial_row(const f32x16 (&a)[TN], int col0, 
             v[k] += pen;
         }
     }
+#pragma unroll
+    for (int k = 0; k < NE; ++k) a[k / 16][k % 16] = v[k];     // (for a caller that goes on with them: one copy in registers, not two)
     // (two maxima and four sums side by side: with one wave per SIMD an instruction that waits for the one before it issues
     // after 8 cycles instead of 5, and 64 additions in a row are half of such waits.  With the row targets loaded together, see
     // the caller: LM head of 50272 columns, us before / here: 8176 rows a sign, d 768, 1048 / 1022; 1048 rows, d 2048, 389 / 384)
@@ -123,10 +127,10 @@ __device__ __forceinline__ void ce_partial_row(const f32x16 (&a)[TN], int col0, 
 #pragma unroll
         for (int k = 0; k < NE; ++k) t[k] = v[k];
 #pragma unroll
-        for (int bit = 0, cnt = NE; cnt > 1; ++bit, cnt >>= 1) {
+        for (int bit = 0, cnt = NE; cnt > 1; ++bit, cnt = (cnt + 1) / 2) {
             const bool odd = (which >> bit) & 1;
 #pragma unroll
-            for (int k = 0; k < cnt / 2; ++k) t[k] = odd ? t[2 * k + 1] : t[2 * k];
+            for (int k = 0; k < (cnt + 1) / 2; ++k) t[k] = odd && 2 * k + 1 < cnt ? t[2 * k + 1] : t[2 * k];
         }
         if (live && mine) *tgt_logit_row = t[0];
     }
@@ -134,6 +138,7 @@ __device__ __forceinline__ void ce_partial_row(const f32x16 (&a)[TN], int col0, 
     const float m2 = mx > mo ? mx : mo;
     const float s2 = (mx > -INFINITY ? sum * __expf(mx - m2) : 0.0f) + (mo > -INFINITY ? so * __expf(mo - m2) : 0.0f);
     if (live && fh == 0) *partial_slot = float2{m2, s2};
+    return m2;
 }
 
 constexpr int kGroupM = 8;                      // tile-rows per band
@@ -232,7 +237,9 @@ __device__ __forceinline__ void gradient_row(f32x16 (&a)[TN], float2 st, int rel
     }
 }
 
-// Epilogues 0 - 3 and 5 - 8 of a wave's 32 TM x 32 TN outputs (rows m0 + wm 32 TM .., columns n0 + wn 32 TN .. of sign `sign`).
+// Epilogues 0 - 3 and 5 - 9 of a wave's 32 TM x 32 TN outputs (rows m0 + wm 32 TM .., columns n0 + wn 32 TN .. of sign `sign`).
+// 9: epilogue 4's pairs, and every logit as its distance from the pair's maximum in steps of 32 / 65535 (a distance of 32
+// and more counts as none: e^-32 of the strip's largest; half a step is 2^-12 of a probability, half of fp16's own half step).
 // 5: 16-bit, the values as they are; 6: 16-bit, times alpha; 7: fp32; 8: added to fp32 sums; all without bias.
 // `stage`: kTileStageBytes<TN> bytes of LDS that are this wave's alone.  NT: non-temporal accesses (see launch_small).
 template <int TN> constexpr int kTileStageBytes = (TN & (TN - 1)) ? 2048 * TN + 512 : 2048 * TN;
@@ -247,7 +254,7 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
     // length is a power of two are XOR-swizzled by the row: the run-wise writes and the row-wise 16-byte reads are free of
     // bank conflicts (16-bit rows of one tile apart, see chunk16 below).  Others have 16 bytes of padding, which leaves two
     // lanes per bank in the writes (15 % of the LDS cycles of a 12-slab launch of 256 x 192 tiles).
-    constexpr bool kOut16 = (EPI == 0 || EPI == 1 || EPI == 5 || EPI == 6);              // 2-byte outputs; else fp32
+    constexpr bool kOut16 = (EPI == 0 || EPI == 1 || EPI == 5 || EPI == 6 || EPI == 9);              // 2-byte outputs; else fp32
     constexpr bool kAdd = EPI == 2 || EPI == 8, kBias = EPI < 3;
     constexpr int RP = kOut16 ? 32 : 16;                         // rows per pass
     constexpr int NPASS = 32 * TM / RP;
@@ -359,7 +366,14 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
     };
     // epilogue 5: what the lane's rows need, all at once
     float2 st[EPI == 5 ? TM : 1];
-    int rel[EPI == 5 ? TM : 1];
+    int rel[EPI == 5 || EPI == 9 ? TM : 1];
+    if constexpr (EPI == 9) {                                  // (here: the targets)
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) {
+            const int r = row0 + tm * 32 + fr;
+            rel[tm] = op.target[r < op.rows ? r : op.rows - 1];
+        }
+    }
     if constexpr (EPI == 5) {
 #pragma unroll
         for (int tm = 0; tm < TM; ++tm) {
@@ -373,7 +387,16 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
 #pragma unroll
     for (int pass = 0; pass < NPASS; ++pass) {
         const int tm = pass * RP / 32;                          // MFMA row block of this pass
-        f32x16 grad[EPI == 5 ? TN : 1];
+        f32x16 grad[EPI == 5 || EPI == 9 ? TN : 1];
+        if constexpr (EPI == 9) {
+#pragma unroll
+            for (int tn = 0; tn < TN; ++tn) grad[tn] = acc[tn][tm];
+            const int r = row0 + tm * 32 + fr, at = r < op.rows ? r : op.rows - 1, strips = 2 * ((n + 64 * TN - 1) / (64 * TN));
+            const float top = ce_partial_row<TN>(grad, ncol0, fh, op.words, r < op.rows, rel[tm], op.hit + at,
+                                                 op.pairs + (size_t)at * strips + ncol0 / (32 * TN));
+#pragma unroll
+            for (int k = 0; k < 16 * TN; ++k) grad[k / 16][k % 16] = __builtin_fmaf(grad[k / 16][k % 16], -0x1p-5f, top * 0x1p-5f);
+        }
         if constexpr (EPI == 5) {
 #pragma unroll
             for (int tn = 0; tn < TN; ++tn) grad[tn] = acc[tn][tm];
@@ -391,7 +414,7 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
                     float v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if constexpr (EPI == 5) v[e] = grad[tn][4 * g + e];
+                        if constexpr (EPI == 5 || EPI == 9) v[e] = grad[tn][4 * g + e];
                         else v[e] = acc[tn][tm][4 * g + e];
                         if constexpr (kOut16 && kBias) v[e] += bvals[tn][g][e];
                         if constexpr (EPI == 6) v[e] *= op.alpha;
@@ -405,7 +428,13 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
                             if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
                             else return __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, f16x2));
                         };
-                        const uint2 o = {pack2(v[0], v[1]), pack2(v[2], v[3])};
+                        uint2 o;
+                        if constexpr (EPI == 9) {              // 0 .. 1 to 0 .. 65535, nearest, what lies outside to the ends: one instruction for two
+                            auto steps2 = [](float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(lo, hi)); };
+                            o = uint2{steps2(v[0], v[1]), steps2(v[2], v[3])};
+                        } else {
+                            o = uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+                        }
                         const int slot = kXor ? (((tn * 4 + g) ^ chunk16(fr)) << 1) + (fh ^ ((fr >> kFlip) & 1)) : run;
                         *(uint2 *)(stage + fr * PITCH + (slot << 3)) = o;
                     } else {
@@ -517,9 +546,9 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
         uint64_t xbase, wbase;          // first row of the tile in x / in the sign's weights (wave-uniform)
         uint32_t xg[LX], wg[LW];        // byte offsets of this lane's loads from those (clamped at ragged edges)
     };
-    // rows of w that exist, and the first one of a tile at column n0 (epilogue 5: G is wider than there are words, by whole tiles too)
-    const int w_rows = [&] { if constexpr (EPI == 5) return op.words; else return n; }();
-    auto w_first = [&](int n0) { if constexpr (EPI == 5) return n0 < w_rows ? n0 : w_rows - 1; else return n0; };
+    // rows of w that exist, and the first one of a tile at column n0 (epilogues 5 and 9: G is wider than there are words, by whole tiles too)
+    const int w_rows = [&] { if constexpr (EPI == 5 || EPI == 9) return op.words; else return n; }();
+    auto w_first = [&](int n0) { if constexpr (EPI == 5 || EPI == 9) return n0 < w_rows ? n0 : w_rows - 1; else return n0; };
     auto setup = [&](int lin, Tile &t) {
         int trow;
         tile_at(lin, tiles_m, tiles_n, t.sign, trow, t.tcol);
@@ -759,7 +788,7 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
             static_assert(kTileStageBytes<TN> <= 1024 * LX, "a pass fits the slice");
             char *stage = (char *)(smem + xfree) + wave * (1024 * LX);
             // (G is read again at once)
-            store_tile<DT, EPI, TM, TN, EPI != 5>(acc, stage, bias, y, sign, m_half, n, m0, n0, wm, wn, lane, op);
+            store_tile<DT, EPI, TM, TN, EPI != 5 && EPI != 9>(acc, stage, bias, y, sign, m_half, n, m0, n0, wm, wn, lane, op);
         }
         if (!has_next) break;
         cur = nxt;
@@ -800,8 +829,8 @@ __global__ __launch_bounds__(256, 2) void linear_mfma_small_kernel(
     tile_at(lin, tiles_m, tiles_n, sign, trow, tcol);
     const int m0 = trow * BM, n0 = tcol * BN;
     uint64_t xbase, wbase;
-    const int w_rows = [&] { if constexpr (EPI == 5) return op.words; else return n; }();      // as in the kernel above
-    const int w_first = EPI == 5 && n0 >= w_rows ? w_rows - 1 : n0;
+    const int w_rows = [&] { if constexpr (EPI == 5 || EPI == 9) return op.words; else return n; }();      // as in the kernel above
+    const int w_first = (EPI == 5 || EPI == 9) && n0 >= w_rows ? w_rows - 1 : n0;
     if constexpr (OP::kPlain) {
         xbase = uniform64((uint64_t)(uintptr_t)(x + ((size_t)sign * m_half + m0) * k));
         wbase = uniform64((uint64_t)(uintptr_t)((sign ? wt_m : wt_p) + (size_t)n0 * k));
