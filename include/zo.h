@@ -368,7 +368,7 @@ int zo_kernel_layernorm(const void *resid, const void *gain, const void *bias, v
  *     dresid = rstd (a - mean_c(a) - xh mean_c(a xh)),    dgain = sum_r dy xh,    dbias = sum_r dy.
  * accumulate non-zero: dresid is added to what the buffer holds (the gradient that passes the LayerNorm by on the residual
  * stream).  dresid may be NULL (gain may be, then), or dgain and dbias both (scratch may be, then).  dresid may not overlap
- * the inputs. */
+ * the inputs.  Both calls: up to 2^23 rows, d up to 2^22. */
 size_t zo_kernel_layernorm_grad_scratch_bytes(int dtype, int rows, int d);
 int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid,
                              void *dgain, void *dbias, void *scratch, int dtype, int rows, int d, int accumulate, void *stream);
@@ -377,11 +377,20 @@ int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain
  *     row_loss[r] = logsumexp(l[r]) - l[r, target[r]],    G = scale (softmax(l) - onehot(target)),    dx = G e,    de = G^T x.
  * A row with target[r] < 0 does not count: row_loss, its row of G and its row of dx are 0 whatever x[r] holds, NaN included.  A
  * target >= vocab makes the row's loss NaN, and dx[r] and de with it.  scale: 1 / (rows that count) for the mean loss, times
- * whatever keeps ZO_FP16 gradients in range.  de is the head's share of the tied embedding's gradient alone.  2-byte
- * dtypes: d and vocab multiples of 8, buffers 16-byte aligned (ZO_EINVAL otherwise). */
+ * whatever keeps ZO_FP16 gradients in range.  de is the head's share of the tied embedding's gradient alone.  Outputs overlap
+ * nothing.  Up to 2^20 rows, d and vocab up to 2^22; 2-byte dtypes: d and vocab multiples of 8, buffers 16-byte aligned
+ * (ZO_EINVAL otherwise).
+ * 2-byte dtypes round G to their type between the products (each sum is off by about as much as its own rounding once more), and
+ * count a probability below e^-32 of the largest among its 32 to 128 neighbours as none.  The scratch holds G for as much of the
+ * vocabulary as 2^30 bytes do (ZO_FP32: 2^28); where that is less than all of it, it is worked piece by piece. */
 size_t zo_kernel_lmhead_grad_scratch_bytes(int dtype, int rows, int d, int vocab);
 int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch,
                           int dtype, int rows, int d, int vocab, float scale, void *stream);
+
+/* How such a call of 2-byte types works on the current device (on 256 compute units where there is none): plan[0 .. 2] the output
+ * tiles of the logits, de and dx (rows << 16 | columns), plan[3] the shares that the contraction over the vocabulary is cut into
+ * for dx, plan[4] the pieces of the vocabulary.  Host only. */
+int zo_kernel_lmhead_grad_plan(int rows, int d, int vocab, int32_t *plan);
 
 /* Global norm of n_tensors gradients and clipping by it: norm[0] = sqrt(sum of all squares), norm[1] = c = max_norm / norm[0] where
  * norm[0] > max_norm, else 1; dst[t] = rn(c src[t]) for every tensor t of numel[t] elements.  A norm that is not a finite number makes c 0 and

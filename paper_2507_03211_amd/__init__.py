@@ -27,7 +27,7 @@ EXPORTS = (
     "zo_kernel_layernorm_pm", "zo_kernel_attention", "zo_kernel_lmhead_scratch_bytes", "zo_kernel_lmhead_ce",
     "zo_kernel_lmhead_ce_noalloc",
     "zo_kernel_layernorm", "zo_kernel_layernorm_grad_scratch_bytes", "zo_kernel_layernorm_grad", "zo_kernel_lmhead_grad_scratch_bytes",
-    "zo_kernel_lmhead_grad", "zo_kernel_grad_clip_scratch_bytes", "zo_kernel_grad_clip",
+    "zo_kernel_lmhead_grad_plan", "zo_kernel_lmhead_grad", "zo_kernel_grad_clip_scratch_bytes", "zo_kernel_grad_clip",
 )
 
 
@@ -97,6 +97,7 @@ def lib():
         L.zo_kernel_layernorm_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
         L.zo_kernel_lmhead_grad_scratch_bytes.restype = sz
         L.zo_kernel_lmhead_grad_scratch_bytes.argtypes = [i32, i32, i32, i32]
+        L.zo_kernel_lmhead_grad_plan.argtypes = [i32, i32, i32, vp]
         L.zo_kernel_lmhead_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, f32, vp]
         L.zo_kernel_grad_clip_scratch_bytes.restype = sz
         L.zo_kernel_grad_clip_scratch_bytes.argtypes = []
@@ -323,6 +324,14 @@ def zo_kernel_layernorm_grad(dy, resid, gain, mean, rstd, dresid, dgain, dbias, 
 
 def zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab):
     return int(lib().zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab))
+
+
+def zo_kernel_lmhead_grad_plan(rows, d, vocab):
+    """Of 2-byte types: {"logits", "de", "dx": (rows, columns) of the output tiles, "shares", "pieces"}."""
+    plan = (ctypes.c_int32 * 5)()
+    _check(lib().zo_kernel_lmhead_grad_plan(rows, d, vocab, plan))
+    tiles = {name: (plan[i] >> 16, plan[i] & 0xffff) for i, name in enumerate(("logits", "de", "dx"))}
+    return dict(tiles, shares=plan[3], pieces=plan[4])
 
 
 def zo_kernel_lmhead_grad(x, e, target, row_loss, dx, de, scratch, dtype, rows, d, vocab, scale, stream=None):

@@ -1341,12 +1341,14 @@ extern "C" int zo_kernel_lmhead_ce_noalloc(const void *x, const void *e_plus, co
 }
 
 // ------------------------------------------------------------------ gradient of the last module
+static bool norm_shape(int rows, int d) { return rows >= 1 && rows <= 1 << 23 && d >= 1 && d <= 1 << 22; }      // (a workgroup a row: grids of 2^32 threads)
+
 extern "C" int zo_kernel_layernorm(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype, int rows, int d,
                                    float ln_eps, void *stream)
 {
     ZO_TRY(check_dtype(dtype));
     if (!resid || !gain || !bias || !y || !mean || !rstd) return fail(ZO_EINVAL, "NULL argument");
-    if (rows < 1 || d < 1) return fail(ZO_EINVAL, "bad shape %d x %d", rows, d);
+    if (!norm_shape(rows, d)) return fail(ZO_EINVAL, "bad shape %d x %d", rows, d);
     if (!(ln_eps > 0.0f)) return fail(ZO_EINVAL, "ln_eps must be positive");
     ZO_HIP(launch_layernorm_stats(resid, gain, bias, y, mean, rstd, dtype, rows, d, ln_eps, (hipStream_t)stream));
     return ZO_OK;
@@ -1354,7 +1356,7 @@ extern "C" int zo_kernel_layernorm(const void *resid, const void *gain, const vo
 
 extern "C" size_t zo_kernel_layernorm_grad_scratch_bytes(int dtype, int rows, int d)
 {
-    return dtype < 0 || dtype > 2 || rows < 1 || d < 1 ? 0 : layernorm_grad_scratch(dtype, rows, d);
+    return dtype < 0 || dtype > 2 || !norm_shape(rows, d) ? 0 : layernorm_grad_scratch(dtype, rows, d);
 }
 
 extern "C" int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid, void *dgain,
@@ -1362,7 +1364,7 @@ extern "C" int zo_kernel_layernorm_grad(const void *dy, const void *resid, const
 {
     ZO_TRY(check_dtype(dtype));
     if (!dy || !resid || !mean || !rstd) return fail(ZO_EINVAL, "NULL argument");
-    if (rows < 1 || d < 1) return fail(ZO_EINVAL, "bad shape %d x %d", rows, d);
+    if (!norm_shape(rows, d)) return fail(ZO_EINVAL, "bad shape %d x %d", rows, d);
     if (!dgain != !dbias) return fail(ZO_EINVAL, "dgain and dbias go together: one of them is NULL");
     if (!dresid && !dgain) return fail(ZO_EINVAL, "no output asked for");
     if (dresid && !gain) return fail(ZO_EINVAL, "gain is NULL");
@@ -1372,9 +1374,26 @@ extern "C" int zo_kernel_layernorm_grad(const void *dy, const void *resid, const
     return ZO_OK;
 }
 
+// Sizes the kernels' 32-bit offsets and launch grids hold, far beyond any in use.
+constexpr int kMaxGradRows = 1 << 20, kMaxGradColumns = 1 << 22;
+
+static bool lmhead_grad_shape(int dtype, int rows, int d, int vocab)
+{
+    return rows >= 1 && rows <= kMaxGradRows && d >= 1 && d <= kMaxGradColumns && vocab >= 2 && vocab <= kMaxGradColumns &&
+           (dtype == ZO_FP32 || (d % 8 == 0 && vocab % 8 == 0));
+}
+
 extern "C" size_t zo_kernel_lmhead_grad_scratch_bytes(int dtype, int rows, int d, int vocab)
 {
-    return dtype < 0 || dtype > 2 || rows < 1 || d < 1 || vocab < 2 ? 0 : head_grad_scratch(dtype, rows, d, vocab);
+    return dtype < 0 || dtype > 2 || !lmhead_grad_shape(dtype, rows, d, vocab) ? 0 : head_grad_scratch(dtype, rows, d, vocab);
+}
+
+extern "C" int zo_kernel_lmhead_grad_plan(int rows, int d, int vocab, int32_t *plan)
+{
+    if (!plan) return fail(ZO_EINVAL, "plan is NULL");
+    if (!lmhead_grad_shape(ZO_BF16, rows, d, vocab)) return fail(ZO_EINVAL, "bad shape: %d rows, d %d, vocab %d", rows, d, vocab);
+    head_grad_mfma_plan(rows, d, vocab, plan);
+    return ZO_OK;
 }
 
 extern "C" int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch_mem, int dtype,
@@ -1382,8 +1401,8 @@ extern "C" int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t
 {
     ZO_TRY(check_dtype(dtype));
     if (!x || !e || !target || !row_loss || !dx || !de || !scratch_mem) return fail(ZO_EINVAL, "NULL argument");
-    if (rows < 1 || d < 1 || vocab < 2) return fail(ZO_EINVAL, "bad shape: %d rows, d %d, vocab %d", rows, d, vocab);
-    if (dtype != ZO_FP32 && (d % 8 || vocab % 8)) return fail(ZO_EINVAL, "d and vocab must be multiples of 8 for 2-byte types");
+    if (!lmhead_grad_shape(dtype, rows, d, vocab))
+        return fail(ZO_EINVAL, "bad shape: %d rows, d %d, vocab %d (up to 2^20, 2^22, 2^22; 2-byte types: d and vocab multiples of 8)", rows, d, vocab);
     if (dtype != ZO_FP32 && ((uintptr_t)x % 16 || (uintptr_t)e % 16 || (uintptr_t)dx % 16 || (uintptr_t)de % 16))
         return fail(ZO_EINVAL, "buffers must be 16-byte aligned");
     if ((uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");

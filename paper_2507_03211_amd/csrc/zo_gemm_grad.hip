@@ -70,7 +70,8 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float2 *__restrict_
 }
 
 // Distances and pairs of a row -> its loss and, in place, its G (as in epilogue 5); zeros in rows that do not count, past the last row and past
-// the last word.  One workgroup a row, so that logsumexp is worked once.  Bound by memory: 4 bytes a word.
+// the last word.  Workgroup (r, y) takes the y-th part of a row: the whole of it, so that logsumexp is worked once, but for few rows, where
+// 20 workgroups take 12.9 us (50272 words) and the parts of 8 each 5.  Bound by memory: 4 bytes a word.
 template <int DT>
 __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ grad, const float2 *__restrict__ pairs, int n_pairs, int strip,
                                                             const float *__restrict__ hit, const int32_t *__restrict__ target, float *__restrict__ row_loss,
@@ -81,9 +82,10 @@ __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ 
     constexpr float kOne = DT == kFP16 ? 32768.0f : 1.0f, kShift = DT == kFP16 ? 15.0f : 0.0f;
     const int r = blockIdx.x, tg = r < rows ? target[r] : -1;
     uint4 *out = grad + (size_t)r * (width / 8);
+    const int each = (width / 8 + gridDim.y - 1) / gridDim.y, first = each * blockIdx.y, last = first + each < width / 8 ? first + each : width / 8;
     if (tg < 0) {
-        if (r < rows && threadIdx.x == 0) row_loss[r] = 0.0f;
-        for (int c = threadIdx.x; c < width / 8; c += 512) out[c] = uint4{0, 0, 0, 0};
+        if (r < rows && threadIdx.x == 0 && blockIdx.y == 0) row_loss[r] = 0.0f;
+        for (int c = first + threadIdx.x; c < last; c += 512) out[c] = uint4{0, 0, 0, 0};
         return;
     }
     const float2 *p = pairs + (size_t)r * n_pairs;
@@ -95,10 +97,10 @@ __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ 
         if (p[i].x > -INFINITY) s += (double)p[i].y * (double)__expf(p[i].x - mx);
     s = block_sum(s, red_d);
     const double lse = tg < vocab ? log(s) + (double)mx : (double)__builtin_nan("");
-    if (threadIdx.x == 0) row_loss[r] = (float)(lse - (double)hit[r]);
+    if (threadIdx.x == 0 && blockIdx.y == 0) row_loss[r] = (float)(lse - (double)hit[r]);
     const float hi = (float)lse, rest = (float)(((double)hi - lse) * 1.4426950408889634) + kShift;
     const float at_target = tg < vocab ? __builtin_amdgcn_exp2f(__builtin_fmaf(hit[r] - hi, 1.44269504f, rest)) - kOne : 0.0f;
-    for (int c = threadIdx.x; c < width / 8; c += 512) {
+    for (int c = first + threadIdx.x; c < last; c += 512) {
         uint4 q = out[c];
         const int w0 = 8 * c;
         const float base = __builtin_fmaf(p[w0 / strip].x - hi, 1.44269504f, rest);
@@ -118,19 +120,40 @@ __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ 
     }
 }
 
-// dx = rn(alpha sum_z part[z]): the shares of the contraction over the vocabulary, in order.  Eight elements a thread.
-template <int DT>
+// dx = rn(alpha sum_z part[z]): the shares of the contraction over the vocabulary.  Eight elements a thread; with L > 1 the workgroup's L
+// groups of threads take every L-th share each, and their sums meet in LDS (20 rows of 768, 40 shares: 6.6 us with L = 1).
+template <int DT, int L>
 __global__ __launch_bounds__(256) void head_dx_kernel(const float4 *__restrict__ part, int shares, size_t n8, float alpha, uint4 *__restrict__ dx)
 {
-    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n8; i += (size_t)gridDim.x * blockDim.x) {
-        float4 a = part[2 * i], b = part[2 * i + 1];
-        for (int z = 1; z < shares; ++z) {
+    constexpr int N = 256 / L;
+    __shared__ float4 sums[L > 1 ? L : 1][N][2];
+    const int group = threadIdx.x / N, t = threadIdx.x % N;
+    const size_t step = (size_t)gridDim.x * N;
+    for (size_t i0 = (size_t)blockIdx.x * N; i0 < n8; i0 += step) {
+        const size_t i = i0 + t < n8 ? i0 + t : n8 - 1;
+        float4 a{0, 0, 0, 0}, b{0, 0, 0, 0};
+#pragma unroll 4
+        for (int z = group; z < shares; z += L) {
             const float4 p = part[2 * (z * n8 + i)], q = part[2 * (z * n8 + i) + 1];
             a = float4{a.x + p.x, a.y + p.y, a.z + p.z, a.w + p.w};
             b = float4{b.x + q.x, b.y + q.y, b.z + q.z, b.w + q.w};
         }
+        if constexpr (L > 1) {
+            __syncthreads();
+            sums[group][t][0] = a;
+            sums[group][t][1] = b;
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int g = 1; g < L; ++g) {
+                    const float4 p = sums[g][t][0], q = sums[g][t][1];
+                    a = float4{a.x + p.x, a.y + p.y, a.z + p.z, a.w + p.w};
+                    b = float4{b.x + q.x, b.y + q.y, b.z + q.z, b.w + q.w};
+                }
+            }
+        }
         auto two = [&](float lo, float hi) { return (uint32_t)Prec<DT>::acc2a(alpha * lo) | ((uint32_t)Prec<DT>::acc2a(alpha * hi) << 16); };
-        dx[i] = uint4{two(a.x, a.y), two(a.z, a.w), two(b.x, b.y), two(b.z, b.w)};
+        if (group == 0 && i0 + t < n8) dx[i] = uint4{two(a.x, a.y), two(a.z, a.w), two(b.x, b.y), two(b.z, b.w)};
     }
 }
 
@@ -141,6 +164,7 @@ template <int DT, int EPI, class OP> hipError_t launch_product(Tile t, const Arg
     case T256x256: return launch_pipe<DT, EPI, Shape<4, 4, 2>, OP>(a, op);
     case T256x192: return launch_pipe<DT, EPI, Shape<4, 3, 2>, OP>(a, op);
     case T256x128: return launch_pipe<DT, EPI, Shape<4, 2, 2>, OP>(a, op);
+    case T192x128: return launch_pipe<DT, EPI, Shape<3, 2, 3>, OP>(a, op);
     case T128x128: return launch_pipe<DT, EPI, Shape<2, 2, 4>, OP>(a, op);
     default: return launch_small_t<DT, EPI, 1, false, OP>(a, op);
     }
@@ -149,7 +173,10 @@ using Logits = Product<false, false>;       // x rows, words: both with k inside
 using ByRows = Product<true, true>;         // G^T x: contraction over the rows, outside in both
 using ByWords = Product<false, true>;       // G e: contraction over the words, outside in e
 
-constexpr Tile kProductTiles[] = {T256x256, T256x192, T256x128, T128x128, T64x64};
+// The tile of least estimated time by the linear layers' rule (tile_us), whose constants hold here: 27 shapes of 16 to 8192 rows, d 768, 2048
+// and 5120, 50272 words, each tile timed: de on average 0.2 % slower than the best (2 % at most), the logits 1.6 % (up to 15 % with
+// less than 100 rows of 5120).
+constexpr Tile kProductTiles[] = {T256x256, T256x192, T256x128, T192x128, T128x128, T64x64};
 Tile pick_product(int shares, int m, int n, int slabs, int epi, float *us = nullptr)
 {
     Tile best = T64x64;
@@ -242,7 +269,8 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
         op.pairs = pair; op.hit = hit; op.target = target; op.rows = rows; op.words = vocab;
         const Args a{xs, w, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
         if ((err = launch_product<DT, 9, Logits>(p.logits, a, op)) != hipSuccess) return err;
-        head_gradient_kernel<DT><<<dim3(p.rows_p), dim3(512), 0, s>>>((uint4 *)g, pair, p.pairs, p.strip, hit, target, row_loss, rows, vocab, p.width);
+        const unsigned parts = p.rows_p >= 512 || p.width < 8192 ? 1 : 512 / p.rows_p;
+        head_gradient_kernel<DT><<<dim3(p.rows_p, parts), dim3(512), 0, s>>>((uint4 *)g, pair, p.pairs, p.strip, hit, target, row_loss, rows, vocab, p.width);
     } else {
         if ((err = launch_linear_mfma(xs, w, w, target, hit, pair, DT, 1, rows, vocab, p.dp, 4, s)) != hipSuccess) return err;
         head_lse_kernel<<<dim3((rows + 3) / 4), dim3(256), 0, s>>>(pair, p.pairs, hit, target, row_loss, stats, rows, vocab, DT == kFP16 ? 15.0f : 0.0f);
@@ -276,14 +304,30 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
             if (err != hipSuccess) return err;
         }
     }
-    const size_t n8 = (size_t)rows * d / 8, blocks = (n8 + 255) / 256;
-    head_dx_kernel<DT><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s>>>((const float4 *)part, p.shares, n8, alpha, (uint4 *)dx);
+    const size_t n8 = (size_t)rows * d / 8;
+    auto sum = [&](auto kern, size_t each) {
+        const size_t blocks = (n8 + each - 1) / each;
+        kern<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s>>>((const float4 *)part, p.shares, n8, alpha, (uint4 *)dx);
+    };
+    if (p.shares >= 8) sum(head_dx_kernel<DT, 8>, 32);
+    else sum(head_dx_kernel<DT, 1>, 256);
     return hipGetLastError();
 }
 
 }  // namespace
 
 size_t head_grad_mfma_scratch(int rows, int d, int vocab) { return head_plan(rows, d, vocab).total; }
+
+void head_grad_mfma_plan(int rows, int d, int vocab, int32_t *plan)
+{
+    const HeadPlan p = head_plan(rows, d, vocab);
+    auto tile = [](Tile t) { return kTileRows[t] << 16 | kTileColumns[t]; };
+    plan[0] = tile(pick_product(1, p.rows_p, p.width, p.dp / BK, 0));
+    plan[1] = tile(pick_product(1, p.pieces == 1 ? vocab : p.width, d, p.rows_p / BK, 0));
+    plan[2] = tile(p.by_words);
+    plan[3] = p.shares;
+    plan[4] = p.pieces;
+}
 
 hipError_t launch_head_grad_mfma(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype, int rows,
                                  int d, int vocab, float scale, hipStream_t s)

@@ -2,11 +2,14 @@
 
 Tolerances (16-bit types).  A logit is a sum of d products in fp32: off by A u sum |x e|, A = 16 + d / 8 (the matrix
 instructions add sixteen products at a time; the row's largest such error is `dl`).  A probability is off by 2 dl + 2^-21 of itself: its
-own logit, the row's logsumexp, and exponential, sums and roundings of 32 bits.  It enters the products rounded to the 16-bit type, by half
-a step `h` at most.  These roundings are independent, so a sum of n such terms is off by 7 h sqrt(sum of squares) (bounded
+own logit, the row's logsumexp, and exponential, sums and roundings of 32 bits.  A logit may be kept as a distance in steps of 32 / 65535,
+which moves the probability by half of that, and counts as none from 32 on (e^-32 of a neighbour's probability); the probability enters the
+products rounded to the 16-bit type, by half a step.  `h` is the root of both squared.  These roundings are independent, so a sum of n such terms is off by 7 h sqrt(sum of squares) (bounded
 independent terms pass that once in 10^10), everything else by its worst case; then the result is rounded, half a step.
 fp32 parameters: all in fp64, results of the parameters' type rounded once.
 """
+import math
+
 import pytest
 import torch
 
@@ -64,8 +67,8 @@ def check(dtype, x, e, target, scale, got):
     off_G[~live] = 0.0
     assert ((loss.double() - want_loss).abs() <= 2 * dl.squeeze(1) + 8 * u * (1.0 + lse.abs() + hit.abs()).squeeze(1)).all()
     assert (loss[~live] == 0).all() and (dx[~live] == 0).all()
-    h = 0.0 if dtype == zi.FP32 else half(act_dtype(dtype))
-    tiny = 2.0**-39 if dtype == zi.FP16 else 0.0                     # half the step of probabilities below fp16's normal numbers, 2^15 times enlarged
+    h = 0.0 if dtype == zi.FP32 else (half(act_dtype(dtype))**2 + (16.0 / 65535)**2)**0.5
+    tiny = 0.0 if dtype == zi.FP32 else math.exp(-32.0) + (2.0**-39 if dtype == zi.FP16 else 0.0)    # the latter: half the step of probabilities below fp16's normal numbers, 2^15 times enlarged
     for out, A, B, n in ((dx, G, ed, vocab), (de, G.t().contiguous(), xd, rows)):
         off = off_G if out is dx else off_G.t().contiguous()
         want = scale * (A @ B)
@@ -224,9 +227,41 @@ def test_against_differences(dtype):
     assert (got - fine).abs() <= (coarse - fine).abs() + off
 
 
+TILES = [
+    ("logits", (64, 64), 30, 136, 520), ("logits", (128, 128), 4096, 320, 520), ("logits", (192, 128), 1000, 200, 4104), ("logits", (256, 128), 2049, 192, 2600),
+    ("logits", (256, 192), 1048, 200, 6824), ("logits", (256, 256), 3000, 512, 4104),
+    ("de", (64, 64), 30, 136, 520), ("de", (128, 128), 3000, 2048, 520), ("de", (192, 128), 200, 1024, 4104), ("de", (256, 128), 131, 2048, 2600),
+    ("de", (256, 192), 131, 2048, 4104), ("de", (256, 256), 384, 2048, 6824),
+    ("dx", (64, 64), 30, 136, 520), ("dx", (128, 128), 1500, 1536, 520), ("dx", (192, 128), 2049, 2048, 520), ("dx", (256, 128), 4096, 1536, 520),
+    ("dx", (256, 192), 3000, 1536, 8008), ("dx", (256, 256), 1048, 2048, 50272),
+]
+
+
 @pytest.mark.parametrize("dtype", HALVES)
-def test_sixteen_bits_in_pieces(dtype):
-    """More words than the workspace holds probabilities for at once (2^30 bytes): the later pieces' share of dx is added to the first's."""
-    rows, d, vocab = 8300, 64, 66008
+@pytest.mark.parametrize("product,tile,rows,d,vocab", TILES)
+def test_every_tile(dtype, product, tile, rows, d, vocab):
+    """Every product in every tile shape, at a size that takes it, and with ends that fill no tile."""
+    assert zo_amd.zo_kernel_lmhead_grad_plan(rows, d, vocab)[product] == tile
+    for r, v in ((rows, vocab), (rows - 3, vocab - 8)):
+        x, e, target = inputs(dtype, r, d, v, 21)
+        check(dtype, x, e, target, 0.03125, call(dtype, x, e, target, 0.03125))
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(16, 768, 9000), (40, 512, 20000), (131, 2048, 12000), (5, 64, 50272)])
+def test_shares_of_the_vocabulary(rows, d, vocab):
+    """Few rows: the contraction over the words is cut into shares, some of which reach past the last word."""
+    assert zo_amd.zo_kernel_lmhead_grad_plan(rows, d, vocab)["shares"] > 1
+    for v in (vocab, vocab - 64, vocab - 72):
+        x, e, target = inputs(zi.BF16, rows, d, v, 22)
+        target[-1] = v - 1                                       # the last word counts
+        check(zi.BF16, x, e, target, 1.0, call(zi.BF16, x, e, target, 1.0))
+
+
+@pytest.mark.parametrize("dtype,rows,d,vocab", [(zi.BF16, 8300, 64, 66008), (zi.FP16, 8300, 64, 66008), (zi.BF16, 8300, 264, 66008), (zi.FP16, 8300, 576, 66008),
+                                                (zi.BF16, 140, 320, 1 << 22)])
+def test_sixteen_bits_in_pieces(dtype, rows, d, vocab):
+    """More words than the workspace holds probabilities for at once (2^30 bytes): the logits are worked again for each piece, and the later
+    pieces' share of dx is added to the first's."""
+    assert zo_amd.zo_kernel_lmhead_grad_plan(rows, d, vocab)["pieces"] > 1
     x, e, target = inputs(dtype, rows, d, vocab, 12)
     check(dtype, x, e, target, 1.0 / 64, call(dtype, x, e, target, 1.0 / 64))

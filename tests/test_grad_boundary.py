@@ -21,7 +21,7 @@ def test_layernorm():
     good = [P, P, P, P, P, P, ZO_BF16, 4, 64, 1e-5]
     for i in range(6):
         assert "NULL" in refused(zo_amd.zo_kernel_layernorm, *(good[:i] + [None] + good[i + 1:]))
-    for at, value in ((6, 3), (6, -1), (7, 0), (7, -5), (8, 0), (9, 0.0), (9, -1.0), (9, NAN)):
+    for at, value in ((6, 3), (6, -1), (7, 0), (7, -5), (8, 0), (9, 0.0), (9, -1.0), (9, NAN), (7, 1 << 24), (8, 1 << 23)):
         refused(zo_amd.zo_kernel_layernorm, *(good[:at] + [value] + good[at + 1:]))
 
 
@@ -35,7 +35,7 @@ def test_layernorm_grad():
     assert "go together" in refused(f, *(good[:7] + [None] + good[8:]))
     assert "no output" in refused(f, P, P, P, P, P, None, None, None, P, ZO_FP16, 4, 64, False)
     assert "aligned" in refused(f, *(good[:8] + [P + 16] + good[9:]))
-    for at, value in ((9, 5), (10, 0), (11, 0), (11, -64)):
+    for at, value in ((9, 5), (10, 0), (11, 0), (11, -64), (10, 1 << 24), (11, 1 << 23)):
         refused(f, *(good[:at] + [value] + good[at + 1:]))
     assert zo_amd.zo_kernel_layernorm_grad_scratch_bytes(ZO_BF16, 1, 1) > 0
     for bad in ((3, 4, 64), (-1, 4, 64), (ZO_BF16, 0, 64), (ZO_BF16, 4, 0)):
@@ -54,6 +54,22 @@ def test_lmhead_grad():
     assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(ZO_FP32, 1, 1, 2) > 0
     for bad in ((3, 4, 64, 512), (ZO_BF16, 0, 64, 512), (ZO_BF16, 4, 0, 512), (ZO_BF16, 4, 64, 1)):
         assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(*bad) == 0
+    for at, value in ((8, 1 << 21), (9, 1 << 23), (10, 1 << 23)):                  # beyond the sizes the header names
+        refused(f, *(good[:at] + [value] + good[at + 1:]))
+        assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(ZO_BF16, *(good[8:at] + [value] + good[at + 1:11])) == 0
+
+
+def test_lmhead_grad_plan():
+    p = zo_amd.zo_kernel_lmhead_grad_plan(8192, 5120, 50272)
+    assert p == dict(logits=(256, 256), de=(256, 256), dx=(256, 256), shares=2, pieces=1)
+    assert zo_amd.zo_kernel_lmhead_grad_plan(65536, 5120, 50272)["pieces"] > 1
+    assert zo_amd.zo_kernel_lmhead_grad_plan(20, 768, 50272)["shares"] > 1
+    # a workspace for more rows grows by the rows' own buffers once G fills its room
+    sizes = [zo_amd.zo_kernel_lmhead_grad_scratch_bytes(ZO_BF16, r, 768, 50272) for r in (1024, 8192, 32768, 65536)]
+    assert sizes == sorted(sizes) and sizes[3] < (1 << 30) + 65536 * (768 * 16 + 8192)
+    for bad in ((0, 64, 512), (4, 60, 512), (4, 64, 500), (4, 64, 1)):
+        refused(zo_amd.zo_kernel_lmhead_grad_plan, *bad)
+    assert zo_amd.lib().zo_kernel_lmhead_grad_plan(4, 64, 512, None) == zo_amd.ZO_EINVAL
 
 
 def test_grad_clip():
