@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void head_rows_kernel(const uint16_t *__restri
     for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < (size_t)rows_p * per_row; i += (size_t)gridDim.x * blockDim.x) {
         const int r = (int)(i / per_row), c = (int)(i % per_row) * 8;
         uint4 v{0, 0, 0, 0};
-        if (r < rows && c < d && (!target || target[r] >= 0)) v = *(const uint4 *)(x + (size_t)r * d + c);
+        if (r < rows && c < d && target[r] >= 0) v = *(const uint4 *)(x + (size_t)r * d + c);
         out[i] = v;
     }
 }
@@ -198,7 +198,7 @@ constexpr size_t kPieceBytes = 1u << 30;
 struct HeadPlan {
     int rows_p, dp, width, pieces, shares, share_words, pairs, strip;
     Tile logits, by_words;
-    size_t xs, es, g, stats, pair, hit, part, total;
+    size_t xs, g, stats, pair, hit, part, total;
 };
 HeadPlan head_plan(int rows, int d, int vocab)
 {
@@ -220,17 +220,13 @@ HeadPlan head_plan(int rows, int d, int vocab)
     p.share_words = (slabs + p.shares - 1) / p.shares * BK;
     p.width = p.share_words * p.shares;
     p.pieces = (vocab + p.width - 1) / p.width;
-    if (p.pieces == 1) {
-        p.logits = pick_product(1, p.rows_p, p.width, p.dp / BK, 0);
-        p.strip = kTileColumns[p.logits] / 2;                    // a wavefront's columns of the tile
-        p.pairs = 2 * ((p.width + kTileColumns[p.logits] - 1) / kTileColumns[p.logits]);
-    } else {
-        p.pairs = mfma_ce_partials(1, rows, vocab, p.dp);
-    }
+    const int columns = p.pieces == 1 ? p.width : vocab;          // of the first product
+    p.logits = pick_product(1, p.rows_p, columns, p.dp / BK, 0);
+    p.strip = kTileColumns[p.logits] / 2;                        // a wavefront's columns of the tile
+    p.pairs = 2 * ((columns + kTileColumns[p.logits] - 1) / kTileColumns[p.logits]);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up(o + bytes); return at; };
     p.xs = take(2 * (size_t)p.rows_p * p.dp);
-    p.es = p.dp == d ? 0 : take(2 * (size_t)vocab * p.dp);
     p.stats = p.pieces == 1 ? 0 : take((size_t)rows * sizeof(float2));
     p.pair = take((size_t)rows * p.pairs * 8);
     p.hit = take(4 * (size_t)rows);
@@ -250,39 +246,37 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
     float *part = (float *)(ws + p.part);
     const float alpha = DT == kFP16 ? scale * 0x1p-15f : scale;
     hipError_t err = hipSuccess;
-    auto copy = [&](const uint16_t *from, const int32_t *tg, uint16_t *to, int n, int n_p) {
-        const size_t blocks = ((size_t)n_p * (p.dp / 8) + 255) / 256;
-        head_rows_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s>>>(from, tg, (uint4 *)to, n, n_p, d, p.dp);
-        return hipGetLastError();
+    const size_t copy_blocks = ((size_t)p.rows_p * (p.dp / 8) + 255) / 256;
+    head_rows_kernel<<<dim3((unsigned)(copy_blocks < 4096 ? copy_blocks : 4096)), dim3(256), 0, s>>>(x, target, (uint4 *)xs, rows, p.rows_p, d, p.dp);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+    auto logits_of = [&](int v0, int words) {
+        Logits::Arg op{};
+        op.ldx = p.dp;
+        op.ldw = op.w_row = d;
+        op.w_end = (uint64_t)(uintptr_t)(e + (size_t)vocab * d);
+        op.stats = stats; op.target = target; op.rows = rows; op.words = words; op.first_word = v0;
+        return op;
     };
-    if ((err = copy(x, target, xs, rows, p.rows_p)) != hipSuccess) return err;
-    const uint16_t *w = e;                                       // words with rows of dp
-    if (p.dp != d) {
-        if ((err = copy(e, nullptr, (uint16_t *)(ws + p.es), vocab, vocab)) != hipSuccess) return err;
-        w = (const uint16_t *)(ws + p.es);
-    }
     float2 *pair = (float2 *)(ws + p.pair);
     float *hit = (float *)(ws + p.hit);
     if (p.pieces == 1) {
-        Logits::Arg op{};
-        op.ldx = op.ldw = p.dp;
-        op.pairs = pair; op.hit = hit; op.target = target; op.rows = rows; op.words = vocab;
-        const Args a{xs, w, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
+        Logits::Arg op = logits_of(0, vocab);
+        op.pairs = pair; op.hit = hit;
+        const Args a{xs, e, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
         if ((err = launch_product<DT, 9, Logits>(p.logits, a, op)) != hipSuccess) return err;
         const unsigned parts = p.rows_p >= 512 || p.width < 8192 ? 1 : 512 / p.rows_p;
         head_gradient_kernel<DT><<<dim3(p.rows_p, parts), dim3(512), 0, s>>>((uint4 *)g, pair, p.pairs, p.strip, hit, target, row_loss, rows, vocab, p.width);
     } else {
-        if ((err = launch_linear_mfma(xs, w, w, target, hit, pair, DT, 1, rows, vocab, p.dp, 4, s)) != hipSuccess) return err;
+        const Args a{xs, e, nullptr, target, hit, pair, 1, rows, vocab, p.dp, s};
+        if ((err = launch_product<DT, 4, Logits>(p.logits, a, logits_of(0, vocab))) != hipSuccess) return err;
         head_lse_kernel<<<dim3((rows + 3) / 4), dim3(256), 0, s>>>(pair, p.pairs, hit, target, row_loss, stats, rows, vocab, DT == kFP16 ? 15.0f : 0.0f);
     }
     if ((err = hipGetLastError()) != hipSuccess) return err;
     for (int v0 = 0; v0 < vocab; v0 += p.width) {
         const int words = vocab - v0 < p.width ? vocab - v0 : p.width;
         if (p.pieces > 1) {
-            Logits::Arg op{};
-            op.ldx = op.ldw = p.dp;
-            op.stats = stats; op.target = target; op.rows = rows; op.words = words; op.first_word = v0;
-            const Args a{xs, w + (size_t)v0 * p.dp, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
+            const Logits::Arg op = logits_of(v0, words);
+            const Args a{xs, e + (size_t)v0 * d, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
             if ((err = launch_product<DT, 5, Logits>(pick_product(1, p.rows_p, p.width, p.dp / BK, 0), a, op)) != hipSuccess) return err;
         }
         {

@@ -24,15 +24,17 @@ constexpr int BK = 64;                      // contraction slab; k is a multiple
 // Product<XK, WK>: rows at a stride of their own, or (XK, WK) with the contraction as the outer index, element (i, k) at
 // [k * stride + i]; `sign` then counts shares of the contraction, each with a partial result of its own.  Shares begin
 // xz / wz elements apart.  An operand with k outside is read through a buffer that ends where its memory does (x_end, w_end: addresses):
-// k beyond it are zeros.
+// k beyond it are zeros.  So is a w with k inside, whose rows may end inside the last slab (kRagged): the lanes whose 16 bytes lie past the
+// row's w_row elements ask for what lies past the buffer.
 struct Plain {
-    static constexpr bool kPlain = true, kXK = false, kWK = false;
+    static constexpr bool kPlain = true, kXK = false, kWK = false, kRagged = false;
     struct Arg {};
 };
 template <bool XK, bool WK> struct Product {
-    static constexpr bool kPlain = false, kXK = XK, kWK = WK;
+    static constexpr bool kPlain = false, kXK = XK, kWK = WK, kRagged = !WK;
     struct Arg {
         uint64_t ldx, ldw, xz, wz, x_end, w_end;
+        int w_row;
         float alpha;                        // epilogue 6: factor of the result
         // epilogues 5 and 9
         const float2 *stats;                // 5: per row, logsumexp (rounded; infinity in rows that do not count) and what goes on top of the exponent
@@ -598,7 +600,7 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
         else return base + 2u * (uint32_t)(slab * BK);
     };
     auto source_x = [&](uint64_t base) { if constexpr (XK) return slab_source<true>(base, op.x_end); else return base; };
-    auto source_w = [&](uint64_t base) { if constexpr (WK) return slab_source<true>(base, op.w_end); else return base; };
+    auto source_w = [&](uint64_t base) { if constexpr (WK || OP::kRagged) return slab_source<true>(base, op.w_end); else return base; };
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4 *)smem;
     const int nk = k / BK;                              // > A (the launcher sees to it)
     // Slabs are numbered through all the tiles of this workgroup.  x slab g lives in x stage g % (A + 1), w slab g in w
@@ -641,6 +643,14 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
             else wf[t] = ws[wrow + t * 256 + slot];
         }
     };
+    // ragged rows of w: what a lane's offsets get in the slab being loaded (a row's chunks are swizzled by two patterns, by the load's parity)
+    uint32_t w_past[2] = {0, 0};
+    auto ragged_slab = [&](bool last) {
+        if constexpr (OP::kRagged) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) w_past[q] = last && (nk - 1) * BK + (lslot ^ (4 * q + (lrow >> 1))) * 8 >= op.w_row ? 0x80000000u : 0u;
+        }
+    };
     // Multiplies j0 .. j1-1 of the TM x TN fragment product of set (wf, xf), quarter q of the slab.  Before multiply j go
     // out: the fragment reads that SH::reads has due there, of set (nwf, nxf) for k-step nks of the slab in stages (nxst,
     // nwst); the global->LDS load that SH::xloads / SH::wloads has due at slot s0 + j, into LDS at `st`.
@@ -659,7 +669,10 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
             const int l0 = is_x ? SH::xloads(s0 + j) : SH::wloads(s0 + j), l1 = is_x ? SH::xloads(s0 + j + 1) : SH::wloads(s0 + j + 1);
             if (l1 > l0) {
 #pragma unroll
-                for (int l = l0; l < l1; ++l) gload_lds16(gbase, offs[l], st + l * 1024u);
+                for (int l = l0; l < l1; ++l) {
+                    if (OP::kRagged && !is_x) gload_lds16(gbase, offs[l] | w_past[l & 1], st + l * 1024u);
+                    else gload_lds16(gbase, offs[l], st + l * 1024u);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             // back and forth over the activation fragments, so that one operand changes from one multiply to
@@ -690,7 +703,8 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
     // the lane offsets (xo, wo).  x(g+A) goes into the activation stage that slab g-1 left at the previous barrier:
     // its loads sit under the multiplies before this slab's barrier; w(g+A) can only follow the barrier: its
     // loads sit under the multiplies after it.
-    auto slab = [&](uint64_t xat, uint64_t wat, const uint32_t (&xo)[LX], const uint32_t (&wo)[LW], bool first) {
+    auto slab = [&](uint64_t xat, uint64_t wat, const uint32_t (&xo)[LX], const uint32_t (&wo)[LW], bool first, bool last = false) {
+        ragged_slab(last);
         const auto xb = source_x(xat);
         const auto wb = source_w(wat);
         const uint32_t stx = lds_x(xfree), stw = lds_w(ws0);
@@ -750,9 +764,9 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
             nxt.wbase = at_w(nxt.wbase, nk - A);
         }
         // all slabs but the last A load A slabs ahead in this tile; the first one starts the accumulators
-        slab(at_x(cur.xbase, A), at_w(cur.wbase, A), cur.xg, cur.wg, true);
+        slab(at_x(cur.xbase, A), at_w(cur.wbase, A), cur.xg, cur.wg, true, A == nk - 1);
         for (int kt = 1; kt < nk - A; ++kt)
-            slab(at_x(cur.xbase, kt + A), at_w(cur.wbase, kt + A), cur.xg, cur.wg, false);
+            slab(at_x(cur.xbase, kt + A), at_w(cur.wbase, kt + A), cur.xg, cur.wg, false, kt + A == nk - 1);
         // the last A load the first A slabs of the next tile
 #pragma unroll
         for (int g = 0; g < A; ++g)
@@ -856,14 +870,23 @@ __global__ __launch_bounds__(256, 2) void linear_mfma_small_kernel(
         }
     }
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4 *)smem;
+    // a load of w's whose 16 bytes lie past the end of a ragged row
+    auto past = [&](int slab, int i) {
+        if constexpr (OP::kRagged) return slab * BK + (int)((lane & 7) ^ swz((wave * LW + i - LX) * 8 + (lane >> 3))) * 8 >= op.w_row;
+        else return false;
+    };
     auto load_slab = [&](int slab, uint32_t stage) {
         const uint32_t st = lds_base + stage * kStageBytes, adv = (uint32_t)slab * (BK * 2);
         const auto xs = [&] { if constexpr (XK) return slab_source<true>(xbase + (uint64_t)adv * op.ldx, op.x_end); else return xbase + adv; }();
-        const auto ws = [&] { if constexpr (WK) return slab_source<true>(wbase + (uint64_t)adv * op.ldw, op.w_end); else return wbase + adv; }();
+        const auto ws = [&] {
+            if constexpr (WK) return slab_source<true>(wbase + (uint64_t)adv * op.ldw, op.w_end);
+            else if constexpr (OP::kRagged) return slab_source<true>(wbase + adv, op.w_end);
+            else return wbase + adv;
+        }();
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             if (i < LX) gload_lds16(xs, off[i], st + (uint32_t)(wave * LX + i) * 1024u);
-            else gload_lds16(ws, off[i], st + (uint32_t)(BM / 8 + wave * LW + i - LX) * 1024u);
+            else gload_lds16(ws, past(slab, i) ? off[i] | 0x80000000u : off[i], st + (uint32_t)(BM / 8 + wave * LW + i - LX) * 1024u);
         }
     };
 
