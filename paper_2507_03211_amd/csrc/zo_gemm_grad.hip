@@ -173,22 +173,65 @@ using Logits = Product<false, false>;       // x rows, words: both with k inside
 using ByRows = Product<true, true>;         // G^T x: contraction over the rows, outside in both
 using ByWords = Product<false, true>;       // G e: contraction over the words, outside in e
 
-// The tile of least estimated time by the linear layers' rule (tile_us), whose constants hold here: 27 shapes of 16 to 8192 rows, d 768, 2048
-// and 5120, 50272 words, each tile timed: de on average 0.2 % slower than the best (2 % at most), the logits 1.6 % (up to 15 % with
-// less than 100 rows of 5120).
+// The tile of least estimated time in us: start + slabs (rounds slab + full busy) + rounds round + operand MB operand + output MB output,
+// where a round of tiles that fills more than half of the CUs also pays slabs busy b, b = 0 .. 1 from half full to full (64 x 64 tiles, two
+// on a CU: slab for one alone, busy for two).  Constants: least relative squares over 2674 shapes (8 - 8192 rows, d 128 - 5120, vocabularies
+// 2 k - 50 k, operands far), every tile of each product timed, for dx with 1 - 40 shares and its sum's launch; shapes' best and up to 1.6 times
+// it.  The pick against the best: logits 1.2 % slower on average (one shape in 25 more than 10 %), de 0.3 %, dx 1.8 %; by the linear
+// layers' constants 1.7, 0.9 and 3.5 %.
+enum ProductKind { kLogits, kByRows, kByWords };
 constexpr Tile kProductTiles[] = {T256x256, T256x192, T256x128, T192x128, T128x128, T64x64};
-Tile pick_product(int shares, int m, int n, int slabs, int epi, float *us = nullptr)
+constexpr int kLeastSlabs[] = {3, 3, 3, 4, 5, 1};
+static const struct { float start, slab, busy, round, operand, output; } kProductCost[3][6] = {
+    {{7.99f, 1.06f, 0.45f, 2.54f, 0.021f, 0.210f},
+     {4.52f, 0.82f, 0.35f, 5.09f, 0.032f, 0.105f},
+     {3.06f, 0.65f, 0.19f, 3.58f, 0.045f, 0.170f},
+     {3.28f, 0.47f, 0.22f, 2.87f, 0.054f, 0.161f},
+     {2.82f, 0.41f, 0.12f, 1.44f, 0.076f, 0.271f},
+     {2.28f, 0.25f, 0.43f, 1.76f, 0.091f, 0.000f}},
+    {{2.47f, 1.12f, 0.33f, 3.66f, 0.015f, 0.069f},
+     {3.59f, 0.85f, 0.35f, 2.47f, 0.020f, 0.041f},
+     {3.19f, 0.60f, 0.28f, 1.98f, 0.045f, 0.000f},
+     {3.35f, 0.51f, 0.20f, 1.48f, 0.020f, 0.000f},
+     {3.23f, 0.40f, 0.14f, 0.92f, 0.019f, 0.000f},
+     {3.46f, 0.23f, 0.41f, 0.23f, 0.000f, 0.069f}},
+    {{3.61f, 1.00f, 0.47f, 4.50f, 0.030f, 0.078f},
+     {3.81f, 0.80f, 0.37f, 2.88f, 0.024f, 0.086f},
+     {2.81f, 0.65f, 0.22f, 1.80f, 0.023f, 0.112f},
+     {3.13f, 0.47f, 0.24f, 1.62f, 0.032f, 0.101f},
+     {2.87f, 0.38f, 0.16f, 1.26f, 0.056f, 0.063f},
+     {2.58f, 0.20f, 0.38f, 0.20f, 0.095f, 0.141f}},
+};
+float product_us(ProductKind kind, int t, int shares, int m, int n, int n_slabs)
+{
+    const auto &c = kProductCost[kind][t];
+    const float n_cu = cu_count() ? (float)cu_count() : 256.0f, slabs = (float)n_slabs, slots = t == T64x64 ? 2 * n_cu : n_cu;
+    const float tiles = (float)shares * (float)((m + kTileRows[t] - 1) / kTileRows[t]) * (float)((n + kTileColumns[t] - 1) / kTileColumns[t]);
+    const float full = __builtin_floorf(tiles / slots), part = tiles / slots - full, rounds = full + (part > 0 ? 1.0f : 0.0f);
+    const float operand_mb = ((float)m + (float)n) * slabs * (float)shares * (BK * 2e-6f), output_mb = (float)m * (float)n * (float)shares * (kind == kByWords ? 4e-6f : 2e-6f);
+    float us = c.start + rounds * c.round + operand_mb * c.operand + output_mb * c.output;
+    if (t == T64x64) {
+        const float lone = part > 0 && part <= 0.5f ? 1.0f : 0.0f;
+        us += slabs * ((rounds - lone) * c.busy + lone * c.slab);
+    } else {
+        us += slabs * (rounds * c.slab + (full + (part > 0.5f ? 2 * part - 1 : 0.0f)) * c.busy);
+    }
+    return us;
+}
+Tile pick_product(ProductKind kind, int shares, int m, int n, int slabs, float *us = nullptr)
 {
     Tile best = T64x64;
     float best_us = 0.0f;
     for (Tile t : kProductTiles) {
-        if (!tile_fits(t, slabs)) continue;
-        const float v = tile_us(t, shares, m, n, slabs, epi);
+        if (slabs < kLeastSlabs[t]) continue;
+        const float v = product_us(kind, t, shares, m, n, slabs);
         if (best_us == 0.0f || v < best_us) { best = t; best_us = v; }
     }
     if (us) *us = best_us;
     return best;
 }
+// of the launch that adds up dx's shares
+float shares_us(int shares, int rows, int d) { return 3.1f + (float)shares * (float)rows * (float)d * (4e-6f * 0.117f) + (shares < 8 ? 0.014f * (float)shares : 0.0f); }
 
 size_t up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
 
@@ -213,15 +256,15 @@ HeadPlan head_plan(int rows, int d, int vocab)
     float best = 0.0f;
     for (int z = 1; z <= 64 && z <= slabs; z += z < 8 ? 1 : z < 16 ? 2 : 4) {
         float us;
-        const Tile t = pick_product(z, rows, d, (slabs + z - 1) / z, 3, &us);
-        us += 4.0f + (float)z * (float)rows * (float)d * 8.0f / 4.0e6f;
+        const Tile t = pick_product(kByWords, z, rows, d, (slabs + z - 1) / z, &us);
+        us += shares_us(z, rows, d);
         if (best == 0.0f || us < best) { best = us; p.shares = z; p.by_words = t; }
     }
     p.share_words = (slabs + p.shares - 1) / p.shares * BK;
     p.width = p.share_words * p.shares;
     p.pieces = (vocab + p.width - 1) / p.width;
     const int columns = p.pieces == 1 ? p.width : vocab;          // of the first product
-    p.logits = pick_product(1, p.rows_p, columns, p.dp / BK, 0);
+    p.logits = pick_product(kLogits, 1, p.rows_p, columns, p.dp / BK);
     p.strip = kTileColumns[p.logits] / 2;                        // a wavefront's columns of the tile
     p.pairs = 2 * ((columns + kTileColumns[p.logits] - 1) / kTileColumns[p.logits]);
     size_t o = 0;
@@ -277,7 +320,7 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
         if (p.pieces > 1) {
             const Logits::Arg op = logits_of(v0, words);
             const Args a{xs, e + (size_t)v0 * d, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
-            if ((err = launch_product<DT, 5, Logits>(pick_product(1, p.rows_p, p.width, p.dp / BK, 0), a, op)) != hipSuccess) return err;
+            if ((err = launch_product<DT, 5, Logits>(pick_product(kLogits, 1, p.rows_p, p.width, p.dp / BK), a, op)) != hipSuccess) return err;
         }
         {
             ByRows::Arg op{};
@@ -286,7 +329,7 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
             op.w_end = (uint64_t)(uintptr_t)(xs + (size_t)p.rows_p * p.dp);
             op.alpha = alpha;
             const Args a{g, xs, nullptr, nullptr, nullptr, de + (size_t)v0 * d, 1, words, d, p.rows_p, s};
-            if ((err = launch_product<DT, 6, ByRows>(pick_product(1, words, d, p.rows_p / BK, 0), a, op)) != hipSuccess) return err;
+            if ((err = launch_product<DT, 6, ByRows>(pick_product(kByRows, 1, words, d, p.rows_p / BK), a, op)) != hipSuccess) return err;
         }
         {
             ByWords::Arg op{};
@@ -316,8 +359,8 @@ void head_grad_mfma_plan(int rows, int d, int vocab, int32_t *plan)
 {
     const HeadPlan p = head_plan(rows, d, vocab);
     auto tile = [](Tile t) { return kTileRows[t] << 16 | kTileColumns[t]; };
-    plan[0] = tile(pick_product(1, p.rows_p, p.width, p.dp / BK, 0));
-    plan[1] = tile(pick_product(1, p.pieces == 1 ? vocab : p.width, d, p.rows_p / BK, 0));
+    plan[0] = tile(pick_product(kLogits, 1, p.rows_p, p.width, p.dp / BK));
+    plan[1] = tile(pick_product(kByRows, 1, p.pieces == 1 ? vocab : p.width, d, p.rows_p / BK));
     plan[2] = tile(p.by_words);
     plan[3] = p.shares;
     plan[4] = p.pieces;

@@ -1013,49 +1013,5 @@ template <int DT, int EPI, int TN, bool NT, class OP = Plain> hipError_t launch_
 enum Tile { T256x256, T256x192, T256x128, T192x128, T128x128, T64x64, T32x32, kTiles };
 constexpr int kTileRows[kTiles] = {256, 256, 256, 192, 128, 64, 32}, kTileColumns[kTiles] = {256, 192, 128, 128, 128, 64, 32};
 
-// Estimated time of a launch in us: start + rounds (slabs slab + epilogue), where a round of tiles that
-// fills more than half of the CUs also pays slabs busy b, b = 0 .. 1 from half full to full (a full chip clocks lower and
-// shares the fabric).  fp32 outputs are paid for by the rounds' share of the chip (their bursts share the memory), with and
-// without the running sum read, the first round at a price of its own: the caches take part of it, and of what a 64 x 64
-// tile writes nearly all, while from the second round on it pays most per byte (half lines).
-// Constants: least squares over 90 shapes (m_half 96 .. 8192, n and k 512 .. 19200) timed with every tile shape; those of
-// fp32 outputs over 973 shapes (m_half 64 .. 8192, n 240 .. 20000, k from 64): one price for both fp32 epilogues and all
-// rounds, from shapes of k >= 512 alone, had sent short contractions with large outputs to 64 x 64 tiles, up to twice the
-// time of the code before the rule (us, that / one price / here: 1374 x 14048 x 384 fp32 57 / 92 / 55, 2185 x 15512 x 512
-// residual 168 / 230 / 170).  Over 1688 shapes of more than 11 us, all epilogues: on average 1.2 % slower than the best tile
-// of each; 12 more than 5 % slower than the code before, the worst 12 %.
-// The 256 x 256 tile gets 3 % credit: near a tie it is the one that long contractions lose least with.  In us, picked
-// here / the former choice between 256 x 256 and a register-staged 128 x 128 kernel, m_half x n x k: 536 x 2304 x 768
-// 9.0 / 17.1, 692 x 5120 x 5120 84 / 115, 1028 x 1024 x 4096 30 / 53, 391 x 704 x 2816 13 / 39, 8192 x 2304 x 768 61 / 70.
-inline bool tile_fits(Tile t, int slabs)
-{
-    constexpr int kLeast[T32x32] = {3, 3, 3, 4, 5, 1};
-    return slabs >= kLeast[t];
-}
-inline float tile_us(Tile t, int n_sign, int m_half, int n, int n_slabs, int epi)
-{
-    struct Out { float first, more; };
-    static const struct { float start, slab, busy, out16; Out rmw, out32; } kCost[T32x32] = {
-        {4.9f, 1.00f, 0.52f, 3.5f, {26.1f, 21.3f}, {9.0f, 11.4f}}, {3.6f, 0.79f, 0.38f, 3.1f, {20.9f, 16.7f}, {7.0f, 9.0f}},
-        {3.6f, 0.59f, 0.28f, 1.6f, {12.0f, 11.4f}, {2.7f, 7.0f}},  {4.1f, 0.49f, 0.21f, 0.9f, {7.9f, 7.6f}, {1.2f, 5.0f}},
-        {4.1f, 0.38f, 0.16f, 0.3f, {4.3f, 4.5f}, {0.0f, 3.1f}},    {2.6f, 0.21f, 0.41f, 0.4f, {0.5f, 2.5f}, {0.0f, 1.3f}}};
-    const float n_cu = cu_count() ? (float)cu_count() : 256.0f, slabs = (float)n_slabs;
-    const auto &c = kCost[t];
-    const float tiles = (float)n_sign * (float)((m_half + kTileRows[t] - 1) / kTileRows[t]) * (float)((n + kTileColumns[t] - 1) / kTileColumns[t]);
-    const float slots = t == T64x64 ? 2 * n_cu : n_cu;        // workgroups at a time
-    const float full = __builtin_floorf(tiles / slots), part = tiles / slots - full, rounds = full + (part > 0 ? 1.0f : 0.0f);
-    float us = c.start;
-    if (t == T64x64) {
-        // two workgroups per CU: `slab` for one alone, `busy` for the two together
-        const float lone = part > 0 && part <= 0.5f ? 1.0f : 0.0f;
-        us += slabs * ((rounds - lone) * c.busy + lone * c.slab);
-    } else {
-        us += slabs * (rounds * c.slab + (full + (part > 0.5f ? 2 * part - 1 : 0.0f)) * c.busy);
-    }
-    const Out &o = epi == 2 ? c.rmw : c.out32;
-    us += epi < 2 ? c.out16 * rounds : full + part < 1 ? o.first * part : o.first + o.more * (full + part - 1);
-    return t == T256x256 ? us * 0.97f : us;
-}
-
 }  // namespace
 }  // namespace zo

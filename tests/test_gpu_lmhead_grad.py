@@ -228,12 +228,12 @@ def test_against_differences(dtype):
 
 
 TILES = [
-    ("logits", (64, 64), 30, 136, 520), ("logits", (128, 128), 4096, 320, 520), ("logits", (192, 128), 1000, 200, 4104), ("logits", (256, 128), 2049, 192, 2600),
-    ("logits", (256, 192), 1048, 200, 6824), ("logits", (256, 256), 3000, 512, 4104),
-    ("de", (64, 64), 30, 136, 520), ("de", (128, 128), 3000, 2048, 520), ("de", (192, 128), 200, 1024, 4104), ("de", (256, 128), 131, 2048, 2600),
-    ("de", (256, 192), 131, 2048, 4104), ("de", (256, 256), 384, 2048, 6824),
-    ("dx", (64, 64), 30, 136, 520), ("dx", (128, 128), 1500, 1536, 520), ("dx", (192, 128), 2049, 2048, 520), ("dx", (256, 128), 4096, 1536, 520),
-    ("dx", (256, 192), 3000, 1536, 8008), ("dx", (256, 256), 1048, 2048, 50272),
+    ("logits", (64, 64), 30, 136, 520), ("logits", (128, 128), 2049, 320, 1000), ("logits", (192, 128), 1048, 200, 3000), ("logits", (256, 128), 1000, 136, 4104),
+    ("logits", (256, 192), 513, 136, 12000), ("logits", (256, 256), 3000, 512, 4104),
+    ("de", (64, 64), 30, 136, 520), ("de", (128, 128), 257, 768, 3000), ("de", (192, 128), 200, 768, 4104), ("de", (256, 128), 131, 1024, 4104),
+    ("de", (256, 192), 131, 136, 33000), ("de", (256, 256), 131, 200, 33000),
+    ("dx", (64, 64), 30, 136, 520), ("dx", (128, 128), 1048, 1024, 1000), ("dx", (192, 128), 2049, 2048, 520), ("dx", (256, 128), 4096, 1536, 520),
+    ("dx", (256, 192), 4096, 1536, 3000), ("dx", (256, 256), 2049, 2048, 6824),
 ]
 
 
