@@ -16,18 +16,17 @@ namespace zo {
 namespace {
 
 // ------------------------------------------------------------------ around the products
-// Rows as the products take them: x [rows, d] -> [rows_p, dp], zeros in rows that do not count (so that whatever these hold meets
-// no sum), in rows beyond the last and in columns beyond d.  Eight elements a thread.
-__global__ __launch_bounds__(256) void head_rows_kernel(const uint16_t *__restrict__ x, const int32_t *__restrict__ target, uint4 *__restrict__ out, int rows,
-                                                        int rows_p, int d, int dp)
+// Row r as the products over rows take it: x [rows, d] -> [rows_p, dp], zeros in rows that do not count (so that whatever these hold meets
+// no sum), in rows beyond the last and in columns beyond d.  Eight elements a thread and turn.
+__device__ __forceinline__ void head_row(const uint16_t *__restrict__ x, uint4 *__restrict__ out, int r, bool counts, int d, int dp, int first, int step)
 {
-    const int per_row = dp / 8;
-    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < (size_t)rows_p * per_row; i += (size_t)gridDim.x * blockDim.x) {
-        const int r = (int)(i / per_row), c = (int)(i % per_row) * 8;
-        uint4 v{0, 0, 0, 0};
-        if (r < rows && c < d && target[r] >= 0) v = *(const uint4 *)(x + (size_t)r * d + c);
-        out[i] = v;
-    }
+    for (int c = first; c < dp / 8; c += step)
+        out[(size_t)r * (dp / 8) + c] = counts && 8 * c < d ? *(const uint4 *)(x + (size_t)r * d + 8 * c) : uint4{0, 0, 0, 0};
+}
+__global__ __launch_bounds__(256) void head_rows_kernel(const uint16_t *__restrict__ x, const int32_t *__restrict__ target, uint4 *__restrict__ out, int rows, int d, int dp)
+{
+    const int r = blockIdx.x;
+    head_row(x, out, r, r < rows && target[r] >= 0, d, dp, threadIdx.x, 256);
 }
 
 // A row's (maximum, sum) pairs -> its loss and what G takes of it: logsumexp rounded to fp32 and the exponent's share on top, which is
@@ -70,25 +69,30 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float2 *__restrict_
 }
 
 // Distances and pairs of a row -> its loss and, in place, its G (as in epilogue 5); zeros in rows that do not count, past the last row and past
-// the last word.  Workgroup (r, y) takes the y-th part of a row: the whole of it, so that logsumexp is worked once, but for few rows, where
-// 20 workgroups take 12.9 us (50272 words) and the parts of 8 each 5.  Bound by memory: 4 bytes a word.
-template <int DT>
+// the last word.  Workgroup (r, y) takes the y-th part of a row, which works its logsumexp again.  us, 50272 words, 1 / 2 / 4 / 8 parts:
+// 20 rows 12.8 / - / 7.5 / 8.1, 300 rows 22.0 / 18.3 / 19.0 / 23.4, 1048 rows 59.7 / 56.2 / 60.4, 2048 rows 92 / 94 / 110.  Bound by memory,
+// 4 bytes a word.  NT: what passes the memory-side cache anyway goes past the L2, 8192 rows 339 -> 306 us (5.4 TB/s); 300 rows 18 -> 20.
+// `xs`, if not null: takes the row of x on the way (see head_row), where the logits come from x itself.
+template <int DT, bool NT>
 __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ grad, const float2 *__restrict__ pairs, int n_pairs, int strip,
                                                             const float *__restrict__ hit, const int32_t *__restrict__ target, float *__restrict__ row_loss,
-                                                            int rows, int vocab, int width)
+                                                            int rows, int vocab, int width, const uint16_t *__restrict__ x, uint4 *__restrict__ xs, int d)
 {
     __shared__ float red_f[16];
     __shared__ double red_d[16];
     constexpr float kOne = DT == kFP16 ? 32768.0f : 1.0f, kShift = DT == kFP16 ? 15.0f : 0.0f;
     const int r = blockIdx.x, tg = r < rows ? target[r] : -1;
     uint4 *out = grad + (size_t)r * (width / 8);
+    auto load = [](const uint4 *at) { return NT ? __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4 *)at)) : *at; };
     const int each = (width / 8 + gridDim.y - 1) / gridDim.y, first = each * blockIdx.y, last = first + each < width / 8 ? first + each : width / 8;
+    if (xs && blockIdx.y == gridDim.y - 1) head_row(x, xs, r, tg >= 0, d, d, threadIdx.x, 512);
     if (tg < 0) {
         if (r < rows && threadIdx.x == 0 && blockIdx.y == 0) row_loss[r] = 0.0f;
         for (int c = first + threadIdx.x; c < last; c += 512) out[c] = uint4{0, 0, 0, 0};
         return;
     }
     const float2 *p = pairs + (size_t)r * n_pairs;
+    uint4 q = first + (int)threadIdx.x < last ? load(out + first + threadIdx.x) : uint4{0, 0, 0, 0};      // on its way while logsumexp is worked
     float mx = -INFINITY;
     for (int i = threadIdx.x; i < n_pairs; i += 512) mx = p[i].x > mx ? p[i].x : mx;
     mx = block_max(mx, red_f);
@@ -101,7 +105,7 @@ __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ 
     const float hi = (float)lse, rest = (float)(((double)hi - lse) * 1.4426950408889634) + kShift;
     const float at_target = tg < vocab ? __builtin_amdgcn_exp2f(__builtin_fmaf(hit[r] - hi, 1.44269504f, rest)) - kOne : 0.0f;
     for (int c = first + threadIdx.x; c < last; c += 512) {
-        uint4 q = out[c];
+        const uint4 next = c + 512 < last ? load(out + c + 512) : uint4{0, 0, 0, 0};
         const int w0 = 8 * c;
         const float base = __builtin_fmaf(p[w0 / strip].x - hi, 1.44269504f, rest);
         uint32_t *words = &q.x;
@@ -116,7 +120,9 @@ __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ 
             };
             words[e] = (uint32_t)Prec<DT>::acc2a(value(lo, w0 + 2 * e)) | ((uint32_t)Prec<DT>::acc2a(value(up, w0 + 2 * e + 1)) << 16);
         }
-        out[c] = q;
+        if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, q), (u32x4 *)(out + c));
+        else out[c] = q;
+        q = next;
     }
 }
 
@@ -289,9 +295,12 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
     float *part = (float *)(ws + p.part);
     const float alpha = DT == kFP16 ? scale * 0x1p-15f : scale;
     hipError_t err = hipSuccess;
-    const size_t copy_blocks = ((size_t)p.rows_p * (p.dp / 8) + 255) / 256;
-    head_rows_kernel<<<dim3((unsigned)(copy_blocks < 4096 ? copy_blocks : 4096)), dim3(256), 0, s>>>(x, target, (uint4 *)xs, rows, p.rows_p, d, p.dp);
-    if ((err = hipGetLastError()) != hipSuccess) return err;
+    // the logits of a whole vocabulary come from x itself where its rows are whole slabs: the copy is made on the way, with G
+    const bool direct = p.pieces == 1 && p.dp == d;
+    if (!direct) {
+        head_rows_kernel<<<dim3(p.rows_p), dim3(256), 0, s>>>(x, target, (uint4 *)xs, rows, d, p.dp);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
     auto logits_of = [&](int v0, int words) {
         Logits::Arg op{};
         op.ldx = p.dp;
@@ -305,10 +314,12 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
     if (p.pieces == 1) {
         Logits::Arg op = logits_of(0, vocab);
         op.pairs = pair; op.hit = hit;
-        const Args a{xs, e, nullptr, nullptr, nullptr, g, 1, p.rows_p, p.width, p.dp, s};
+        const Args a{direct ? x : xs, e, nullptr, nullptr, nullptr, g, 1, direct ? rows : p.rows_p, p.width, p.dp, s};
         if ((err = launch_product<DT, 9, Logits>(p.logits, a, op)) != hipSuccess) return err;
-        const unsigned parts = p.rows_p >= 512 || p.width < 8192 ? 1 : 512 / p.rows_p;
-        head_gradient_kernel<DT><<<dim3(p.rows_p, parts), dim3(512), 0, s>>>((uint4 *)g, pair, p.pairs, p.strip, hit, target, row_loss, rows, vocab, p.width);
+        const int enough = (2048 + p.rows_p - 1) / p.rows_p, parts = enough < 4 ? enough : 4;
+        auto gradient = p.rows_p * (size_t)p.width * 2 > (size_t)256 << 20 ? head_gradient_kernel<DT, true> : head_gradient_kernel<DT, false>;
+        gradient<<<dim3(p.rows_p, parts), dim3(512), 0, s>>>((uint4 *)g, pair, p.pairs, p.strip, hit, target, row_loss, rows, vocab, p.width, x,
+                                                             direct ? (uint4 *)xs : nullptr, d);
     } else {
         const Args a{xs, e, nullptr, target, hit, pair, 1, rows, vocab, p.dp, s};
         if ((err = launch_product<DT, 4, Logits>(p.logits, a, logits_of(0, vocab))) != hipSuccess) return err;

@@ -668,7 +668,8 @@ hipError_t head_grad_f64(const double *x, const float *e, const int32_t *target,
                                                                                    scale, v0 > 0, (int)dx_tiles);
             return hipGetLastError();
         };
-        const bool many = (long)((rows + 31) / 32) * ((d + 31) / 32) >= 256;
+        // 32 x 32 outputs a workgroup where dx has enough of them (or de too many of 16 x 16 for a grid of 2^32 threads)
+        const bool many = (long)((rows + 31) / 32) * ((d + 31) / 32) >= 256 || (long)((n + 15) / 16) * ((d + 15) / 16) > 1l << 22;
         if ((err = many ? products(head_products_kernel<2, 4>, 32, 4) : products(head_products_kernel<1, 8>, 16, 8)) != hipSuccess) return err;
     }
     return hipSuccess;
