@@ -435,7 +435,7 @@ __global__ __launch_bounds__(64 * W) void head_products_kernel(const double *__r
 // ------------------------------------------------------------------ global norm and clipping
 // Chunk c of a batch: its tensor (found by the lanes side by side), where it starts and its elements.
 struct ClipPlace { uint64_t src, dst; size_t at; uint32_t n; };
-template <typename W> __device__ __forceinline__ ClipPlace clip_place(const ClipBatch &b, uint32_t c)
+template <int N> __device__ __forceinline__ ClipPlace clip_place(const ClipBatchOf<N> &b, uint32_t c)
 {
     const int lane = threadIdx.x & 63;
     int t = -1;
@@ -481,15 +481,15 @@ template <typename W> __device__ __forceinline__ W clip_element(const uint4 &v, 
 
 // sum g^2 of a batch of tensors, one partial sum per workgroup, in fp64: no square of an fp32 number leaves its range, and the
 // sum of 10^9 squares is good to 1e-11 whatever their order.  `seen`: slots that an earlier batch has written (these add to it).
-template <int DT>
-__global__ __launch_bounds__(256) void grad_norm_kernel(ClipBatch b, double *__restrict__ part, int seen)
+template <int DT, int N>
+__global__ __launch_bounds__(256) void grad_norm_kernel(ClipBatchOf<N> b, double *__restrict__ part, int seen)
 {
     using W = typename Prec<DT>::W;
     __shared__ double red[16];
     constexpr int E = 16 / sizeof(W);
     double s[4] = {0.0, 0.0, 0.0, 0.0};                         // side by side: a chain of one would wait for each fma
     for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
-        const ClipPlace t = clip_place<W>(b, c);
+        const ClipPlace t = clip_place(b, c);
         clip_chunk((const W *)t.src + t.at, t.n, [&](uint32_t, const uint4 &v) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -506,8 +506,8 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(ClipBatch b, double *__r
 // partial sums itself, in the same order.  Gradients of up to the memory-side cache's 256 MiB are found there the second time: stores past it
 // leave them there (125 M bf16 gradients into another buffer 122 us, 150 with plain stores; from the last chunk down 122).  117 us with
 // one launch a pass (501 MB that must move, 98 us at the copy rate), where tables of 124 tensors took two.
-template <int DT>
-__global__ __launch_bounds__(256) void grad_scale_kernel(ClipBatch b, const double *__restrict__ part, int n_part, float max_norm, double *__restrict__ out, bool write_norm)
+template <int DT, int N>
+__global__ __launch_bounds__(256) void grad_scale_kernel(ClipBatchOf<N> b, const double *__restrict__ part, int n_part, float max_norm, double *__restrict__ out, bool write_norm)
 {
     using P = Prec<DT>;
     using W = typename P::W;
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(ClipBatch b, const doub
     const double coef = !finite ? 0.0 : norm > (double)max_norm ? (double)max_norm / norm : 1.0;
     if (write_norm && blockIdx.x == 0 && threadIdx.x == 0) { out[0] = norm; out[1] = coef; }
     for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
-        const ClipPlace t = clip_place<W>(b, c);
+        const ClipPlace t = clip_place(b, c);
         if (coef == 1.0 && t.dst == t.src) continue;
         const uint32_t n = t.n;
         W *dst = (W *)t.dst + t.at;
@@ -690,10 +690,11 @@ hipError_t launch_head_grad(const void *x, const void *e, const int32_t *target,
 }
 
 namespace {
-template <class F> hipError_t clip_batches(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, F &&f)
+// f(batch, whether it is the first) over batches of N tensors
+template <int N, class F> hipError_t clip_batches(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, F &&f)
 {
     // tensors of a batch: as many as its table holds, and chunk numbers of 31 bits
-    ClipBatch b{};
+    ClipBatchOf<N> b{};
     bool first = true;
     auto flush = [&] {
         if (b.n == 0) return hipSuccess;
@@ -706,7 +707,7 @@ template <class F> hipError_t clip_batches(const void *const *src, void *const *
     for (int i = 0; i < n_tensors; ++i) {
         if (numel[i] == 0) continue;
         const uint64_t chunks = (numel[i] + kClipChunk - 1) / kClipChunk;
-        if (b.n == kClipMax || b.chunks + chunks >= (1ull << 31)) {
+        if (b.n == N || b.chunks + chunks >= (1ull << 31)) {
             const hipError_t e = flush();
             if (e != hipSuccess) return e;
         }
@@ -717,30 +718,41 @@ template <class F> hipError_t clip_batches(const void *const *src, void *const *
     }
     return flush();
 }
+
+template <int DT, int N>
+hipError_t grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, float max_norm, double *norm, double *part, hipStream_t s)
+{
+    int slots = 0;
+    auto grid = [](const ClipBatchOf<N> &b) { return dim3(b.chunks < kClipSlots ? b.chunks : kClipSlots); };
+    hipError_t err = clip_batches<N>(src, dst, numel, n_tensors, [&](const ClipBatchOf<N> &b, bool) {
+        grad_norm_kernel<DT, N><<<grid(b), dim3(256), 0, s>>>(b, part, slots);
+        slots = (int)grid(b).x > slots ? (int)grid(b).x : slots;
+        return hipGetLastError();
+    });
+    if (err != hipSuccess) return err;
+    bool done = false;
+    err = clip_batches<N>(src, dst, numel, n_tensors, [&](const ClipBatchOf<N> &b, bool first) {
+        grad_scale_kernel<DT, N><<<grid(b), dim3(256), 0, s>>>(b, part, slots, max_norm, norm, first);
+        done = true;
+        return hipGetLastError();
+    });
+    if (err != hipSuccess || done) return err;
+    grad_scale_kernel<DT, N><<<dim3(1), dim3(256), 0, s>>>(ClipBatchOf<N>{}, part, 0, max_norm, norm, true);
+    return hipGetLastError();
+}
 }  // namespace
 
 hipError_t launch_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm, double *norm,
                             void *scratch, hipStream_t s)
 {
-    double *part = (double *)scratch;
-    int slots = 0;
-    hipError_t err = clip_batches(src, dst, numel, n_tensors, [&](const ClipBatch &b, bool) {
-        const int grid = (int)(b.chunks < kClipSlots ? b.chunks : kClipSlots);
-        ZO_DISPATCH_DT(dtype, (grad_norm_kernel<DT><<<dim3(grid), dim3(256), 0, s>>>(b, part, slots)));
-        slots = grid > slots ? grid : slots;
-        return hipGetLastError();
-    });
-    if (err != hipSuccess) return err;
-    bool done = false;
-    err = clip_batches(src, dst, numel, n_tensors, [&](const ClipBatch &b, bool first) {
-        const int grid = (int)(b.chunks < kClipSlots ? b.chunks : kClipSlots);
-        ZO_DISPATCH_DT(dtype, (grad_scale_kernel<DT><<<dim3(grid), dim3(256), 0, s>>>(b, part, slots, max_norm, norm, first)));
-        done = true;
-        return hipGetLastError();
-    });
-    if (err != hipSuccess || done) return err;
-    ZO_DISPATCH_DT(dtype, (grad_scale_kernel<DT><<<dim3(1), dim3(256), 0, s>>>(ClipBatch{}, part, 0, max_norm, norm, true)));
-    return hipGetLastError();
+    auto go = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        // a kernel's arguments are copied at each launch, 4 KiB of the long table: a few small tensors take 11.4 us with the short one, 12.4 with
+        // the long; more tensors than the short table holds would take launches of 4 us each
+        auto f = n_tensors <= kClipFew ? grad_clip<DT, kClipFew> : grad_clip<DT, kClipMax>;
+        return f(src, dst, numel, n_tensors, max_norm, norm, (double *)scratch, s);
+    };
+    return dtype == kFP32 ? go(std::integral_constant<int, kFP32>{}) : dtype == kBF16 ? go(std::integral_constant<int, kBF16>{}) : go(std::integral_constant<int, kFP16>{});
 }
 
 }  // namespace zo

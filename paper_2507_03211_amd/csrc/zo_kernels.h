@@ -127,15 +127,16 @@ hipError_t launch_head_grad_mfma(const void *x, const void *e, const int32_t *ta
 
 constexpr uint32_t kClipChunk = 16384;     // elements per chunk
 constexpr uint32_t kClipSlots = 1024;      // workgroups of a pass at most, each with a partial sum of its own
-// Tensors of a pass over gradients, twenty bytes each: those of a 12-layer model go into one launch.
-constexpr int kClipMax = 201;
-struct ClipBatch {
-    uint64_t src[kClipMax];                // address, 48 bits; above it the elements of the last chunk less one
-    uint64_t dst[kClipMax];
-    uint32_t first[kClipMax];              // first chunk
+// Tensors of a pass over gradients, twenty bytes each: those of a 12-layer model go into one launch.  A few tensors take a shorter table.
+constexpr int kClipMax = 201, kClipFew = 40;
+template <int N> struct ClipBatchOf {
+    uint64_t src[N];                       // address, 48 bits; above it the elements of the last chunk less one
+    uint64_t dst[N];
+    uint32_t first[N];                     // first chunk
     int n;
     uint32_t chunks;
 };
+using ClipBatch = ClipBatchOf<kClipMax>;
 static_assert(kClipChunk <= 1 << 16, "the last chunk's elements less one are a 16-bit number");
 static_assert(sizeof(ClipBatch) + 64 <= 4096, "passed by value: a kernel takes 4 KiB of arguments");
 // dst may be src, tensor by tensor.  `scratch`: kClipSlots doubles; `norm`: the norm and the coefficient

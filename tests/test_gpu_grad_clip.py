@@ -16,7 +16,8 @@ from grad_util import Out, generator, half, least, normal, param_dtype
 
 pytestmark = pytest.mark.gpu
 DTYPES = [zi.FP32, zi.BF16, zi.FP16]
-LISTS = [[1], [7, 1], [16384], [16383, 16385, 3], [5, 0, 100001, 8, 64], [300000] + [768] * 300, [40] * 125, [1 << 22, 9], [17] * 700]
+LISTS = [[1], [7, 1], [16384], [16383, 16385, 3], [5, 0, 100001, 8, 64], [300000] + [768] * 300, [40] * 125, [1 << 22, 9], [17] * 700,
+         [17] * 40, [17] * 41]
 
 
 def scratch():
