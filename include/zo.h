@@ -389,7 +389,8 @@ int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t *target, v
 
 /* How such a call of 2-byte types works on the current device (on 256 compute units where there is none): plan[0 .. 2] the output
  * tiles of the logits, de and dx (rows << 16 | columns), plan[3] the shares that the contraction over the vocabulary is cut into
- * for dx, plan[4] the pieces of the vocabulary.  Host only. */
+ * for dx, plan[4] the pieces of the vocabulary, plan[5] a piece's words whose de plan[1]'s tiles work, plan[6] the tile of the words
+ * behind them, if any.  plan holds 7 numbers.  Host only. */
 int zo_kernel_lmhead_grad_plan(int rows, int d, int vocab, int32_t *plan);
 
 /* Global norm of n_tensors gradients and clipping by it: norm[0] = sqrt(sum of all squares), norm[1] = c = max_norm / norm[0] where

@@ -327,11 +327,11 @@ def zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab):
 
 
 def zo_kernel_lmhead_grad_plan(rows, d, vocab):
-    """Of 2-byte types: {"logits", "de", "dx": (rows, columns) of the output tiles, "shares", "pieces"}."""
-    plan = (ctypes.c_int32 * 5)()
+    """Of 2-byte types: {"logits", "de", "dx", "de_rest": (rows, columns) of the output tiles, "shares", "pieces", "de_words"}."""
+    plan = (ctypes.c_int32 * 7)()
     _check(lib().zo_kernel_lmhead_grad_plan(rows, d, vocab, plan))
-    tiles = {name: (plan[i] >> 16, plan[i] & 0xffff) for i, name in enumerate(("logits", "de", "dx"))}
-    return dict(tiles, shares=plan[3], pieces=plan[4])
+    tiles = {name: (plan[i] >> 16, plan[i] & 0xffff) for i, name in ((0, "logits"), (1, "de"), (2, "dx"), (6, "de_rest"))}
+    return dict(tiles, shares=plan[3], pieces=plan[4], de_words=plan[5])
 
 
 def zo_kernel_lmhead_grad(x, e, target, row_loss, dx, de, scratch, dtype, rows, d, vocab, scale, stream=None):

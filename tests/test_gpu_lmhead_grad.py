@@ -247,6 +247,20 @@ def test_every_tile(dtype, product, tile, rows, d, vocab):
         check(dtype, x, e, target, 0.03125, call(dtype, x, e, target, 0.03125))
 
 
+@pytest.mark.parametrize("dtype,rows,d,vocab,words,rest", [
+    (zi.BF16, 520, 648, 50272, 43520, (192, 128)), (zi.FP16, 520, 968, 20000, 16384, (128, 128)), (zi.BF16, 1024, 392, 33000, 32768, (64, 64)),
+    (zi.FP16, 1024, 520, 50272, 43520, (192, 128)), (zi.BF16, 1024, 1032, 33000, 26112, (256, 128)), (zi.FP16, 2048, 264, 33000, 32768, (64, 64)),
+    (zi.BF16, 2048, 648, 33000, 21760, (256, 192))])
+def test_words_behind_whole_rounds(dtype, rows, d, vocab, words, rest):
+    """de's last words in a launch and tiles of their own."""
+    p = zo_amd.zo_kernel_lmhead_grad_plan(rows, d, vocab)
+    assert (p["de_words"], p["de_rest"]) == (words, rest)
+    for r, v in ((rows, vocab), (rows - 3, vocab - 8)):
+        x, e, target = inputs(dtype, r, d, v, 23)
+        target[0], target[1], target[2] = words - 1, words, v - 1
+        check(dtype, x, e, target, 0.03125, call(dtype, x, e, target, 0.03125))
+
+
 @pytest.mark.parametrize("rows,d,vocab", [(16, 768, 9000), (40, 512, 20000), (131, 2048, 12000), (5, 64, 50272)])
 def test_shares_of_the_vocabulary(rows, d, vocab):
     """Few rows: the contraction over the words is cut into shares, some of which reach past the last word."""

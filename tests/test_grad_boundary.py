@@ -61,7 +61,7 @@ def test_lmhead_grad():
 
 def test_lmhead_grad_plan():
     p = zo_amd.zo_kernel_lmhead_grad_plan(8192, 5120, 50272)
-    assert p == dict(logits=(256, 256), de=(256, 256), dx=(256, 256), shares=2, pieces=1)
+    assert p == dict(logits=(256, 256), de=(256, 256), dx=(256, 256), shares=2, pieces=1, de_words=49152, de_rest=(192, 128))
     assert zo_amd.zo_kernel_lmhead_grad_plan(65536, 5120, 50272)["pieces"] > 1
     assert zo_amd.zo_kernel_lmhead_grad_plan(20, 768, 50272)["shares"] > 1
     # a workspace for more rows grows by the rows' own buffers once G fills its room
