@@ -397,7 +397,8 @@ int zo_kernel_lmhead_grad_plan(int rows, int d, int vocab, int32_t *plan);
  * norm[0] > max_norm, else 1; dst[t] = rn(c src[t]) for every tensor t of numel[t] elements.  A norm that is not a finite number makes c 0 and
  * every dst zeros, as a g that is not finite leaves theta alone.  The sums are taken in fp64.
  *   src, dst, numel  host arrays of n_tensors device pointers and counts, read before the call returns; tensors of dtype's storage
- *                    type, 16-byte aligned.  dst[t] may be src[t], and otherwise overlaps no tensor.  numel 0: skipped.
+ *                    type, 16-byte aligned.  dst[t] may be src[t], and otherwise overlaps no tensor (ZO_EINVAL if it does: a
+ *                    tensor clipped in place is listed once).  numel 0: skipped.
  *   max_norm         > 0; infinity for the norm alone (dst[t] = src[t] is then not touched)
  *   norm             device, double[2] */
 size_t zo_kernel_grad_clip_scratch_bytes(void);

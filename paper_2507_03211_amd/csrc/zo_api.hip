@@ -1411,6 +1411,35 @@ extern "C" int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t
     return ZO_OK;
 }
 
+// Whether a dst of a clipping overlaps another one, or a src that is not its own: -1 if not, else the number of a tensor that does; -2: no
+// memory.  `each`: bytes of an element.
+static int clip_overlap(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, size_t each)
+{
+    struct Range { uintptr_t first, end; int tensor; };
+    Range few[256], *r = few;
+    if (n_tensors > 256 && !(r = new (std::nothrow) Range[n_tensors])) return -2;
+    int n = 0, bad = -1;
+    bool sorted = true;
+    for (int i = 0; i < n_tensors; ++i) {
+        if (numel[i] == 0) continue;
+        r[n] = Range{(uintptr_t)dst[i], (uintptr_t)dst[i] + numel[i] * each, i};
+        if (n && r[n].first < r[n - 1].first) sorted = false;
+        ++n;
+    }
+    if (!sorted) std::sort(r, r + n, [](const Range &a, const Range &b) { return a.first < b.first; });
+    for (int k = 1; k < n && bad < 0; ++k)
+        if (r[k].first < r[k - 1].end) bad = r[k].tensor;
+    for (int i = 0; i < n_tensors && bad < 0; ++i) {
+        if (numel[i] == 0 || src[i] == dst[i]) continue;
+        const uintptr_t first = (uintptr_t)src[i], end = first + numel[i] * each;
+        // the last dst that starts before this src ends
+        const Range *at = std::lower_bound(r, r + n, end, [](const Range &a, uintptr_t v) { return a.first < v; });
+        if (at != r && at[-1].end > first) bad = i;
+    }
+    if (r != few) delete[] r;
+    return bad;
+}
+
 extern "C" size_t zo_kernel_grad_clip_scratch_bytes(void) { return kClipSlots * sizeof(double); }
 
 extern "C" int zo_kernel_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm, double *norm,
@@ -1429,6 +1458,9 @@ extern "C" int zo_kernel_grad_clip(const void *const *src, void *const *dst, con
         if ((uint64_t)(uintptr_t)src[i] >> 48 || (uint64_t)(uintptr_t)dst[i] >> 48) return fail(ZO_EINVAL, "tensor %d: not a device address", i);
         if (numel[i] >= 1ull << 44) return fail(ZO_EINVAL, "tensor %d has %llu elements", i, (unsigned long long)numel[i]);
     }
+    const int bad = clip_overlap(src, dst, numel, n_tensors, dtype == ZO_FP32 ? 4 : 2);
+    if (bad == -2) return fail(ZO_ENOMEM, "no host memory for %d tensors", n_tensors);
+    if (bad >= 0) return fail(ZO_EINVAL, "tensor %d overlaps another tensor's dst", bad);
     ZO_HIP(launch_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, norm, scratch_mem, (hipStream_t)stream));
     return ZO_OK;
 }

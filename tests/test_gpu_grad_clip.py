@@ -98,6 +98,24 @@ def test_squares_beyond_fp32():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("count", [9, 300])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_neighbours_in_one_buffer(dtype, count, shift):
+    """Tensors that adjoin, listed from the last one to the first: clipped in place, or into the next one's place, where nothing else lies."""
+    n = 64
+    base = normal((2 * count * n,), param_dtype(dtype), generator(5), 0.01)
+    buf = base.clone()
+    parts = [buf[2 * n * i:2 * n * i + n] for i in range(count)][::-1]
+    to = [buf[2 * n * i + n * shift:2 * n * i + n * (1 + shift)] for i in range(count)][::-1]
+    norm = torch.empty(2, dtype=torch.float64, device=DEV)
+    zo_amd.zo_kernel_grad_clip(parts, to, [n] * count, count, dtype, 0.01, norm, scratch())
+    src = [base[2 * n * i:2 * n * i + n] for i in range(count)][::-1]
+    check(dtype, src, float(torch.tensor(0.01, dtype=torch.float32)), (to, norm.tolist()))
+    other = base.view(count, 2, n)[:, 1 - shift]
+    assert torch.equal(buf.view(count, 2, n)[:, 1 - shift], other)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_same_bits_every_time_and_tables_kept(dtype):
     src = tensors(dtype, [70000, 5, 123456, 768, 31])
     first = clip(dtype, src, 0.5)

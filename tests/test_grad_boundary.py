@@ -74,11 +74,17 @@ def test_lmhead_grad_plan():
 
 def test_grad_clip():
     #       src dst numel n dtype max_norm norm scratch
-    good = [[P, P], [P, P], [4, 4], 2, ZO_BF16, 1.0, P, P]
+    good = [[P, P + 64], [P, P + 64], [4, 4], 2, ZO_BF16, 1.0, P, P]
     f = zo_amd.zo_kernel_grad_clip
     for at, value in ((0, [P, None]), (1, [None, P]), (0, [P + 8, P]), (1, [P, P + 2]), (2, [4, 1 << 60]), (3, -1), (4, 3), (5, 0.0), (5, -1.0),
                       (5, NAN), (6, None), (7, None), (6, P + 4), (7, P + 16)):
         refused(f, *(good[:at] + [value] + good[at + 1:]))
+    # a tensor listed twice, one that ends in the next, a dst where another's src or its own lies, in order and not, more than a few
+    for src, dst, n in (([P, P], [P, P], [4, 4]), ([P, P + 64], [P, P + 64], [33, 4]), ([P, P + 64], [P + 64, P], [4, 4]), ([P], [P + 16], [9]),
+                        ([P + 144, P], [P + 512, P + 128], [8, 9]),
+                        ([P + 64 * i for i in range(300, 0, -1)] + [P + 64 * 7 + 16], [P + 64 * i for i in range(300, 0, -1)] + [P + 64 * 400], [32] * 301)):
+        with pytest.raises(zo_amd.ZoError, match="overlaps"):
+            f(src, dst, n, len(src), ZO_BF16, 1.0, P, P)
     L = zo_amd.lib()
     for tables in ((None, None, None), (None, (ctypes.c_void_p * 1)(P), (ctypes.c_uint64 * 1)(4))):
         assert L.zo_kernel_grad_clip(*tables, 1, ZO_BF16, 1.0, P, P, None) == zo_amd.ZO_EINVAL
