@@ -375,7 +375,7 @@ int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain
 
 /* Tied LM head and cross entropy, forward and backward: for x [rows, d] and e [vocab, d], logits l = x e^T,
  *     row_loss[r] = logsumexp(l[r]) - l[r, target[r]],    G = scale (softmax(l) - onehot(target)),    dx = G e,    de = G^T x.
- * A row with target[r] < 0 does not count: row_loss, its row of G and its row of dx are 0 whatever x[r] holds, NaN included.  A
+ * A row with target[r] < 0 does not count: row_loss, its row of G and its row of dx (of a finite e) are 0 whatever x[r] holds, NaN included.  A
  * target >= vocab makes the row's loss NaN, and dx[r] and de with it.  scale: 1 / (rows that count) for the mean loss, times
  * whatever keeps ZO_FP16 gradients in range.  de is the head's share of the tied embedding's gradient alone.  Outputs overlap
  * nothing.  Up to 2^20 rows, d and vocab up to 2^22; 2-byte dtypes: d and vocab multiples of 8, buffers 16-byte aligned

@@ -306,15 +306,16 @@ __global__ __launch_bounds__(256) void head_stats_kernel(const double *__restric
     double mx = -INFINITY;
     for (int c = threadIdx.x; c < words; c += blockDim.x) mx = lg[c] > mx ? lg[c] : mx;
     mx = block_max(mx, red);
+    const double ref = mx > -INFINITY ? mx : 0.0;              // of minus infinities and NaN alone: their sum is 0 or NaN
     double s = 0.0;
-    for (int c = threadIdx.x; c < words; c += blockDim.x) s += exp(lg[c] - mx);
+    for (int c = threadIdx.x; c < words; c += blockDim.x) s += exp(lg[c] - ref);
     s = block_sum(s, red);
     if (threadIdx.x != 0) return;
     RowState st = first_word ? state[r] : RowState{-INFINITY, 0.0, 0.0};
     const int at = target[r] - first_word;
     if (at >= 0 && at < words) st.hit = lg[at];
-    const double top = st.max > mx ? st.max : mx;
-    st.sum = (st.max > -INFINITY ? st.sum * exp(st.max - top) : 0.0) + s * exp(mx - top);
+    const double top = st.max > ref ? st.max : ref;
+    st.sum = (first_word ? st.sum * exp(st.max - top) : 0.0) + s * exp(ref - top);
     st.max = top;
     state[r] = st;
 }

@@ -165,6 +165,25 @@ def test_numbers_that_are_not_finite(dtype, rows):
         assert torch.isfinite(loss[keep]).all() and torch.isfinite(dx[keep]).all()
 
 
+@pytest.mark.parametrize("dtype,rows,d,vocab", [
+    (zi.BF16, 10, 64, 1000), (zi.FP16, 10, 64, 1000), (zi.BF16, 600, 128, 4096), (zi.FP16, 600, 128, 4096), (zi.BF16, 140, 320, 1 << 22), (zi.FP32, 10, 64, 304),
+    (zi.FP32, 100, 16, 6000), (zi.FP32, 2100, 16, 17000)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_words_that_are_not_finite(dtype, rows, d, vocab, bad):
+    """Whole neighbourhoods of words that are not finite, and no others: a row that counts has a loss only where the formula has one."""
+    x, e, target = inputs(dtype, rows, d, vocab, 16)
+    for words in (slice(0, 512), slice(vocab - 512, vocab)) if vocab > 1024 else (slice(0, 256),):
+        if (dtype, rows) == (zi.FP32, 2100):
+            words = slice(0, 16000) if words.start == 0 else slice(16000, vocab)         # a whole piece of logits, and a part of one
+        bent = e.clone()
+        bent[words] = bad
+        loss, dx, de = call(dtype, x, bent, target, 1.0)
+        live = target >= 0
+        logits = torch.where(live[:, None], x.double(), 0.0) @ bent.double().t()
+        want = torch.logsumexp(logits, 1) - logits.gather(1, target.clamp(min=0).long()[:, None]).squeeze(1)
+        assert torch.equal(torch.isfinite(loss[live]), torch.isfinite(want[live])) and (loss[~live] == 0).all() and torch.isnan(dx[live]).all()
+
+
 @pytest.mark.parametrize("dtype", [zi.FP32, zi.BF16, zi.FP16])
 @pytest.mark.parametrize("rows,d,vocab", [(16, 256, 4096), (520, 256, 4096)])
 def test_same_bits_every_time_on_any_stream(dtype, rows, d, vocab):
