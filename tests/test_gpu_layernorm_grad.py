@@ -119,7 +119,7 @@ def test_backward(dtype, rows, d):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("rows,d", [(37, 768), (12, 2052), (5, 333)])
+@pytest.mark.parametrize("rows,d", [(37, 768), (12, 2052), (5, 333), (1003, 768), (300, 5120), (600, 333), (400, 2601), (300, 12288), (270, 13001)])
 def test_accumulates_and_leaves_out(dtype, rows, d):
     c = case(dtype, rows, d, 5)
     before = normal((rows, d), resid_dtype(dtype), generator(3), 0.2)
