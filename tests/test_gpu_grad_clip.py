@@ -132,6 +132,21 @@ def test_same_bits_every_time_and_tables_kept(dtype):
         assert norm.tolist() == first[1] and all(torch.equal(a, b) for a, b in zip(outs, first[0]))
 
 
+def test_more_elements_than_32_bits_count():
+    n, max_norm = (1 << 32) + 9, 0.5
+    src = torch.empty(n, dtype=torch.bfloat16, device=DEV).normal_(0.0, 0.01, generator=generator(31))
+    out = Out((n,), torch.bfloat16)
+    norm = torch.empty(2, dtype=torch.float64, device=DEV)
+    zo_amd.zo_kernel_grad_clip([src], [out.t], [n], 1, zi.BF16, max_norm, norm, scratch())
+    torch.cuda.synchronize()
+    assert out.whole()
+    want = float(sum(t.double().square().sum() for t in src.split(1 << 28)))**0.5
+    assert abs(float(norm[0]) - want) <= 2.0**-40 * want             # 2^12 in a chain here, and the oracle's own sums
+    for t, o in zip(src.split(1 << 28), out.t.split(1 << 28)):
+        w = max_norm / want * t.double()
+        assert ((o.double() - w).abs() <= (half(t.dtype) * (1 + 2.0**-20) + 2.0**-22) * w.abs() + least(t.dtype)).all()
+
+
 def test_bytes_of_a_model():
     """The tensors of a 3-layer model side by side in one buffer, clipped into another: nothing between them is touched."""
     d, f = 96, 384

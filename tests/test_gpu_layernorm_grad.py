@@ -177,6 +177,37 @@ def test_constant_rows_and_what_is_not_finite(dtype, rows, d):
     assert not torch.isfinite(dh[1]).any() and not torch.isfinite(dg).all()
 
 
+@pytest.mark.parametrize("d", [1100, 1101])
+def test_more_elements_than_32_bits_count(d):
+    """Rows by fours and one by one; those around 2^31 and 2^32 bytes and elements, and the sums over all of them."""
+    dtype, rows = zi.BF16, (1 << 32) // d + 1000
+    g = generator(41)
+    h = torch.empty((rows, d), device=DEV).normal_(0.5, 1.0, generator=g)
+    dy = torch.empty((rows, d), dtype=torch.bfloat16, device=DEV).normal_(0.0, 0.1, generator=g)
+    gain, bias = (1.0 + normal((d,), torch.float64, g, 0.3)).to(torch.bfloat16), normal((d,), torch.bfloat16, g, 0.3)
+    y, mean, rstd = Out((rows, d), torch.bfloat16), Out((rows,), torch.float32), Out((rows,), torch.float32)
+    zo_amd.zo_kernel_layernorm(h, gain, bias, y.t, mean.t, rstd.t, dtype, rows, d, EPS)
+    dh, dg, db = backward(dtype, rows, d, dy, h, gain, mean.t, rstd.t)
+    assert y.whole() and mean.whole() and rstd.whole()
+    for at in (0, (1 << 29) // d, (1 << 30) // d, (1 << 31) // d, rows - 300):
+        part = slice(max(at - 100, 0), at + 300)
+        n = h[part].shape[0]
+        m, r = stats64(h[part])
+        # K u = 2^-16.8 of values around 1, of their mean and, by the same sums, of rstd; of y, values up to 6 times both
+        assert ((mean.t[part].double() - m).abs() <= 2.0**-14).all() and ((rstd.t[part].double() / r - 1).abs() <= 2.0**-14).all()
+        want = (h[part].double() - m[:, None]) * r[:, None] * gain.double() + bias.double()
+        assert ((y.t[part].double() - want).abs() <= half(torch.bfloat16) * want.abs() + 2.0**-12 * (1 + want.abs())).all()
+        check_backward(dtype, n, d, dy[part], h[part], gain, mean.t[part], rstd.t[part], (dh[part], None, None))
+    sums = torch.zeros((4, d), dtype=torch.float64, device=DEV)
+    for a in range(0, rows, 1 << 16):
+        v = dy[a:a + (1 << 16)].double()
+        vx = v * (h[a:a + (1 << 16)].double() - mean.t[a:a + (1 << 16), None].double()) * rstd.t[a:a + (1 << 16), None].double()
+        sums += torch.stack((vx.sum(0), vx.abs().sum(0), v.sum(0), v.abs().sum(0)))
+    u = unit(dtype)
+    for have, want, size in ((dg, sums[0], sums[1]), (db, sums[2], sums[3])):
+        assert ((have.double() - want).abs() <= half(torch.bfloat16) * want.abs() * 1.01 + 1.01 * (K(rows) + 4) * u * size).all()
+
+
 @pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
 @pytest.mark.parametrize("d", [768, 5120])
 def test_buffers_off_their_alignment(dtype, d):

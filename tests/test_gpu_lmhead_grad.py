@@ -43,8 +43,8 @@ def call(dtype, x, e, target, scale, stream=None):
     return loss.t, dx.t, de.t
 
 
-def check(dtype, x, e, target, scale, got):
-    """x's rows of targets < 0 are taken as zeros; the scale is an fp32 number, as the call gets it."""
+def check(dtype, x, e, target, scale, got, words=slice(None)):
+    """x's rows of targets < 0 are taken as zeros; the scale is an fp32 number, as the call gets it.  `words`: whose de is looked at."""
     scale = float(torch.tensor(scale, dtype=torch.float32))
     loss, dx, de = got
     (rows, d), vocab = x.shape, e.shape[0]
@@ -69,8 +69,8 @@ def check(dtype, x, e, target, scale, got):
     assert (loss[~live] == 0).all() and (dx[~live] == 0).all()
     h = 0.0 if dtype == zi.FP32 else (half(act_dtype(dtype))**2 + (16.0 / 65535)**2)**0.5
     tiny = 0.0 if dtype == zi.FP32 else math.exp(-32.0) + (2.0**-39 if dtype == zi.FP16 else 0.0)    # the latter: half the step of probabilities below fp16's normal numbers, 2^15 times enlarged
-    for out, A, B, n in ((dx, G, ed, vocab), (de, G.t().contiguous(), xd, rows)):
-        off = off_G if out is dx else off_G.t().contiguous()
+    for out, A, B, n in ((dx, G, ed, vocab), (de[words], G[:, words].t().contiguous(), xd, rows)):
+        off = off_G if out is dx else off_G[:, words].t().contiguous()
         want = scale * (A @ B)
         t = out.dtype
         tol = half(t) * want.abs() + abs(scale) * (
@@ -244,6 +244,20 @@ def test_against_differences(dtype):
     if dtype == zi.FP32:
         off = off + 7 * 2.0**-24 * (e.abs().max().double() + step * ve.abs().max()) * torch.sqrt(de.double().square().sum()) / step
     assert (got - fine).abs() <= (coarse - fine).abs() + off
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(6, 520, 1 << 22), (1 << 20, 2056, 16)])
+def test_more_bytes_than_32_bits_count(rows, d, vocab):
+    g = generator(51)
+    x = torch.empty((rows, d), dtype=torch.bfloat16, device=DEV).normal_(0.0, 1.0, generator=g)
+    e = torch.empty((vocab, d), dtype=torch.bfloat16, device=DEV).normal_(0.0, 0.05, generator=g)
+    target = torch.randint(0, vocab, (rows,), device=DEV, generator=g).to(torch.int32)
+    target[rows // 2], target[rows - 1], target[0] = -1, vocab - 1, (1 << 31) // d % vocab
+    words = slice(None)
+    if vocab > 1 << 20:
+        middle = (1 << 30) // d                                     # its bytes pass 2^31 there, and 2^32 near the end
+        words = torch.cat([torch.arange(a, b, device=DEV) for a, b in ((0, 1000), (middle - 1000, middle + 1000), (2 * middle - 1000, vocab))])
+    check(zi.BF16, x, e, target, 1.0 / rows, call(zi.BF16, x, e, target, 1.0 / rows), words)
 
 
 TILES = [
