@@ -106,19 +106,26 @@ __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ 
     const float at_target = tg < vocab ? __builtin_amdgcn_exp2f(__builtin_fmaf(hit[r] - hi, 1.44269504f, rest)) - kOne : 0.0f;
     for (int c = first + threadIdx.x; c < last; c += 512) {
         const uint4 next = c + 512 < last ? load(out + c + 512) : uint4{0, 0, 0, 0};
-        const int w0 = 8 * c;
-        const float base = __builtin_fmaf(p[w0 / strip].x - hi, 1.44269504f, rest);
-        uint32_t *words = &q.x;
+        if (8 * c < vocab) {                                   // (words are a multiple of eight)
+            const float base = __builtin_fmaf(p[8 * c / strip].x - hi, 1.44269504f, rest);
+            const float none = base - INFINITY;                // of the last step; a row that is not a number stays one
+            uint32_t *words = &q.x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = words[e] & 0xffff, up = words[e] >> 16;
-            auto value = [&](uint32_t steps, int w) {
-                float v = __builtin_amdgcn_exp2f(__builtin_fmaf((float)steps, -1.44269504f * 32.0f / 65535.0f, steps == 65535 ? -INFINITY : base));
-                v = base == base ? v : base;                   // (a row that is not a number, whatever its steps)
-                v = w == tg ? at_target : v;
-                return w < vocab ? v : 0.0f;
-            };
-            words[e] = (uint32_t)Prec<DT>::acc2a(value(lo, w0 + 2 * e)) | ((uint32_t)Prec<DT>::acc2a(value(up, w0 + 2 * e + 1)) << 16);
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = words[e] & 0xffff, up = words[e] >> 16;
+                auto value = [&](uint32_t steps) {
+                    return __builtin_amdgcn_exp2f(__builtin_fmaf((float)steps, -1.44269504f * 32.0f / 65535.0f, steps == 65535 ? none : base));
+                };
+                words[e] = pack2<DT>(value(lo), value(up));
+            }
+            if (c == tg >> 3) {
+                const uint32_t t = Prec<DT>::acc2a(at_target);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if ((tg & 7) >> 1 == e) words[e] = tg & 1 ? (words[e] & 0xffff) | t << 16 : (words[e] & ~0xffffu) | t;
+            }
+        } else {
+            q = uint4{0, 0, 0, 0};
         }
         if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, q), (u32x4 *)(out + c));
         else out[c] = q;
@@ -158,7 +165,7 @@ __global__ __launch_bounds__(256) void head_dx_kernel(const float4 *__restrict__
                 }
             }
         }
-        auto two = [&](float lo, float hi) { return (uint32_t)Prec<DT>::acc2a(alpha * lo) | ((uint32_t)Prec<DT>::acc2a(alpha * hi) << 16); };
+        auto two = [&](float lo, float hi) { return pack2<DT>(alpha * lo, alpha * hi); };
         if (group == 0 && i0 + t < n8) dx[i] = uint4{two(a.x, a.y), two(a.z, a.w), two(b.x, b.y), two(b.z, b.w)};
     }
 }

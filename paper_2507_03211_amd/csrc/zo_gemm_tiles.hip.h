@@ -20,6 +20,14 @@ namespace {
 
 constexpr int BK = 64;                      // contraction slab; k is a multiple of it
 
+// two outputs per conversion instruction (round to nearest even, as the single one does)
+template <int DT> __device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    const f32x2 pr = {lo, hi};
+    if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, f16x2));
+}
+
 // How a kernel's operands lie in memory.  Plain: rows of k elements (a linear layer's activations and weights, per sign).
 // Product<XK, WK>: rows at a stride of their own, or (XK, WK) with the contraction as the outer index, element (i, k) at
 // [k * stride + i]; `sign` then counts shares of the contraction, each with a partial result of its own.  Shares begin
@@ -424,18 +432,12 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
                     }
                     const int run = tn * 8 + 2 * g + fh;         // which run of 4 columns of the row
                     if constexpr (kOut16) {
-                        // two outputs per conversion instruction (round to nearest even, as the single one does)
-                        auto pack2 = [](float lo, float hi) {
-                            const f32x2 pr = {lo, hi};
-                            if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
-                            else return __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, f16x2));
-                        };
                         uint2 o;
                         if constexpr (EPI == 9) {              // 0 .. 1 to 0 .. 65535, nearest, what lies outside to the ends: one instruction for two
                             auto steps2 = [](float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(lo, hi)); };
                             o = uint2{steps2(v[0], v[1]), steps2(v[2], v[3])};
                         } else {
-                            o = uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+                            o = uint2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
                         }
                         const int slot = kXor ? (((tn * 4 + g) ^ chunk16(fr)) << 1) + (fh ^ ((fr >> kFlip) & 1)) : run;
                         *(uint2 *)(stage + fr * PITCH + (slot << 3)) = o;
