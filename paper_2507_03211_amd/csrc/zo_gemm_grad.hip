@@ -69,8 +69,10 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float2 *__restrict_
 }
 
 // Distances and pairs of a row -> its loss and, in place, its G (as in epilogue 5); zeros in rows that do not count, past the last row and past
-// the last word.  Workgroup (r, y) takes the y-th part of a row, which works its logsumexp again.  us, 50272 words, 1 / 2 / 4 / 8 parts:
-// 20 rows 12.8 / - / 7.5 / 8.1, 300 rows 22.0 / 18.3 / 19.0 / 23.4, 1048 rows 59.7 / 56.2 / 60.4, 2048 rows 92 / 94 / 110.  Bound by memory,
+// the last word.  Workgroup (r, y) takes the y-th part of a row, which works its logsumexp again; four of them are on a CU.  us of the
+// whole call with 1 / 2 / 4 parts, 768 x 50272: 20 rows 70.4 / 66.2 / 64.1, 100 rows 81.4 / 77.3 / 76.1, 300 rows 138.4 / 135.8 / 136.5,
+// 600 rows 218.4 / 218.0 / 221.2, 1048 rows 317 / 312 / 318, 2048 rows 541 / 544 / 557; 512 x 10000: 64 rows 28.8 / 28.1 / 27.8, 300 rows
+// 44.4 / 44.4 / 46.4, 500 rows 47.4 / 48.5 / 52.5, 1000 rows 69.4 / 72.1 / 80.8.  Bound by memory,
 // 4 bytes a word.  NT: what passes the memory-side cache anyway goes past the L2, 8192 rows 339 -> 306 us (5.4 TB/s); 300 rows 18 -> 20.
 // `xs`, if not null: takes the row of x on the way (see head_row), where the logits come from x itself.
 template <int DT, bool NT>
@@ -346,7 +348,7 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
         op.pairs = pair; op.hit = hit;
         const Args a{direct ? x : xs, e, nullptr, nullptr, nullptr, g, 1, direct ? rows : p.rows_p, p.width, p.dp, s};
         if ((err = launch_product<DT, 9, Logits>(p.logits, a, op)) != hipSuccess) return err;
-        const int enough = (2048 + p.rows_p - 1) / p.rows_p, parts = enough < 4 ? enough : 4;
+        const int enough = 640 / p.rows_p, parts = enough < 1 ? 1 : enough < 4 ? enough : 4;
         auto gradient = p.rows_p * (size_t)p.width * 2 > (size_t)256 << 20 ? head_gradient_kernel<DT, true> : head_gradient_kernel<DT, false>;
         gradient<<<dim3(p.rows_p, parts), dim3(512), 0, s>>>((uint4 *)g, pair, p.pairs, p.strip, hit, target, row_loss, rows, vocab, p.width, x,
                                                              direct ? (uint4 *)xs : nullptr, d);
