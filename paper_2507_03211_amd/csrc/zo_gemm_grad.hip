@@ -188,6 +188,35 @@ using Logits = Product<false, false>;       // x rows, words: both with k inside
 using ByRows = Product<true, true>;         // G^T x: contraction over the rows, outside in both
 using ByWords = Product<false, true>;       // G e: contraction over the words, outside in e
 
+// dx's shares and de in one launch, where few rows have both in 64 x 64 tiles: dx reads e while de is written.  dx first, and rings of two stages,
+// five workgroups to a CU, for both.  us of the whole call, two launches / one: 20 rows of 768 x 50272 64.1 / 61.0 (rings of three 64.3, of four
+// 72.4, de first 64.4, the two interleaved 73.7), 20 of 2048 156.5 / 144.1, 64 of 512 x 10000 27.7 / 25.1, 100 of 512 x 20000 39.8 / 35.9,
+// 20 of 5120 x 8192 70.6 / 67.5.  Long contractions want the deeper ring and stay by themselves: by slabs a
+// share, 1 row of 4096 x 32000 (62) 195.0 / 181.3, 33 of 4096 x 20000 (78) 106.0 / 109.6, 64 of 2048 x 50272 (98) 155.7 / 153.2, 1 of 5120 x 128000
+// (125) 821.9 / 873.4, 20 of 8192 x 50272 (196) 572.7 / 585.7; 4000 rows of 8 x 64, 63 slabs in de, 50.8 / 62.9.
+constexpr int kBothSlabs = 64, kBothRows = 512;
+struct SmallTiles { const uint16_t *x, *w; void *y; int m, n, k, tiles_m, tiles_n, total; };
+constexpr int kBothStages = 2;
+template <int DT>
+__global__ __launch_bounds__(256, 2) void head_both_kernel(SmallTiles a, SmallTiles b, ByWords::Arg op_a, ByRows::Arg op_b, int blocks_a)
+{
+    if ((int)blockIdx.x < blocks_a)
+        small_tile<DT, 7, 1, false, ByWords, kBothStages>(a.x, a.w, nullptr, nullptr, nullptr, a.y, a.m, a.n, a.k, a.tiles_m, a.tiles_n, a.total, op_a, (int)blockIdx.x);
+    else
+        small_tile<DT, 6, 1, false, ByRows, kBothStages>(b.x, b.w, nullptr, nullptr, nullptr, b.y, b.m, b.n, b.k, b.tiles_m, b.tiles_n, b.total, op_b, (int)blockIdx.x - blocks_a);
+}
+template <int DT> hipError_t launch_both(const Args &dx, const ByWords::Arg &op_dx, const Args &de, const ByRows::Arg &op_de)
+{
+    auto tiles = [](const Args &a) {
+        const int tm = (a.m_half + 63) / 64, tn = (a.n + 63) / 64;
+        return SmallTiles{(const uint16_t *)a.x, (const uint16_t *)a.wt_p, a.y, a.m_half, a.n, a.k, tm, tn, a.n_sign * tm * tn};
+    };
+    const SmallTiles a = tiles(dx), b = tiles(de);
+    const int blocks_a = (a.total + 7) / 8 * 8, blocks_b = (b.total + 7) / 8 * 8;
+    head_both_kernel<DT><<<dim3(blocks_a + blocks_b), dim3(256), kBothStages * kSmallStageBytes<1>, dx.s>>>(a, b, op_dx, op_de, blocks_a);
+    return hipGetLastError();
+}
+
 // The tile of least estimated time in us: start + slabs (rounds slab + full busy) + rounds round + operand MB operand + output MB output,
 // where a round of tiles that fills more than half of the CUs also pays slabs busy b, b = 0 .. 1 from half full to full (64 x 64 tiles, two
 // on a CU: slab for one alone, busy for two).  Constants: least relative squares over 2674 shapes (8 - 8192 rows, d 128 - 5120, vocabularies
@@ -358,6 +387,11 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
         head_lse_kernel<<<dim3((rows + 3) / 4), dim3(256), 0, s>>>(pair, p.pairs, hit, target, row_loss, stats, rows, vocab, DT == kFP16 ? 15.0f : 0.0f);
     }
     if ((err = hipGetLastError()) != hipSuccess) return err;
+    ByWords::Arg op_by_words{};
+    op_by_words.ldx = p.width; op_by_words.ldw = d;
+    op_by_words.xz = p.share_words; op_by_words.wz = (uint64_t)p.share_words * d;
+    op_by_words.w_end = (uint64_t)(uintptr_t)(e + (size_t)vocab * d);
+    auto by_words = [&](int v0) { return Args{g, e + (size_t)v0 * d, nullptr, nullptr, nullptr, part, p.shares, rows, d, p.share_words, s}; };
     for (int v0 = 0; v0 < vocab; v0 += p.width) {
         const int words = vocab - v0 < p.width ? vocab - v0 : p.width;
         if (p.pieces > 1) {
@@ -373,21 +407,18 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
             op.alpha = alpha;
             const Words w = pick_words(words, d, p.rows_p / BK);
             const Args a{g, xs, nullptr, nullptr, nullptr, de + (size_t)v0 * d, 1, w.words, d, p.rows_p, s};
+            if (p.pieces == 1 && w.tile == T64x64 && w.words == words && p.by_words == T64x64 && p.share_words <= kBothSlabs * BK && p.rows_p <= kBothRows) {
+                if ((err = launch_both<DT>(by_words(v0), op_by_words, a, op)) != hipSuccess) return err;
+                continue;
+            }
             if ((err = launch_product<DT, 6, ByRows>(w.tile, a, op)) != hipSuccess) return err;
             if (w.words < words) {
                 const Args b{g + w.words, xs, nullptr, nullptr, nullptr, de + (size_t)(v0 + w.words) * d, 1, words - w.words, d, p.rows_p, s};
                 if ((err = launch_product<DT, 6, ByRows>(w.rest, b, op)) != hipSuccess) return err;
             }
         }
-        {
-            ByWords::Arg op{};
-            op.ldx = p.width; op.ldw = d;
-            op.xz = p.share_words; op.wz = (uint64_t)p.share_words * d;
-            op.w_end = (uint64_t)(uintptr_t)(e + (size_t)vocab * d);
-            const Args a{g, e + (size_t)v0 * d, nullptr, nullptr, nullptr, part, p.shares, rows, d, p.share_words, s};
-            err = v0 == 0 ? launch_product<DT, 7, ByWords>(p.by_words, a, op) : launch_product<DT, 8, ByWords>(p.by_words, a, op);
-            if (err != hipSuccess) return err;
-        }
+        err = v0 == 0 ? launch_product<DT, 7, ByWords>(p.by_words, by_words(v0), op_by_words) : launch_product<DT, 8, ByWords>(p.by_words, by_words(v0), op_by_words);
+        if (err != hipSuccess) return err;
     }
     const size_t n8 = (size_t)rows * d / 8;
     auto sum = [&](auto kern, size_t each) {

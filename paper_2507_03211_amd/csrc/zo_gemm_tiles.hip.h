@@ -822,14 +822,15 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
 // m_half 160, n 2560, k 10240: 155 us on 128 x 128 register-staged tiles, 95 on pipelined 128 x 128, 50 here (240 CUs).
 constexpr int kSmallStages = 4;
 template <int TN> constexpr int kSmallStageBytes = (64 + 64 * TN) * BK * 2;
-template <int DT, int EPI, int TN, bool NT, class OP = Plain>
-__global__ __launch_bounds__(256, 2) void linear_mfma_small_kernel(
+template <int DT, int EPI, int TN, bool NT, class OP, int ST>
+__device__ __forceinline__ void small_tile(
     const uint16_t *__restrict__ x, const uint16_t *__restrict__ wt_p, const uint16_t *__restrict__ wt_m, const uint16_t *__restrict__ b_p,
-    const uint16_t *__restrict__ b_m, void *__restrict__ y, int m_half, int n, int k, int tiles_m, int tiles_n, int total, typename OP::Arg op)
+    const uint16_t *__restrict__ b_m, void *__restrict__ y, int m_half, int n, int k, int tiles_m, int tiles_n, int total, const typename OP::Arg &op,
+    int block)
 {
     constexpr bool XK = OP::kXK, WK = OP::kWK;
     constexpr int CHX = 8, CHW = 8 * TN;                        // chunks of a k row, where k lies outside
-    constexpr int ST = kSmallStages, BM = 64, BN = 64 * TN, LX = 2, LW = 2 * TN, L = LX + LW, CPR = BK / 8;
+    constexpr int BM = 64, BN = 64 * TN, LX = 2, LW = 2 * TN, L = LX + LW, CPR = BK / 8;
     constexpr uint32_t kStageBytes = kSmallStageBytes<TN>;
     extern __shared__ __attribute__((aligned(16))) uint4 smem[];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -839,8 +840,8 @@ __global__ __launch_bounds__(256, 2) void linear_mfma_small_kernel(
 
     // consecutive workgroup ids go round-robin to the 8 XCDs; each takes a contiguous share of the tile list
     const int per_xcd = (total + 7) / 8;
-    const int lin = ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3);
-    if (((int)blockIdx.x >> 3) >= per_xcd || lin >= total) return;
+    const int lin = (block & 7) * per_xcd + (block >> 3);
+    if ((block >> 3) >= per_xcd || lin >= total) return;
     int sign, trow, tcol;
     tile_at(lin, tiles_m, tiles_n, sign, trow, tcol);
     const int m0 = trow * BM, n0 = tcol * BN;
@@ -953,6 +954,13 @@ __global__ __launch_bounds__(256, 2) void linear_mfma_small_kernel(
         __syncthreads();                                          // every wave is done with the ring
         store_tile<DT, EPI, 1, TN, NT>(acc, (char *)smem + wave * kTileStageBytes<TN>, sign ? b_m : b_p, y, sign, m_half, n, m0, n0, wm, wn, lane, op);
     }
+}
+template <int DT, int EPI, int TN, bool NT, class OP = Plain>
+__global__ __launch_bounds__(256, 2) void linear_mfma_small_kernel(
+    const uint16_t *__restrict__ x, const uint16_t *__restrict__ wt_p, const uint16_t *__restrict__ wt_m, const uint16_t *__restrict__ b_p,
+    const uint16_t *__restrict__ b_m, void *__restrict__ y, int m_half, int n, int k, int tiles_m, int tiles_n, int total, typename OP::Arg op)
+{
+    small_tile<DT, EPI, TN, NT, OP, kSmallStages>(x, wt_p, wt_m, b_p, b_m, y, m_half, n, k, tiles_m, tiles_n, total, op, (int)blockIdx.x);
 }
 
 // ------------------------------------------------------------------ launchers

@@ -280,6 +280,19 @@ def test_every_tile(dtype, product, tile, rows, d, vocab):
         check(dtype, x, e, target, 0.03125, call(dtype, x, e, target, 0.03125))
 
 
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows,d,vocab,slabs", [(100, 512, 20000, 20), (300, 64, 8192, 5), (65, 72, 50272, 13), (512, 8, 64, 8), (4000, 8, 64, 63), (64, 2048, 50272, 99)])
+def test_small_tiles_together_and_apart(dtype, rows, d, vocab, slabs):
+    """de and dx in 64 x 64 tiles: one launch up to 512 rows and shares of 64 slabs, two beyond."""
+    p = zo_amd.zo_kernel_lmhead_grad_plan(rows, d, vocab)
+    assert p["de"] == p["dx"] == (64, 64) and p["de_words"] == vocab
+    assert max(-(-(-(-vocab // 64)) // p["shares"]), -(-rows // 64)) == slabs
+    for r, v in ((rows, vocab), (rows - 3, vocab - 8)):
+        x, e, target = inputs(dtype, r, d, v, 24)
+        scale = min(0.03125, 1e3 / float(x.abs().max()))
+        check(dtype, x, e, target, scale, call(dtype, x, e, target, scale))
+
+
 @pytest.mark.parametrize("dtype,rows,d,vocab,words,rest", [
     (zi.BF16, 520, 648, 50272, 43520, (192, 128)), (zi.FP16, 520, 968, 20000, 16384, (128, 128)), (zi.BF16, 1024, 392, 33000, 32768, (64, 64)),
     (zi.FP16, 1024, 520, 50272, 43520, (192, 128)), (zi.BF16, 1024, 1032, 33000, 26112, (256, 128)), (zi.FP16, 2048, 264, 33000, 32768, (64, 64)),
