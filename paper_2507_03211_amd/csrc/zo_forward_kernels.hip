@@ -519,7 +519,7 @@ __global__ __launch_bounds__(256) void ce_finish_kernel(const float2 *__restrict
     mx = wave_max(mx);
     double s = 0.0;
     auto add = [&](float2 q) {
-        if (q.x > -INFINITY) s += (double)q.y * exp((double)q.x - (double)mx);
+        if (q.y != 0.0f) s += (double)q.y * exp((double)q.x - (double)mx);      // (NaN is not left out, whatever its maximum)
     };
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256) void head_lse_kernel(const float2 *__restrict_
     mx = wave_max(mx);
     double s = 0.0;
     auto add = [&](float2 q) {
-        if (q.x != -INFINITY) s += (double)q.y * (double)__expf(q.x - mx);
+        if (q.y != 0.0f) s += (double)q.y * (double)__expf(q.x - mx);           // (NaN is not left out, whatever its maximum)
     };
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
@@ -98,9 +98,9 @@ __global__ __launch_bounds__(512) void head_gradient_kernel(uint4 *__restrict__ 
     float mx = -INFINITY;
     for (int i = threadIdx.x; i < n_pairs; i += 512) mx = p[i].x > mx ? p[i].x : mx;
     mx = block_max(mx, red_f);
-    double s = 0.0;                                             // (a strip of NaN alone is not left out: it has no maximum)
+    double s = 0.0;                                             // (a strip with a NaN is not left out, whatever its maximum)
     for (int i = threadIdx.x; i < n_pairs; i += 512)
-        if (p[i].x != -INFINITY) s += (double)p[i].y * (double)__expf(p[i].x - mx);
+        if (p[i].y != 0.0f) s += (double)p[i].y * (double)__expf(p[i].x - mx);
     s = block_sum(s, red_d);
     const double lse = tg < vocab ? log(s) + (double)mx : (double)__builtin_nan("");
     if (threadIdx.x == 0 && blockIdx.y == 0) row_loss[r] = (float)(lse - (double)hit[r]);

@@ -145,8 +145,10 @@ __device__ __forceinline__ float ce_partial_row(f32x16 (&a)[TN], int col0, int f
         if (live && mine) *tgt_logit_row = t[0];
     }
     const float mo = __shfl_xor(mx, 32, 64), so = __shfl_xor(sum, 32, 64);
-    const float m2 = mx > mo ? mx : mo;
-    const float s2 = (mx > -INFINITY ? sum * __expf(mx - m2) : 0.0f) + (mo > -INFINITY ? so * __expf(mo - m2) : 0.0f);
+    const float m2 = __builtin_fmaxf(mx, mo);          // (the number, where the other is none)
+    // a half without a maximum above minus infinity adds its sum as it is: 0, or NaN if one of its logits is
+    auto share = [&](float m, float s) { return m > -INFINITY ? s * __expf(m - m2) : s; };
+    const float s2 = share(mx, sum) + share(mo, so);
     if (live && fh == 0) *partial_slot = float2{m2, s2};
     return m2;
 }

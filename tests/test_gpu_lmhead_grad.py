@@ -325,3 +325,24 @@ def test_sixteen_bits_in_pieces(dtype, rows, d, vocab):
     assert zo_amd.zo_kernel_lmhead_grad_plan(rows, d, vocab)["pieces"] > 1
     x, e, target = inputs(dtype, rows, d, vocab, 12)
     check(dtype, x, e, target, 1.0 / 64, call(dtype, x, e, target, 1.0 / 64))
+
+
+# words of a strip's last, partly filled part and of a strip's halves: a strip of 32 to 128 words is held by two halves of a wavefront, in turns of four
+PARTS = {"first of the last eight": lambda v: torch.arange(v - 8, v - 4), "last four": lambda v: torch.arange(v - 4, v), "last eight": lambda v: torch.arange(v - 8, v),
+         "last one": lambda v: torch.arange(v - 1, v), "last strip": lambda v: torch.arange((v - 1) // 128 * 128, v),
+         "one half's": lambda v: torch.arange(256, 384)[(torch.arange(128) >> 2) % 2 == 0], "other half's": lambda v: torch.arange(256, 384)[(torch.arange(128) >> 2) % 2 == 1]}
+
+
+@pytest.mark.parametrize("dtype,rows,d,vocab", [
+    (zi.BF16, 10, 64, 520), (zi.FP16, 10, 64, 1000), (zi.BF16, 2049, 320, 1000), (zi.FP16, 1048, 200, 3000), (zi.BF16, 1000, 136, 4104), (zi.FP16, 513, 136, 12008),
+    (zi.BF16, 3000, 512, 4104), (zi.BF16, 8300, 64, 66056), (zi.FP16, 8300, 264, 66008), (zi.FP32, 10, 64, 504), (zi.FP32, 100, 16, 6000), (zi.FP32, 2100, 16, 17000)])
+def test_a_few_words_that_are_nan(dtype, rows, d, vocab):
+    """Fewer NaN words than a strip has: every row that counts is NaN throughout, as the formula has it."""
+    x, e, target = inputs(dtype, rows, d, vocab, 17)
+    live = target >= 0
+    for name, words in PARTS.items():
+        bent = e.clone()
+        bent[words(vocab).to(DEV)] = float("nan")
+        loss, dx, de = call(dtype, x, bent, target, 1.0)
+        assert torch.isnan(loss[live]).all() and (loss[~live] == 0).all(), name
+        assert torch.isnan(dx[live]).all() and torch.isnan(de).all(), name
