@@ -241,6 +241,12 @@ __device__ __forceinline__ void gradient_row(f32x16 (&a)[TN], float2 st, int rel
     }
 #pragma unroll
     for (int k = 0; k < 16 * TN; ++k) a[k / 16][k % 16] = __builtin_amdgcn_exp2f(__builtin_fmaf(a[k / 16][k % 16] - st.x, 1.44269504f, st.y));
+    // rows that do not count: zeros whatever the words hold (a word that is not a number gives no number less infinity)
+    const bool none = st.x == INFINITY;
+    if (__builtin_amdgcn_ballot_w64(none) != 0) {
+#pragma unroll
+        for (int k = 0; k < 16 * TN; ++k) a[k / 16][k % 16] = none ? 0.0f : a[k / 16][k % 16];
+    }
     const bool mine = rel >= 0 && rel < 32 * TN && ((rel >> 2) & 1) == fh;
     const int which = mine ? (rel >> 5) * 16 + ((rel >> 3) & 3) * 4 + (rel & 3) : -1;
     if (__builtin_amdgcn_ballot_w64(mine) != 0) {

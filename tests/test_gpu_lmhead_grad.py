@@ -346,3 +346,14 @@ def test_a_few_words_that_are_nan(dtype, rows, d, vocab):
         loss, dx, de = call(dtype, x, bent, target, 1.0)
         assert torch.isnan(loss[live]).all() and (loss[~live] == 0).all(), name
         assert torch.isnan(dx[live]).all() and torch.isnan(de).all(), name
+
+
+@pytest.mark.parametrize("dtype,rows,d,vocab", [(zi.BF16, 40, 64, 1000), (zi.FP16, 600, 128, 4096), (zi.BF16, 8300, 64, 66008), (zi.FP16, 8300, 64, 66008),
+                                                (zi.FP32, 100, 16, 6000), (zi.FP32, 2100, 16, 17000)])
+def test_no_row_counts_and_words_are_nan(dtype, rows, d, vocab):
+    """G is 0 throughout: no word gets a gradient, whatever words hold."""
+    x, e, target = inputs(dtype, rows, d, vocab, 19)
+    e[7], e[vocab - 1], e[vocab // 2] = float("nan"), float("inf"), float("nan")
+    target[:] = -1
+    loss, _, de = call(dtype, x, e, target, 1.0)
+    assert (loss == 0).all() and (de == 0).all()
