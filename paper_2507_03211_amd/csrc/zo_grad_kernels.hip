@@ -314,8 +314,10 @@ __global__ __launch_bounds__(256) void head_stats_kernel(const double *__restric
     RowState st = first_word ? state[r] : RowState{-INFINITY, 0.0, 0.0};
     const int at = target[r] - first_word;
     if (at >= 0 && at < words) st.hit = lg[at];
-    const double top = st.max > ref ? st.max : ref;
-    st.sum = (first_word ? st.sum * exp(st.max - top) : 0.0) + s * exp(ref - top);
+    const double top = st.max > mx ? st.max : mx;
+    // what has no maximum above minus infinity adds its sum as it is: 0, or NaN if one of its logits is
+    auto share = [&](double m, double v) { return m > -INFINITY ? v * exp(m - top) : v; };
+    st.sum = share(st.max, st.sum) + share(mx, s);
     st.max = top;
     state[r] = st;
 }

@@ -357,3 +357,26 @@ def test_no_row_counts_and_words_are_nan(dtype, rows, d, vocab):
     target[:] = -1
     loss, _, de = call(dtype, x, e, target, 1.0)
     assert (loss == 0).all() and (de == 0).all()
+
+
+@pytest.mark.parametrize("words", [slice(0, 15936), slice(15936, 17000), slice(0, 9000)])
+def test_fp32_pieces_of_no_probability(words):
+    """A piece of the vocabulary (15936 words of 2100 rows) whose logits are all minus infinity, while those of the other are about -1000."""
+    rows, d, vocab = 2100, 16, 17000
+    x, e, target = inputs(zi.FP32, rows, d, vocab, 18, lean=0.0)
+    x[:, 0], x[:, 1], e[:, 1] = 1.0, 1000.0, -1.0
+    e[words, 0] = -float("inf")
+    lost = torch.zeros(vocab, dtype=torch.bool, device=DEV)
+    lost[words] = True
+    rest = torch.nonzero(~lost).squeeze(1)
+    live = target >= 0
+    target[live] = rest[target[live].long() % len(rest)].int()
+    loss, _, de = call(zi.FP32, x, e, target, 1.0)
+    # over the words that are left: a sum of d products and of len(rest) exponentials in fp64, values of 1000
+    logits = x @ e[rest].double().t()
+    place = (torch.cumsum(~lost, 0) - 1).clamp(min=0)             # (a row that does not count has none)
+    hit = logits.gather(1, place[target.clamp(min=0).long()][:, None])
+    lse = torch.logsumexp(logits, 1, keepdim=True)
+    want = torch.where(live, (lse - hit).squeeze(1), 0.0)
+    assert ((loss - want).abs() <= 2.0**-50 * 1000 * (16 + d)).all()
+    assert (de[lost] == 0).all() and torch.isfinite(de).all()
