@@ -394,7 +394,8 @@ int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t *target, v
 int zo_kernel_lmhead_grad_plan(int rows, int d, int vocab, int32_t *plan);
 
 /* Global norm of n_tensors gradients and clipping by it: norm[0] = sqrt(sum of all squares), norm[1] = c = max_norm / norm[0] where
- * norm[0] > max_norm, else 1; dst[t] = rn(c src[t]) for every tensor t of numel[t] elements.  A norm that is not a finite number makes c 0 and
+ * norm[0] > max_norm, else 1; dst[t] = rn(c src[t]) for every tensor t of numel[t] elements (2-byte types: c, whatever its size, and the
+ * product rounded to 24 bits first).  A norm that is not a finite number makes c 0 and
  * every dst zeros, as a g that is not finite leaves theta alone.  The sums are taken in fp64.
  *   src, dst, numel  host arrays of n_tensors device pointers and counts, read before the call returns; tensors of dtype's storage
  *                    type, 16-byte aligned.  dst[t] may be src[t], and otherwise overlaps no tensor (ZO_EINVAL if it does: a

@@ -522,6 +522,9 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(ClipBatchOf<N> b, const
     const bool finite = norm - norm == 0.0;
     const double coef = !finite ? 0.0 : norm > (double)max_norm ? (double)max_norm / norm : 1.0;
     if (write_norm && blockIdx.x == 0 && threadIdx.x == 0) { out[0] = norm; out[1] = coef; }
+    // c as a fraction from a half to one and a power of two: c itself may lie beyond fp32's range where c src does not
+    int power;
+    const float fraction = (float)frexp(coef, &power);
     for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
         const ClipPlace t = clip_place(b, c);
         if (coef == 1.0 && t.dst == t.src) continue;
@@ -532,9 +535,9 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(ClipBatchOf<N> b, const
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float g = P::w2f(clip_element<W>(v, e));
-                // fp32: the product in fp64, rounded once.  16-bit types: the fp32 product's rounding is 2^-13 of theirs and less
+                // fp32: the product in fp64, rounded once.  16-bit types: c's rounding to fp32 and the product's are 2^-12 of their half step and less
                 if constexpr (DT == kFP32) o.w[e] = finite ? (float)(coef * (double)g) : 0.0f;
-                else o.w[e] = P::f2w(finite ? (float)coef * g : 0.0f);
+                else o.w[e] = P::f2w(finite ? ldexpf(fraction * g, power) : 0.0f);
             }
             if (i + E <= n) __builtin_nontemporal_store(o.v, (u32x4 *)(dst + i));
             else

@@ -167,3 +167,15 @@ def test_bytes_of_a_model():
     for a, n in zip(firsts, numels):
         hit[a:a + n] = True
     assert (out[~hit] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,size,max_norm", [
+    (zi.BF16, 1e38, 1.0), (zi.BF16, 1e38, 1e-3), (zi.BF16, 1e38, 1e-6), (zi.BF16, 1e38, 2.0**-126), (zi.BF16, 1e30, 2.0**-100), (zi.BF16, 1.0, 2.0**-120),
+    (zi.FP16, 1e4, 2.0**-10), (zi.FP16, 1e4, 2.0**-20), (zi.FP32, 1e38, 1e-6), (zi.FP32, 1e38, 2.0**-126)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_coefficients_below_fp32s_range(dtype, size, max_norm, in_place):
+    """Norms up to 2^250 times the limit: the coefficient itself is beyond fp32 (bf16, fp32), what it makes of a gradient is not."""
+    g = generator(12)
+    src = [(normal((n,), torch.float64, g).clamp(-3, 3) * size).to(param_dtype(dtype)) for n in (40000, 77, 1)]
+    max_norm = float(torch.tensor(max_norm, dtype=torch.float32))
+    check(dtype, src, max_norm, clip(dtype, src, max_norm, in_place))
