@@ -228,3 +228,50 @@ def test_buffers_off_their_alignment(dtype, d):
         zo_amd.zo_kernel_layernorm(move(h), move(gain), move(bias), y, mean, rstd, dtype, rows, d, EPS)
         outs.append(y.double())
     assert ((outs[0] - outs[1]).abs() <= 2 * half(act_dtype(dtype)) * outs[0].abs() + 2.0**-16).all()
+
+
+# more rows than the kernel for few of them takes, in numbers that fill no workgroup's share: every size of a row that stays in registers, by
+# fours and one by one, each at its longest and in between, and rows beyond it
+MANY = [(257, 4), (261, 256), (1003, 300), (1003, 512), (517, 772), (517, 1000), (1003, 1024), (1003, 1280), (517, 1300), (1003, 1536), (517, 1540),
+        (517, 2048), (1003, 2560), (301, 3076), (517, 4096), (301, 4100), (259, 5124), (301, 8192), (259, 8196), (301, 12288), (259, 12292),
+        (1003, 1), (1003, 511), (517, 513), (517, 2047), (301, 2049), (301, 4095), (301, 4097), (259, 5003), (259, 8191), (259, 8193)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,d", MANY)
+def test_backward_of_many_rows(dtype, rows, d):
+    c = case(dtype, rows, d, 6)
+    both = backward(dtype, rows, d, *c)
+    check_backward(dtype, rows, d, *c, both)
+    before = normal((rows, d), resid_dtype(dtype), generator(4), 0.2)
+    added = backward(dtype, rows, d, *c, before=before)
+    check_backward(dtype, rows, d, *c, added, before=before)
+    only_dh = backward(dtype, rows, d, *c, weights=False)
+    only_w = backward(dtype, rows, d, *c, dresid=False)
+    assert torch.equal(both[0], only_dh[0])
+    for i in (1, 2):
+        assert torch.equal(both[i], only_w[i]) and torch.equal(both[i], added[i])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 768, 1536, 2048, 4096, 5120, 8192, 12288])
+@pytest.mark.parametrize("which", range(4))
+def test_many_rows_off_their_alignment(dtype, d, which):
+    """One of dy, resid, gain and dresid starts an element behind a boundary, where rows would else be taken by fours."""
+    rows = 301
+    dy, h, gain, m, r = case(dtype, rows, d, 7)
+
+    def shifted(t):
+        raw = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+        raw[1:] = t.reshape(-1)
+        return raw[1:].view(t.shape)
+
+    ins = [shifted(t) if which == i else t for i, t in enumerate((dy, h, gain))]
+    guard = torch.full((rows * d + 2,), 7.0, dtype=resid_dtype(dtype), device=DEV)
+    dh = guard[1:-1].view(rows, d) if which == 3 else torch.empty((rows, d), dtype=resid_dtype(dtype), device=DEV)
+    dg, db = (Out((d,), param_dtype(dtype)) for _ in range(2))
+    scratch = Out((zo_amd.zo_kernel_layernorm_grad_scratch_bytes(dtype, rows, d),), torch.uint8)
+    zo_amd.zo_kernel_layernorm_grad(*ins, m, r, dh, dg.t, db.t, scratch.t, dtype, rows, d, False)
+    torch.cuda.synchronize()
+    assert scratch.whole() and dg.whole() and db.whole() and guard[0] == 7.0 and guard[-1] == 7.0
+    check_backward(dtype, rows, d, dy, h, gain, m, r, (dh, dg.t, db.t))
