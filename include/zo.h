@@ -400,7 +400,9 @@ int zo_kernel_lmhead_grad_plan(int rows, int d, int vocab, int32_t *plan);
  *   src, dst, numel  host arrays of n_tensors device pointers and counts, read before the call returns; tensors of dtype's storage
  *                    type, 16-byte aligned.  dst[t] may be src[t], and otherwise overlaps no tensor (ZO_EINVAL if it does: a
  *                    tensor clipped in place is listed once).  numel 0: skipped.
- *   max_norm         > 0; infinity for the norm alone (dst[t] = src[t] is then not touched)
+ *   max_norm         > 0.  Infinity: no finite norm is clipped, dst[t] = src[t] is not touched and another dst[t] is a copy; but a norm that
+ *                    is not finite makes every dst zeros at this max_norm too, dst[t] = src[t] included: to look at such gradients
+ *                    afterwards, give another dst
  *   norm             device, double[2] */
 size_t zo_kernel_grad_clip_scratch_bytes(void);
 int zo_kernel_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm,
