@@ -360,15 +360,15 @@ int zo_kernel_lmhead_ce_noalloc(const void *x, const void *e_plus, const void *e
  * ---------------------------------------------------------------------- */
 
 /* LayerNorm of resid [rows, d] with its statistics kept: mean[r] = sum h / d, rstd[r] = (sum (h - mean)^2 / d + ln_eps)^-1/2,
- * y = gain (h - mean) rstd + bias. */
+ * y = gain (h - mean) rstd + bias.  Outputs overlap neither the inputs nor each other (ZO_EINVAL if they do); ZO_FP32: y may be resid. */
 int zo_kernel_layernorm(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype,
                         int rows, int d, float ln_eps, void *stream);
 
 /* Its backward pass.  With xh = (h - mean) rstd and a = dy gain, per row:
  *     dresid = rstd (a - mean_c(a) - xh mean_c(a xh)),    dgain = sum_r dy xh,    dbias = sum_r dy.
  * accumulate non-zero: dresid is added to what the buffer holds (the gradient that passes the LayerNorm by on the residual
- * stream).  dresid may be NULL (gain may be, then), or dgain and dbias both (scratch may be, then).  dresid may not overlap
- * the inputs.  Both calls: up to 2^23 rows, d up to 2^22. */
+ * stream).  dresid may be NULL (gain may be, then), or dgain and dbias both (scratch may be, then).  Outputs
+ * overlap neither the inputs nor each other (ZO_EINVAL if they do).  Both calls: up to 2^23 rows, d up to 2^22. */
 size_t zo_kernel_layernorm_grad_scratch_bytes(int dtype, int rows, int d);
 int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid,
                              void *dgain, void *dbias, void *scratch, int dtype, int rows, int d, int accumulate, void *stream);

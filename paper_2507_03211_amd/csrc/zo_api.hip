@@ -1341,6 +1341,18 @@ extern "C" int zo_kernel_lmhead_ce_noalloc(const void *x, const void *e_plus, co
 }
 
 // ------------------------------------------------------------------ gradient of the last module
+// A call's buffers, the outputs first: ZO_EINVAL if one of these overlaps any other.  NULL ones are left out.
+struct Buffer { const char *name; const void *at; size_t bytes; };
+template <int N> static int check_apart(const Buffer (&b)[N], int outputs)
+{
+    for (int i = 0; i < outputs; ++i)
+        for (int j = i + 1; j < N; ++j) {
+            const uintptr_t p = (uintptr_t)b[i].at, q = (uintptr_t)b[j].at;
+            if (p && q && (p < q ? q - p < b[i].bytes : p - q < b[j].bytes)) return fail(ZO_EINVAL, "%s overlaps %s", b[i].name, b[j].name);
+        }
+    return ZO_OK;
+}
+
 static bool norm_shape(int rows, int d) { return rows >= 1 && rows <= 1 << 23 && d >= 1 && d <= 1 << 22; }      // (a workgroup a row: grids of 2^32 threads)
 
 extern "C" int zo_kernel_layernorm(const void *resid, const void *gain, const void *bias, void *y, void *mean, void *rstd, int dtype, int rows, int d,
@@ -1350,6 +1362,11 @@ extern "C" int zo_kernel_layernorm(const void *resid, const void *gain, const vo
     if (!resid || !gain || !bias || !y || !mean || !rstd) return fail(ZO_EINVAL, "NULL argument");
     if (!norm_shape(rows, d)) return fail(ZO_EINVAL, "bad shape %d x %d", rows, d);
     if (!(ln_eps > 0.0f)) return fail(ZO_EINVAL, "ln_eps must be positive");
+    const size_t n = (size_t)rows * d, stat = rows * resid_bytes(dtype), weight = d * elem_bytes(dtype);
+    const bool in_place = dtype == ZO_FP32 && y == resid;       // one type, and a thread writes what it alone reads last
+    const Buffer buffers[] = {{"y", y, n * act_bytes(dtype)}, {"mean", mean, stat}, {"rstd", rstd, stat},
+                              {"resid", in_place ? nullptr : resid, n * resid_bytes(dtype)}, {"gain", gain, weight}, {"bias", bias, weight}};
+    ZO_TRY(check_apart(buffers, 3));
     ZO_HIP(launch_layernorm_stats(resid, gain, bias, y, mean, rstd, dtype, rows, d, ln_eps, (hipStream_t)stream));
     return ZO_OK;
 }
@@ -1370,6 +1387,10 @@ extern "C" int zo_kernel_layernorm_grad(const void *dy, const void *resid, const
     if (dresid && !gain) return fail(ZO_EINVAL, "gain is NULL");
     if (dgain && !scratch_mem) return fail(ZO_EINVAL, "scratch is NULL");
     if (dgain && (uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");
+    const size_t n = (size_t)rows * d, stat = rows * resid_bytes(dtype), weight = d * elem_bytes(dtype);
+    const Buffer buffers[] = {{"dresid", dresid, n * resid_bytes(dtype)}, {"dgain", dgain, weight}, {"dbias", dbias, weight}, {"dy", dy, n * act_bytes(dtype)},
+                              {"resid", resid, n * resid_bytes(dtype)}, {"gain", dresid ? gain : nullptr, weight}, {"mean", mean, stat}, {"rstd", rstd, stat}};
+    ZO_TRY(check_apart(buffers, 3));
     ZO_HIP(launch_layernorm_grad(dy, resid, gain, mean, rstd, dresid, dgain, dbias, scratch_mem, dtype, rows, d, accumulate != 0, (hipStream_t)stream));
     return ZO_OK;
 }

@@ -275,3 +275,16 @@ def test_many_rows_off_their_alignment(dtype, d, which):
     torch.cuda.synchronize()
     assert scratch.whole() and dg.whole() and db.whole() and guard[0] == 7.0 and guard[-1] == 7.0
     check_backward(dtype, rows, d, dy, h, gain, m, r, (dh, dg.t, db.t))
+
+
+@pytest.mark.parametrize("rows,d", [(5, 7), (67, 64), (1003, 768), (3, 13001)])
+def test_fp32_in_place(rows, d):
+    """fp32 parameters: y over the residual stream it is made of, bit for bit as beside it."""
+    g, h, gain = rows_of(zi.FP32, rows, d, 11)
+    bias = normal((d,), torch.float32, g, 0.3)
+    outs = []
+    for y in (torch.empty_like(h), h.clone()):
+        mean, rstd = (torch.empty(rows, dtype=torch.float64, device=DEV) for _ in range(2))
+        zo_amd.zo_kernel_layernorm(y if len(outs) else h, gain, bias, y, mean, rstd, zi.FP32, rows, d, EPS)
+        outs.append((y, mean, rstd))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))

@@ -92,3 +92,37 @@ def test_grad_clip():
         f([P], [P, P], [4, 4], 2, ZO_BF16, 1.0, P, P)                       # a table shorter than n_tensors
     with pytest.raises(TypeError):
         f((ctypes.c_uint64 * 1)(P), [P], [4], 1, ZO_BF16, 1.0, P, P)         # an array of another type
+
+
+def overlaps(f, args, moves):
+    """`moves`: (argument, address, words of the refusal)."""
+    for at, address, words in moves:
+        assert words in refused(f, *(args[:at] + [address] + args[at + 1:]))
+
+
+A = [(i + 1) << 20 for i in range(9)]                           # buffers that lie apart
+
+
+def test_layernorm_outputs_lie_apart():
+    for dtype, wide, narrow, weight in ((ZO_FP32, 8, 8, 4), (ZO_BF16, 4, 2, 2), (ZO_FP16, 4, 2, 2)):
+        args = A[:6] + [dtype, 4, 64, 1e-5]                     # resid gain bias y mean rstd
+        resid, gain, bias, y, mean, rstd = A[:6]
+        moves = [(3, resid + 256 * wide - narrow, "y overlaps resid"), (3, resid - 256 * narrow + 1, "y overlaps resid"), (3, gain, "y overlaps gain"),
+                 (3, bias + 64 * weight - 2, "y overlaps bias"), (4, y + 255 * narrow, "y overlaps mean"), (5, mean, "mean overlaps rstd"), (5, mean + 3 * wide, "mean overlaps rstd"),
+                 (5, resid, "rstd overlaps resid"), (4, gain, "mean overlaps gain")]
+        if dtype != ZO_FP32:
+            moves.append((3, resid, "y overlaps resid"))
+        overlaps(zo_amd.zo_kernel_layernorm, args, moves)
+
+
+def test_layernorm_gradients_lie_apart():
+    for dtype, wide, narrow, weight in ((ZO_FP32, 8, 8, 4), (ZO_BF16, 4, 2, 2), (ZO_FP16, 4, 2, 2)):
+        for rows in (4, 1000):
+            #       dy resid gain mean rstd dresid dgain dbias scratch
+            args = A[:9] + [dtype, rows, 64, False]
+            dy, resid, gain, mean, rstd, dresid, dgain, dbias = A[:8]
+            overlaps(zo_amd.zo_kernel_layernorm_grad, args, [
+                (5, resid, "dresid overlaps resid"), (5, dy, "dresid overlaps dy"), (5, dy + 64 * rows * narrow - 1, "dresid overlaps dy"), (6, gain, "dgain overlaps gain"),
+                (7, gain, "dbias overlaps gain"), (6, dbias, "dgain overlaps dbias"), (7, dgain + 64 * weight - 1, "dgain overlaps dbias"),
+                (6, dy + 2, "dgain overlaps dy"), (7, mean, "dbias overlaps mean"), (6, rstd + rows * wide - 2, "dgain overlaps rstd"),
+                (6, dresid + 64 * (rows - 1) * wide, "dresid overlaps dgain")])
