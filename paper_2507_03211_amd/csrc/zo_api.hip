@@ -1395,13 +1395,18 @@ extern "C" int zo_kernel_layernorm_grad(const void *dy, const void *resid, const
     return ZO_OK;
 }
 
-// Sizes the kernels' 32-bit offsets and launch grids hold, far beyond any in use.
+// Sizes the kernels' 32-bit offsets hold, far beyond any in use.  What a launch grid holds is up to the plan of a call.
 constexpr int kMaxGradRows = 1 << 20, kMaxGradColumns = 1 << 22;
 
 static bool lmhead_grad_shape(int dtype, int rows, int d, int vocab)
 {
     return rows >= 1 && rows <= kMaxGradRows && d >= 1 && d <= kMaxGradColumns && vocab >= 2 && vocab <= kMaxGradColumns &&
            (dtype == ZO_FP32 || (d % 8 == 0 && vocab % 8 == 0));
+}
+
+static int head_grad_too_large(int rows, int d, int vocab)
+{
+    return fail(ZO_EINVAL, "%d rows, d %d, vocab %d: a product has more tiles than one launch holds", rows, d, vocab);
 }
 
 extern "C" size_t zo_kernel_lmhead_grad_scratch_bytes(int dtype, int rows, int d, int vocab)
@@ -1413,8 +1418,7 @@ extern "C" int zo_kernel_lmhead_grad_plan(int rows, int d, int vocab, int32_t *p
 {
     if (!plan) return fail(ZO_EINVAL, "plan is NULL");
     if (!lmhead_grad_shape(ZO_BF16, rows, d, vocab)) return fail(ZO_EINVAL, "bad shape: %d rows, d %d, vocab %d", rows, d, vocab);
-    head_grad_mfma_plan(rows, d, vocab, plan);
-    return ZO_OK;
+    return head_grad_mfma_plan(rows, d, vocab, plan) ? ZO_OK : head_grad_too_large(rows, d, vocab);
 }
 
 extern "C" int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch_mem, int dtype,
@@ -1428,7 +1432,9 @@ extern "C" int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t
         return fail(ZO_EINVAL, "buffers must be 16-byte aligned");
     if ((uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");
     if (!(scale - scale == 0.0f)) return fail(ZO_EINVAL, "scale must be a finite number");
-    ZO_HIP(launch_head_grad(x, e, target, row_loss, dx, de, scratch_mem, dtype, rows, d, vocab, scale, (hipStream_t)stream));
+    const hipError_t err = launch_head_grad(x, e, target, row_loss, dx, de, scratch_mem, dtype, rows, d, vocab, scale, (hipStream_t)stream);
+    if (err == hipErrorNotSupported) return head_grad_too_large(rows, d, vocab);
+    ZO_HIP(err);
     return ZO_OK;
 }
 

@@ -308,8 +308,17 @@ constexpr size_t kPieceBytes = 1u << 30;
 struct HeadPlan {
     int rows_p, dp, width, pieces, shares, share_words, pairs, strip;
     Tile logits, by_words;
+    Words by_rows;                              // of a whole piece
+    bool both;                                  // de and dx in one launch
+    bool fits;                                  // every launch's tiles
     size_t xs, g, stats, pair, hit, part, total;
 };
+// A launch's size is counted in threads, by 32 bits: workgroups of 256, one a tile where tiles are 64 x 64 (the larger ones' kernel has one a CU).
+constexpr int64_t kMostBlocks = (1ll << 24) - 8;
+int64_t small_blocks(Tile t, int shares, int m, int n)
+{
+    return t == T64x64 ? ((int64_t)shares * ((m + 63) / 64) * ((n + 63) / 64) + 7) / 8 * 8 : 0;
+}
 HeadPlan head_plan(int rows, int d, int vocab)
 {
     HeadPlan p{};
@@ -334,6 +343,12 @@ HeadPlan head_plan(int rows, int d, int vocab)
     p.logits = pick_product(kLogits, 1, p.rows_p, columns, p.dp / BK);
     p.strip = kTileColumns[p.logits] / 2;                        // a wavefront's columns of the tile
     p.pairs = 2 * ((columns + kTileColumns[p.logits] - 1) / kTileColumns[p.logits]);
+    const int words = vocab < p.width ? vocab : p.width;
+    p.by_rows = pick_words(words, d, p.rows_p / BK);
+    p.both = p.pieces == 1 && p.by_rows.tile == T64x64 && p.by_rows.words == words && p.by_words == T64x64 && p.share_words <= kBothSlabs * BK && p.rows_p <= kBothRows;
+    // (a piece's logits are 2^30 bytes; its words behind whole rounds of tiles are fewer than a round)
+    const int64_t de = small_blocks(p.by_rows.tile, 1, p.by_rows.words, d), dx = small_blocks(p.by_words, p.shares, rows, d);
+    p.fits = small_blocks(p.logits, 1, p.rows_p, columns) <= kMostBlocks && de <= kMostBlocks && dx <= kMostBlocks && (!p.both || de + dx <= kMostBlocks);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up(o + bytes); return at; };
     p.xs = take(2 * (size_t)p.rows_p * p.dp);
@@ -351,6 +366,7 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
                      int vocab, float scale, hipStream_t s)
 {
     const HeadPlan p = head_plan(rows, d, vocab);
+    if (!p.fits) return hipErrorNotSupported;
     uint16_t *xs = (uint16_t *)(ws + p.xs), *g = (uint16_t *)(ws + p.g);
     float2 *stats = (float2 *)(ws + p.stats);
     float *part = (float *)(ws + p.part);
@@ -405,9 +421,9 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
             op.x_end = (uint64_t)(uintptr_t)(g + (size_t)p.rows_p * p.width);
             op.w_end = (uint64_t)(uintptr_t)(xs + (size_t)p.rows_p * p.dp);
             op.alpha = alpha;
-            const Words w = pick_words(words, d, p.rows_p / BK);
+            const Words w = words == p.width || p.pieces == 1 ? p.by_rows : pick_words(words, d, p.rows_p / BK);
             const Args a{g, xs, nullptr, nullptr, nullptr, de + (size_t)v0 * d, 1, w.words, d, p.rows_p, s};
-            if (p.pieces == 1 && w.tile == T64x64 && w.words == words && p.by_words == T64x64 && p.share_words <= kBothSlabs * BK && p.rows_p <= kBothRows) {
+            if (p.both) {
                 if ((err = launch_both<DT>(by_words(v0), op_by_words, a, op)) != hipSuccess) return err;
                 continue;
             }
@@ -432,20 +448,25 @@ hipError_t head_grad(const uint16_t *x, const uint16_t *e, const int32_t *target
 
 }  // namespace
 
-size_t head_grad_mfma_scratch(int rows, int d, int vocab) { return head_plan(rows, d, vocab).total; }
-
-void head_grad_mfma_plan(int rows, int d, int vocab, int32_t *plan)
+size_t head_grad_mfma_scratch(int rows, int d, int vocab)
 {
     const HeadPlan p = head_plan(rows, d, vocab);
+    return p.fits ? p.total : 0;
+}
+
+bool head_grad_mfma_plan(int rows, int d, int vocab, int32_t *plan)
+{
+    const HeadPlan p = head_plan(rows, d, vocab);
+    if (!p.fits) return false;
     auto tile = [](Tile t) { return kTileRows[t] << 16 | kTileColumns[t]; };
     plan[0] = tile(pick_product(kLogits, 1, p.rows_p, p.width, p.dp / BK));
-    const Words w = pick_words(p.pieces == 1 ? vocab : p.width, d, p.rows_p / BK);
-    plan[1] = tile(w.tile);
+    plan[1] = tile(p.by_rows.tile);
     plan[2] = tile(p.by_words);
     plan[3] = p.shares;
     plan[4] = p.pieces;
-    plan[5] = w.words;
-    plan[6] = tile(w.rest);
+    plan[5] = p.by_rows.words;
+    plan[6] = tile(p.by_rows.rest);
+    return true;
 }
 
 hipError_t launch_head_grad_mfma(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype, int rows,

@@ -635,6 +635,16 @@ int head_f64_width(int rows, int vocab)
     const long w = (1l << 25) / rows / 64 * 64;
     return w >= vocab ? vocab : (int)(w < 64 ? 64 : w);
 }
+// 32 x 32 outputs a workgroup where dx has enough of them (or de too many of 16 x 16 for a grid of 2^32 threads)
+bool head_f64_many(int rows, int d, int words)
+{
+    return (long)((rows + 31) / 32) * ((d + 31) / 32) >= 256 || (long)((words + 15) / 16) * ((d + 15) / 16) > 1l << 22;
+}
+// Does a grid, counted in threads by 32 bits, hold both products' workgroups of 256?
+bool head_f64_fits(int rows, int d, int vocab)
+{
+    return ((long)((rows + 31) / 32) + (head_f64_width(rows, vocab) + 31) / 32) * ((d + 31) / 32) < 1l << 24;
+}
 size_t head_f64_state(int rows) { return ((size_t)rows * sizeof(RowState) + 255) / 256 * 256; }
 
 hipError_t head_grad_f64(const double *x, const float *e, const int32_t *target, double *row_loss, double *dx, float *de, void *scratch, int rows, int d,
@@ -674,9 +684,7 @@ hipError_t head_grad_f64(const double *x, const float *e, const int32_t *target,
                                                                                    scale, v0 > 0, (int)dx_tiles);
             return hipGetLastError();
         };
-        // 32 x 32 outputs a workgroup where dx has enough of them (or de too many of 16 x 16 for a grid of 2^32 threads)
-        const bool many = (long)((rows + 31) / 32) * ((d + 31) / 32) >= 256 || (long)((n + 15) / 16) * ((d + 15) / 16) > 1l << 22;
-        if ((err = many ? products(head_products_kernel<2, 4>, 32, 4) : products(head_products_kernel<1, 8>, 16, 8)) != hipSuccess) return err;
+        if ((err = head_f64_many(rows, d, n) ? products(head_products_kernel<2, 4>, 32, 4) : products(head_products_kernel<1, 8>, 16, 8)) != hipSuccess) return err;
     }
     return hipSuccess;
 }
@@ -685,6 +693,7 @@ hipError_t head_grad_f64(const double *x, const float *e, const int32_t *target,
 size_t head_grad_scratch(int dtype, int rows, int d, int vocab)
 {
     if (dtype != kFP32) return head_grad_mfma_scratch(rows, d, vocab);
+    if (!head_f64_fits(rows, d, vocab)) return 0;
     return head_f64_state(rows) + (size_t)rows * head_f64_width(rows, vocab) * sizeof(double);
 }
 
@@ -692,6 +701,7 @@ hipError_t launch_head_grad(const void *x, const void *e, const int32_t *target,
                             int d, int vocab, float scale, hipStream_t s)
 {
     if (dtype != kFP32) return launch_head_grad_mfma(x, e, target, row_loss, dx, de, scratch, dtype, rows, d, vocab, scale, s);
+    if (!head_f64_fits(rows, d, vocab)) return hipErrorNotSupported;
     return head_grad_f64((const double *)x, (const float *)e, target, (double *)row_loss, (double *)dx, (float *)de, scratch, rows, d, vocab, (double)scale, s);
 }
 

@@ -116,12 +116,13 @@ hipError_t launch_layernorm_stats(const void *resid, const void *gain, const voi
 size_t layernorm_grad_scratch(int dtype, int rows, int d);
 hipError_t launch_layernorm_grad(const void *dy, const void *resid, const void *gain, const void *mean, const void *rstd, void *dresid, void *dgain,
                                  void *dbias, void *scratch, int dtype, int rows, int d, bool accumulate, hipStream_t s);
+// 0 bytes, hipErrorNotSupported (before anything is launched) and no plan where a product has more tiles than a launch holds
 size_t head_grad_scratch(int dtype, int rows, int d, int vocab);
 hipError_t launch_head_grad(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype,
                             int rows, int d, int vocab, float scale, hipStream_t s);
 // the same on the matrix cores (16-bit types; d and vocab multiples of 8, buffers on 16 bytes)
 size_t head_grad_mfma_scratch(int rows, int d, int vocab);
-void head_grad_mfma_plan(int rows, int d, int vocab, int32_t *plan);      // see zo_kernel_lmhead_grad_plan
+bool head_grad_mfma_plan(int rows, int d, int vocab, int32_t *plan);      // see zo_kernel_lmhead_grad_plan
 hipError_t launch_head_grad_mfma(const void *x, const void *e, const int32_t *target, void *row_loss, void *dx, void *de, void *scratch, int dtype,
                                  int rows, int d, int vocab, float scale, hipStream_t s);
 

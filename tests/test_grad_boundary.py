@@ -126,3 +126,19 @@ def test_layernorm_gradients_lie_apart():
                 (7, gain, "dbias overlaps gain"), (6, dbias, "dgain overlaps dbias"), (7, dgain + 64 * weight - 1, "dgain overlaps dbias"),
                 (6, dy + 2, "dgain overlaps dy"), (7, mean, "dbias overlaps mean"), (6, rstd + rows * wide - 2, "dgain overlaps rstd"),
                 (6, dresid + 64 * (rows - 1) * wide, "dresid overlaps dgain")])
+
+
+@pytest.mark.parametrize("dtype,rows,d,vocab", [
+    (ZO_BF16, 1 << 20, 64, 1 << 17), (ZO_FP16, 1 << 20, 128, 1 << 22), (ZO_BF16, 1 << 18, 8, 1 << 18), (ZO_FP16, 100, 1 << 14, 1 << 22), (ZO_BF16, 128, 1 << 15, 1 << 21),
+    (ZO_FP32, 1, 1 << 12, 1 << 22), (ZO_FP32, 1 << 20, 1 << 14, 64)])
+def test_lmhead_grad_of_more_tiles_than_a_launch_holds(dtype, rows, d, vocab):
+    """Grids count threads by 32 bits: 2^24 workgroups of 256, refused before anything is launched.  A quarter of each such size is taken."""
+    assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab) == 0
+    assert "tiles" in refused(zo_amd.zo_kernel_lmhead_grad, *A[:7], dtype, rows, d, vocab, 1.0)
+    quarter = (rows >> 2, d, vocab) if rows > 1 << 10 else (rows, d >> 2, vocab)
+    if rows * vocab < 1 << 40:
+        assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, *quarter) > 0
+    if dtype != ZO_FP32:
+        assert "tiles" in refused(zo_amd.zo_kernel_lmhead_grad_plan, rows, d, vocab)
+        # with more to do for each tile the products have larger ones, which do not count
+        assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, max(rows, 256), max(d, 256), vocab) > 0
