@@ -378,7 +378,7 @@ int zo_kernel_layernorm_grad(const void *dy, const void *resid, const void *gain
  * A row with target[r] < 0 does not count: row_loss, its row of G and its row of dx (of a finite e) are 0 whatever x[r] holds, NaN included.  A
  * target >= vocab makes the row's loss NaN, and dx[r] and de with it.  scale: 1 / (rows that count) for the mean loss, times
  * whatever keeps ZO_FP16 gradients in range.  de is the head's share of the tied embedding's gradient alone.  Outputs overlap
- * nothing.  Up to 2^20 rows, d and vocab up to 2^22; 2-byte dtypes: d and vocab multiples of 8, buffers 16-byte aligned
+ * nothing (ZO_EINVAL if they overlap inputs or each other).  Up to 2^20 rows, d and vocab up to 2^22; 2-byte dtypes: d and vocab multiples of 8, buffers 16-byte aligned
  * (ZO_EINVAL otherwise).  Nor does a call take products of more tiles than a launch holds (ZO_EINVAL, and 0 scratch bytes): 2-byte
  * dtypes, rows x vocab of about 2^36 and more with d up to 128, vocab x d so with up to 128 rows; ZO_FP32, (rows + vocab) x d of about 2^34.
  * 2-byte dtypes round G to their type between the products (each sum is off by about as much as its own rounding once more), and

@@ -1432,6 +1432,10 @@ extern "C" int zo_kernel_lmhead_grad(const void *x, const void *e, const int32_t
         return fail(ZO_EINVAL, "buffers must be 16-byte aligned");
     if ((uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");
     if (!(scale - scale == 0.0f)) return fail(ZO_EINVAL, "scale must be a finite number");
+    const size_t n_x = (size_t)rows * d * act_bytes(dtype), n_e = (size_t)vocab * d * elem_bytes(dtype);
+    const Buffer buffers[] = {{"row_loss", row_loss, rows * resid_bytes(dtype)}, {"dx", dx, n_x}, {"de", de, n_e}, {"x", x, n_x}, {"e", e, n_e},
+                              {"target", target, rows * sizeof(int32_t)}};
+    ZO_TRY(check_apart(buffers, 3));
     const hipError_t err = launch_head_grad(x, e, target, row_loss, dx, de, scratch_mem, dtype, rows, d, vocab, scale, (hipStream_t)stream);
     if (err == hipErrorNotSupported) return head_grad_too_large(rows, d, vocab);
     ZO_HIP(err);

@@ -134,7 +134,7 @@ def test_layernorm_gradients_lie_apart():
 def test_lmhead_grad_of_more_tiles_than_a_launch_holds(dtype, rows, d, vocab):
     """Grids count threads by 32 bits: 2^24 workgroups of 256, refused before anything is launched.  A quarter of each such size is taken."""
     assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, rows, d, vocab) == 0
-    assert "tiles" in refused(zo_amd.zo_kernel_lmhead_grad, *A[:7], dtype, rows, d, vocab, 1.0)
+    assert "tiles" in refused(zo_amd.zo_kernel_lmhead_grad, *[(i + 1) << 44 for i in range(7)], dtype, rows, d, vocab, 1.0)
     quarter = (rows >> 2, d, vocab) if rows > 1 << 10 else (rows, d >> 2, vocab)
     if rows * vocab < 1 << 40:
         assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, *quarter) > 0
@@ -142,3 +142,12 @@ def test_lmhead_grad_of_more_tiles_than_a_launch_holds(dtype, rows, d, vocab):
         assert "tiles" in refused(zo_amd.zo_kernel_lmhead_grad_plan, rows, d, vocab)
         # with more to do for each tile the products have larger ones, which do not count
         assert zo_amd.zo_kernel_lmhead_grad_scratch_bytes(dtype, max(rows, 256), max(d, 256), vocab) > 0
+
+
+def test_lmhead_gradients_lie_apart():
+    for dtype, wide, narrow, weight in ((ZO_FP32, 8, 8, 4), (ZO_BF16, 4, 2, 2), (ZO_FP16, 4, 2, 2)):
+        args = A[:7] + [dtype, 4, 64, 512, 1.0]                  # x e target row_loss dx de scratch
+        x, e, target, row_loss, dx, de = A[:6]
+        overlaps(zo_amd.zo_kernel_lmhead_grad, args, [
+            (4, x, "dx overlaps x"), (4, x + 256 * narrow - 16, "dx overlaps x"), (5, e, "de overlaps e"), (5, e - 16, "de overlaps e"), (5, x - 512 * 64 * weight + 16, "de overlaps x"),
+            (4, de + 16, "dx overlaps de"), (3, target, "row_loss overlaps target"), (3, dx + 256 * narrow - wide, "row_loss overlaps dx"), (4, target, "dx overlaps target")])
