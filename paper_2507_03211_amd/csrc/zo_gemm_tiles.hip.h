@@ -120,7 +120,8 @@ __device__ __forceinline__ float ce_partial_row(f32x16 (&a)[TN], int col0, int f
     // from 2 up is lost in the sum, and base 2 needs no scale: c = mx, differences exact.
     // LM head of 50272 columns, before -> after in us: 8176 rows a sign, d 768, 1071 -> 1056; 2048 rows 286 -> 279; 1048
     // rows, d 2048, 391 -> 387.  Error against fp64 unchanged (rms 2.6e-7 at logits of about 1, 3.4e-6 at 8).
-    const float ms = mx > -INFINITY ? mx : 0.0f;      // a strip that lies wholly past the vocabulary: 2^(-inf - 0) = 0
+    // (no logit above minus infinity, as past the vocabulary, or none that is a number: the lowest number, and the sum is 0 or NaN)
+    const float ms = __builtin_fmaxf(mx, -0x1.fffffep127f);
     const float L = __builtin_fabsf(ms) > 0x1p30f ? 1.0f : 1.44269504f, c = ms * L;
     float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -144,11 +145,9 @@ __device__ __forceinline__ float ce_partial_row(f32x16 (&a)[TN], int col0, int f
         }
         if (live && mine) *tgt_logit_row = t[0];
     }
-    const float mo = __shfl_xor(mx, 32, 64), so = __shfl_xor(sum, 32, 64);
-    const float m2 = __builtin_fmaxf(mx, mo);          // (the number, where the other is none)
-    // a half without a maximum above minus infinity adds its sum as it is: 0, or NaN if one of its logits is
-    auto share = [&](float m, float s) { return m > -INFINITY ? s * __expf(m - m2) : s; };
-    const float s2 = share(mx, sum) + share(mo, so);
+    const float mo = __shfl_xor(ms, 32, 64), so = __shfl_xor(sum, 32, 64);
+    const float m2 = __builtin_fmaxf(ms, mo);
+    const float s2 = sum * __expf(ms - m2) + so * __expf(mo - m2);
     if (live && fh == 0) *partial_slot = float2{m2, s2};
     return m2;
 }
