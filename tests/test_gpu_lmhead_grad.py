@@ -380,3 +380,18 @@ def test_fp32_pieces_of_no_probability(words):
     want = torch.where(live, (lse - hit).squeeze(1), 0.0)
     assert ((loss - want).abs() <= 2.0**-50 * 1000 * (16 + d)).all()
     assert (de[lost] == 0).all() and torch.isfinite(de).all()
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows", [12, 384])
+@pytest.mark.parametrize("size", [1.5, 2.0, 2.5, 3.0])
+def test_small_probabilities(dtype, rows, size):
+    """Rows sure of one word, the others' probabilities from about 2^-20 to 2^-45: in fp16 G holds those below 2^-29 as subnormal numbers, and
+    most words' gradient is made of them alone."""
+    d, vocab = 128, 776
+    x, e, target = inputs(dtype, rows, d, vocab, 20, std=0.3)
+    word = torch.arange(rows, device=DEV) % 12 * 3
+    x = (e[word].double() * size).to(act_dtype(dtype))
+    target = torch.where(target >= 0, word, -1).int()
+    scale = 2.0**24
+    check(dtype, x, e, target, scale / rows, call(dtype, x, e, target, scale / rows))
