@@ -347,8 +347,10 @@ int zo_kernel_lmhead_ce_noalloc(const void *x, const void *e_plus, const void *e
  * Gradient of the last module.  The final LayerNorm and the tied LM head are the
  * one module whose exact gradient needs no other module's: these calls give it,
  * for programs that train that module by its gradient and the blocks by Eq. 2, or
- * that hold g against z . grad L.  One copy of the parameters, rows in any number;
- * bare buffers, as above.  Types go with dtype as everywhere: activations (x, y
+ * that hold its own g against z . grad L.  One copy of the parameters, rows in any
+ * number; bare buffers, as above: a model handle neither hands out the residual
+ * stream that these start from nor leaves the last module out of a step, so such a
+ * program makes its forward pass of the calls above.  Types go with dtype as everywhere: activations (x, y
  * and their gradients dx, dy) are 16-bit, or double for ZO_FP32; the residual
  * stream, its gradient, mean, rstd and row losses fp32, or double for ZO_FP32; a
  * parameter's gradient has the parameter's type.  Every sum is taken in fp32 (fp64

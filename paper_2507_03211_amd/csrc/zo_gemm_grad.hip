@@ -189,7 +189,8 @@ using ByRows = Product<true, true>;         // G^T x: contraction over the rows,
 using ByWords = Product<false, true>;       // G e: contraction over the words, outside in e
 
 // dx's shares and de in one launch, where few rows have both in 64 x 64 tiles: dx reads e while de is written.  dx first, and rings of two stages,
-// five workgroups to a CU, for both.  us of the whole call, two launches / one: 20 rows of 768 x 50272 64.1 / 61.0 (rings of three 64.3, of four
+// five workgroups to a CU, for both.  us of the whole call, over and over on the same buffers (20 rows take 69.5 where every call has an
+// e and a de of its own, 61.7 beside that on one pair), two launches / one: 20 rows of 768 x 50272 64.1 / 61.0 (rings of three 64.3, of four
 // 72.4, de first 64.4, the two interleaved 73.7), 20 of 2048 156.5 / 144.1, 64 of 512 x 10000 27.7 / 25.1, 100 of 512 x 20000 39.8 / 35.9,
 // 20 of 5120 x 8192 70.6 / 67.5.  Long contractions want the deeper ring and stay by themselves: by slabs a
 // share, 1 row of 4096 x 32000 (62) 195.0 / 181.3, 33 of 4096 x 20000 (78) 106.0 / 109.6, 64 of 2048 x 50272 (98) 155.7 / 153.2, 1 of 5120 x 128000

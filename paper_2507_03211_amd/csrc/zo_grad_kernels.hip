@@ -282,7 +282,9 @@ bool norm_grad_few(int dtype, int rows, int d) { return rows <= 256 && (d <= 512
 
 // How many workgroups a backward pass over many rows has, each with a share of the weights' gradient: one a CU, and two rows (eight, where
 // wavefronts have rows of their own) for each at least.  The kernel for any length, where a row is a workgroup's whole latency: one row, 1024
-// at most (4096 rows of 2603, 256 / 512 / 1024 workgroups 205 / 143 / 102 us).
+// at most.  us with 256 / 512 / 1024 / 2048 of them, bf16: 1000 rows of 13001 251 / 141 / 83 / 83, 4096 rows of 8193 723 / 438 / 297 / 242, of
+// 13001 1180 / 705 / 523 / 389; fp32 parameters, 4096 rows of 5120 655 / 478 / 344 / 290.  2048 would take twice the scratch, 16 KiB a
+// column, for rows longer than any in use.
 int norm_grad_shares(int dtype, int rows, int d)
 {
     const bool registers = norm_grad_in_registers(dtype, d, d % 4 == 0);
