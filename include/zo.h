@@ -411,6 +411,31 @@ size_t zo_kernel_grad_clip_scratch_bytes(void);
 int zo_kernel_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm,
                         double *norm, void *scratch, void *stream);
 
+/* One AdamW step over n_tensors tensors.  With t = step, for every element:
+ *     g = c grad,   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *     p <- p - (lr weight_decay p + lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)).
+ * Each scalar is worked in fp64 and rounded to fp32 once, each operation between tensors is one fp32 rounding: the same bits every time.
+ *   param, grad, state, numel  host arrays of n_tensors device pointers and counts, read before the call returns; param and grad of dtype's
+ *                    storage type; all 16-byte aligned.  numel 0: skipped.  No tensor's parameters or state overlap anything else
+ *                    (ZO_EINVAL if they do); gradients may lie as they like.
+ *   state            a tensor's moments, zo_kernel_adamw_state_bytes(numel, state_bits) bytes, all zero before step 1: blocks of 256
+ *                    elements (the last one whole, zeros behind the tensor's end).  state_bits 32: a block is 256 fp32 m, then 256 fp32 v.
+ *                    state_bits 8: 256 e4m3 numbers, 256 more and two fp32 scales, 520 bytes: m = number x scale[0], sqrt(v) = number
+ *                    x scale[1], each scale its block's largest magnitude / 448, nearest even; a v above zero is never held as zero.  A
+ *                    moment of three bits behind the first moves once a step changes it by 1/32 to 1/16 of itself beside its block's largest.
+ *                    A block with a new moment that is not finite gets a scale that is not a number.
+ *   step             counts from 1
+ *   norm, max_norm   NULL: c = 1.  Else device: the gradients' global norm (norm[0] of zo_kernel_grad_clip), and c = max_norm / norm[0] where
+ *                    norm[0] > max_norm, else 1: a program that has the norm alone need not have the clipped gradients written; one that
+ *                    has clipped them gives max_norm infinity.  A norm that is not finite: the call writes nothing.
+ *   rounding, seed   ZO_ROUND_NEAREST, or ZO_ROUND_STOCHASTIC for the parameters (16-bit types; see zo_set_update_rounding) with words of
+ *                    stream 3 for (seed, the tensor's place in the list, element): a seed of its own for each call
+ * lr, weight_decay >= 0, beta1 and beta2 in [0, 1), eps > 0. */
+size_t zo_kernel_adamw_state_bytes(uint64_t numel, int state_bits);
+int zo_kernel_adamw(void *const *param, const void *const *grad, void *const *state, const uint64_t *numel, int n_tensors, int dtype,
+                    int state_bits, double lr, double beta1, double beta2, double eps, double weight_decay, uint64_t step,
+                    const double *norm, float max_norm, int rounding, uint64_t seed, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

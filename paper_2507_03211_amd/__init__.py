@@ -28,6 +28,7 @@ EXPORTS = (
     "zo_kernel_lmhead_ce_noalloc",
     "zo_kernel_layernorm", "zo_kernel_layernorm_grad_scratch_bytes", "zo_kernel_layernorm_grad", "zo_kernel_lmhead_grad_scratch_bytes",
     "zo_kernel_lmhead_grad_plan", "zo_kernel_lmhead_grad", "zo_kernel_grad_clip_scratch_bytes", "zo_kernel_grad_clip",
+    "zo_kernel_adamw_state_bytes", "zo_kernel_adamw",
 )
 
 
@@ -102,6 +103,10 @@ def lib():
         L.zo_kernel_grad_clip_scratch_bytes.restype = sz
         L.zo_kernel_grad_clip_scratch_bytes.argtypes = []
         L.zo_kernel_grad_clip.argtypes = [vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        f64 = ctypes.c_double
+        L.zo_kernel_adamw_state_bytes.restype = sz
+        L.zo_kernel_adamw_state_bytes.argtypes = [u64, i32]
+        L.zo_kernel_adamw.argtypes = [vp, vp, vp, vp, i32, i32, i32, f64, f64, f64, f64, f64, u64, vp, f32, i32, u64, vp]
         _lib = L
     return _lib
 
@@ -359,3 +364,18 @@ def zo_kernel_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, norm, scrat
     if min(len(src), len(dst), len(numel)) < n_tensors:
         raise ValueError("n_tensors is %d, the tables hold %d, %d and %d" % (n_tensors, len(src), len(dst), len(numel)))
     _check(lib().zo_kernel_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, _ptr(norm), _ptr(scratch), _stream(stream)))
+
+
+def zo_kernel_adamw_state_bytes(numel, state_bits):
+    return int(lib().zo_kernel_adamw_state_bytes(numel, state_bits))
+
+
+def zo_kernel_adamw(param, grad, state, numel, n_tensors, dtype, state_bits, lr, beta1, beta2, eps, weight_decay, step, norm=None,
+                    max_norm=float("inf"), rounding=ZO_ROUND_NEAREST, seed=0, stream=None):
+    """`param`, `grad`, `state`: lists of tensors or addresses, `numel`: list of counts; or ctypes arrays of them (c_void_p, c_uint64)."""
+    param, grad, state = (_table(t, ctypes.c_void_p) for t in (param, grad, state))
+    numel = _table(numel, ctypes.c_uint64)
+    if min(len(param), len(grad), len(state), len(numel)) < n_tensors:
+        raise ValueError("n_tensors is %d, the tables hold %d, %d, %d and %d" % (n_tensors, len(param), len(grad), len(state), len(numel)))
+    _check(lib().zo_kernel_adamw(param, grad, state, numel, n_tensors, dtype, state_bits, lr, beta1, beta2, eps, weight_decay, step, _ptr(norm),
+                                 max_norm, rounding, seed, _stream(stream)))

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -1493,5 +1494,83 @@ extern "C" int zo_kernel_grad_clip(const void *const *src, void *const *dst, con
     if (bad == -2) return fail(ZO_ENOMEM, "no host memory for %d tensors", n_tensors);
     if (bad >= 0) return fail(ZO_EINVAL, "tensor %d overlaps another tensor's dst", bad);
     ZO_HIP(launch_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, norm, scratch_mem, (hipStream_t)stream));
+    return ZO_OK;
+}
+
+// ------------------------------------------------------------------ AdamW
+// Whether tensors that a call writes overlap each other or ones that it reads: -1 if not, else the number of one that does.  `written` is
+// sorted here.
+namespace {
+struct Range { uintptr_t first, end; int tensor; };
+int ranges_overlap(Range *written, int n, const Range *read, int n_read)
+{
+    auto before = [](const Range &a, const Range &b) { return a.first < b.first; };
+    if (!std::is_sorted(written, written + n, before)) std::sort(written, written + n, before);
+    for (int k = 1; k < n; ++k)
+        if (written[k].first < written[k - 1].end) return written[k].tensor;
+    for (int i = 0; i < n_read; ++i) {
+        // the last one that starts before this one ends
+        const Range *at = std::lower_bound(written, written + n, read[i].end, [](const Range &a, uintptr_t v) { return a.first < v; });
+        if (at != written && at[-1].end > read[i].first) return read[i].tensor;
+    }
+    return -1;
+}
+}  // namespace
+
+extern "C" size_t zo_kernel_adamw_state_bytes(uint64_t numel, int state_bits)
+{
+    if ((state_bits != 8 && state_bits != 32) || numel >= 1ull << 44) return 0;
+    return (numel + kAdamBlock - 1) / kAdamBlock * (state_bits == 8 ? kAdamBlockBytes<8> : kAdamBlockBytes<32>);
+}
+
+extern "C" int zo_kernel_adamw(void *const *param, const void *const *grad, void *const *state, const uint64_t *numel, int n_tensors, int dtype, int state_bits,
+                               double lr, double beta1, double beta2, double eps, double weight_decay, uint64_t step, const double *norm, float max_norm,
+                               int rounding, uint64_t seed, void *stream)
+{
+    ZO_TRY(check_dtype(dtype));
+    if (n_tensors < 0) return fail(ZO_EINVAL, "n_tensors %d is negative", n_tensors);
+    if (n_tensors && (!param || !grad || !state || !numel)) return fail(ZO_EINVAL, "NULL argument");
+    if (state_bits != 8 && state_bits != 32) return fail(ZO_EINVAL, "state_bits %d: 8 or 32", state_bits);
+    if (rounding != ZO_ROUND_NEAREST && rounding != ZO_ROUND_STOCHASTIC) return fail(ZO_EINVAL, "rounding %d unknown", rounding);
+    if (rounding == ZO_ROUND_STOCHASTIC && dtype == ZO_FP32) return fail(ZO_EINVAL, "stochastic rounding is for ZO_BF16 / ZO_FP16 storage");
+    if (!(beta1 >= 0.0 && (float)beta1 < 1.0f) || !(beta2 >= 0.0 && (float)beta2 < 1.0f)) return fail(ZO_EINVAL, "beta1 and beta2 are in [0, 1)");
+    if (!((float)eps > 0.0f && eps <= 3e38)) return fail(ZO_EINVAL, "eps must be positive, as an fp32 number too");
+    if (step < 1) return fail(ZO_EINVAL, "step counts from 1");
+    // 1 - beta^t without the difference of two numbers near one; at beta = 0 the logarithm is minus infinity and this is 1
+    auto corrected = [step](double beta) { return -std::expm1((double)step * std::log(beta)); };
+    const double rate = lr / corrected(beta1);
+    if (!(lr >= 0.0 && rate <= 3e38) || !(weight_decay >= 0.0 && lr * weight_decay <= 3e38)) return fail(ZO_EINVAL, "lr and weight_decay must be finite and not negative");
+    if (norm && !(max_norm > 0.0f)) return fail(ZO_EINVAL, "max_norm must be positive");
+    if ((uintptr_t)norm % 8) return fail(ZO_EINVAL, "norm must be 8-byte aligned");
+    const size_t each = elem_bytes(dtype);
+    Range few[3 * 64 + 1], *r = few;
+    if (n_tensors > 64 && !(r = new (std::nothrow) Range[3 * (size_t)n_tensors + 1])) return fail(ZO_ENOMEM, "no host memory for %d tensors", n_tensors);
+    auto check = [&] {
+        int n = 0, n_read = 0;
+        Range *read = r + 2 * (size_t)n_tensors;
+        for (int i = 0; i < n_tensors; ++i) {
+            if (numel[i] == 0) continue;
+            if (!param[i] || !grad[i] || !state[i]) return fail(ZO_EINVAL, "tensor %d is NULL", i);
+            const uintptr_t p = (uintptr_t)param[i], g = (uintptr_t)grad[i], s = (uintptr_t)state[i];
+            if (p % 16 || g % 16 || s % 16) return fail(ZO_EINVAL, "tensor %d is not 16-byte aligned", i);
+            if ((p | g | s) >> 48) return fail(ZO_EINVAL, "tensor %d: not a device address", i);
+            if (numel[i] >= 1ull << 44) return fail(ZO_EINVAL, "tensor %d has %llu elements", i, (unsigned long long)numel[i]);
+            r[n++] = Range{p, p + numel[i] * each, i};
+            r[n++] = Range{s, s + zo_kernel_adamw_state_bytes(numel[i], state_bits), i};
+            read[n_read++] = Range{g, g + numel[i] * each, i};
+        }
+        if (norm) read[n_read++] = Range{(uintptr_t)norm, (uintptr_t)norm + sizeof(double), n_tensors};
+        const int bad = ranges_overlap(r, n, read, n_read);
+        if (bad == n_tensors) return fail(ZO_EINVAL, "norm overlaps a tensor's parameters or state");
+        return bad >= 0 ? fail(ZO_EINVAL, "tensor %d overlaps another tensor's parameters or state, or its own", bad) : (int)ZO_OK;
+    };
+    const int status = check();
+    if (r != few) delete[] r;
+    ZO_TRY(status);
+    AdamScalars k{};
+    k.b1 = (float)beta1; k.c1 = (float)(1.0 - beta1); k.b2 = (float)beta2; k.c2 = (float)(1.0 - beta2);
+    k.decay = (float)(lr * weight_decay); k.rate = (float)rate; k.root = (float)(1.0 / std::sqrt(corrected(beta2))); k.eps = (float)eps;
+    k.norm = norm; k.max_norm = max_norm; k.seed = seed;
+    ZO_HIP(launch_adamw(param, grad, state, numel, n_tensors, dtype, state_bits, k, rounding == ZO_ROUND_STOCHASTIC, (hipStream_t)stream));
     return ZO_OK;
 }

@@ -144,4 +144,29 @@ static_assert(sizeof(ClipBatch) + 64 <= 4096, "passed by value: a kernel takes 4
 hipError_t launch_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm, double *norm,
                             void *scratch, hipStream_t s);
 
+// ---- AdamW (zo_adamw.hip) ----
+constexpr int kAdamBlock = 256;            // elements of a state's block
+template <int BITS> constexpr size_t kAdamBlockBytes = BITS == 32 ? 2 * 4 * kAdamBlock : 2 * kAdamBlock + 8;
+constexpr uint32_t kAdamChunk = 4096;      // elements per chunk
+constexpr uint32_t kAdamGrid = 2048;       // workgroups of a launch at most
+// Tensors of a launch, 28 bytes each; a few take a shorter table (as in clipping: arguments are copied at each launch)
+constexpr int kAdamMax = 140, kAdamFew = 40;
+template <int N> struct AdamBatchOf {
+    uint64_t param[N];                     // address, 48 bits; above it the elements of the last chunk less one
+    uint64_t grad[N];
+    uint64_t state[N];
+    uint32_t first[N];                     // first chunk
+    int n;
+    uint32_t chunks;
+};
+struct AdamScalars {
+    float b1, c1, b2, c2, decay, rate, root, eps, max_norm;     // c = 1 - b; lr weight_decay; lr / (1 - beta1^t); (1 - beta2^t)^-1/2
+    const double *norm;                    // may be null
+    uint64_t seed;
+    uint32_t first_tensor;                 // number of the table's first tensor
+};
+static_assert(sizeof(AdamBatchOf<kAdamMax>) + sizeof(AdamScalars) + 64 <= 4096, "passed by value: a kernel takes 4 KiB of arguments");
+hipError_t launch_adamw(void *const *param, const void *const *grad, void *const *state, const uint64_t *numel, int n_tensors, int dtype, int bits,
+                        const AdamScalars &k, bool stochastic, hipStream_t s);
+
 }  // namespace zo
