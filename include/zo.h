@@ -411,6 +411,36 @@ size_t zo_kernel_grad_clip_scratch_bytes(void);
 int zo_kernel_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm,
                         double *norm, void *scratch, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Gradient of a decoder block's parts, to carry the last module's on into the blocks in front of it, and the step that makes
+ * weights of gradients.  Conventions, types and scratch as in the part above.  The last feed-forward layer, from the gradient `dres` of the
+ * residual stream that the final LayerNorm's backward pass leaves (fp32): linear_grad of the down-projection (epilogue 2, dy = dres, relu_x), of the
+ * up-projection (epilogue 0, dy = the former's dx), layernorm_grad with accumulate into dres.  The attention's half: linear_grad of the
+ * output projection (epilogue 2, dy = dres), attention_grad, linear_grad of the stacked queries', keys' and values' projection, layernorm_grad.
+ * ---------------------------------------------------------------------- */
+
+/* Backward pass of one sign's zo_kernel_linear_pm, w [n, k] as stored: with G [rows, n] the gradient in front of the epilogue,
+ *     dx = G w,   dw = G^T x,   db = sum_r G.
+ *   epilogue         the forward call's.  0, 2, 3: G = dy; 1: G = dy where y > 0, else 0, whatever dy holds there, with y what the forward call
+ *                    left.  dy is in the activation type for 0 and 1, fp32 (fp64 for ZO_FP32) for 2 and 3; the residual stream's own
+ *                    gradient is dy, untouched.  3 has no db.
+ *   relu_x           non-zero: x is itself what a ReLU left (epilogue 1 of the layer before), and dx is the gradient in front of it: 0
+ *                    where x is not above 0.  That layer's call then takes dx with epilogue 0 and saves a pass over its dy and y.
+ *   dx, dw, db       any of them may be NULL, not all.  Outputs overlap neither the inputs nor each other (ZO_EINVAL if they do); x (without dw
+ *                    and relu_x) and w (without dx) may be NULL.
+ * 2-byte dtypes: n and k multiples of 8, buffers 16-byte aligned (ZO_EINVAL otherwise); an fp32 dy is rounded to the type for the products,
+ * once an element, and summed for db as it is; ZO_FP16 gradients want a scale that keeps them in range.  Up to 2^20 rows, n and k up to 2^22;
+ * nor does a call take products of more tiles than a launch holds (ZO_EINVAL, and 0 scratch bytes): with few slabs of 64 in the sum, results of
+ * about 2^36 elements, ZO_FP32 2^34. */
+size_t zo_kernel_linear_grad_scratch_bytes(int dtype, int rows, int n, int k, int epilogue);
+int zo_kernel_linear_grad(const void *x, const void *w, const void *y, const void *dy, void *dx, void *dw, void *db, void *scratch,
+                          int dtype, int rows, int n, int k, int epilogue, int relu_x, void *stream);
+
+/* How such a call of 2-byte types works on the current device (on 256 compute units where there is none): plan[0], plan[1] the output tiles
+ * of dx and dw (rows << 16 | columns), plan[2], plan[3] the shares their sums are cut into, plan[4] the columns of the copy it makes of
+ * G (0: none), plan[5] the shares of db's sums.  plan holds 6 numbers.  Host only. */
+int zo_kernel_linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan);
+
 /* One AdamW step over n_tensors tensors.  With t = step, for every element:
  *     g = c grad,   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
  *     p <- p - (lr weight_decay p + lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)).

@@ -28,6 +28,7 @@ EXPORTS = (
     "zo_kernel_lmhead_ce_noalloc",
     "zo_kernel_layernorm", "zo_kernel_layernorm_grad_scratch_bytes", "zo_kernel_layernorm_grad", "zo_kernel_lmhead_grad_scratch_bytes",
     "zo_kernel_lmhead_grad_plan", "zo_kernel_lmhead_grad", "zo_kernel_grad_clip_scratch_bytes", "zo_kernel_grad_clip",
+    "zo_kernel_linear_grad_scratch_bytes", "zo_kernel_linear_grad_plan", "zo_kernel_linear_grad",
     "zo_kernel_adamw_state_bytes", "zo_kernel_adamw",
 )
 
@@ -103,6 +104,10 @@ def lib():
         L.zo_kernel_grad_clip_scratch_bytes.restype = sz
         L.zo_kernel_grad_clip_scratch_bytes.argtypes = []
         L.zo_kernel_grad_clip.argtypes = [vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        L.zo_kernel_linear_grad_scratch_bytes.restype = sz
+        L.zo_kernel_linear_grad_scratch_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.zo_kernel_linear_grad_plan.argtypes = [i32, i32, i32, i32, vp]
+        L.zo_kernel_linear_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
         f64 = ctypes.c_double
         L.zo_kernel_adamw_state_bytes.restype = sz
         L.zo_kernel_adamw_state_bytes.argtypes = [u64, i32]
@@ -364,6 +369,23 @@ def zo_kernel_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, norm, scrat
     if min(len(src), len(dst), len(numel)) < n_tensors:
         raise ValueError("n_tensors is %d, the tables hold %d, %d and %d" % (n_tensors, len(src), len(dst), len(numel)))
     _check(lib().zo_kernel_grad_clip(src, dst, numel, n_tensors, dtype, max_norm, _ptr(norm), _ptr(scratch), _stream(stream)))
+
+
+def zo_kernel_linear_grad_scratch_bytes(dtype, rows, n, k, epilogue):
+    return int(lib().zo_kernel_linear_grad_scratch_bytes(dtype, rows, n, k, epilogue))
+
+
+def zo_kernel_linear_grad_plan(rows, n, k, epilogue):
+    """Of 2-byte types: {"dx", "dw": (rows, columns) of the output tiles, "dx_shares", "dw_shares", "copy_columns", "db_shares"}."""
+    plan = (ctypes.c_int32 * 6)()
+    _check(lib().zo_kernel_linear_grad_plan(rows, n, k, epilogue, plan))
+    return dict(dx=(plan[0] >> 16, plan[0] & 0xffff), dw=(plan[1] >> 16, plan[1] & 0xffff), dx_shares=plan[2], dw_shares=plan[3], copy_columns=plan[4],
+                db_shares=plan[5])
+
+
+def zo_kernel_linear_grad(x, w, y, dy, dx, dw, db, scratch, dtype, rows, n, k, epilogue, relu_x=False, stream=None):
+    _check(lib().zo_kernel_linear_grad(_ptr(x), _ptr(w), _ptr(y), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(db), _ptr(scratch), dtype, rows, n, k, epilogue,
+                                       int(relu_x), _stream(stream)))
 
 
 def zo_kernel_adamw_state_bytes(numel, state_bits):

@@ -1497,6 +1497,56 @@ extern "C" int zo_kernel_grad_clip(const void *const *src, void *const *dst, con
     return ZO_OK;
 }
 
+// ------------------------------------------------------------------ gradient of a decoder block's parts
+static bool linear_grad_shape(int dtype, int rows, int n, int k, int epilogue)
+{
+    return rows >= 1 && rows <= kMaxGradRows && n >= 1 && n <= kMaxGradColumns && k >= 1 && k <= kMaxGradColumns && epilogue >= 0 && epilogue <= 3 &&
+           (dtype == ZO_FP32 || (n % 8 == 0 && k % 8 == 0));
+}
+
+static int linear_grad_too_large(int rows, int n, int k)
+{
+    return fail(ZO_EINVAL, "%d rows, n %d, k %d: a product has more tiles than one launch holds", rows, n, k);
+}
+
+extern "C" size_t zo_kernel_linear_grad_scratch_bytes(int dtype, int rows, int n, int k, int epilogue)
+{
+    return dtype < 0 || dtype > 2 || !linear_grad_shape(dtype, rows, n, k, epilogue) ? 0 : linear_grad_scratch(dtype, rows, n, k, epilogue);
+}
+
+extern "C" int zo_kernel_linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan)
+{
+    if (!plan) return fail(ZO_EINVAL, "plan is NULL");
+    if (!linear_grad_shape(ZO_BF16, rows, n, k, epilogue)) return fail(ZO_EINVAL, "bad shape: %d rows, n %d, k %d, epilogue %d", rows, n, k, epilogue);
+    return linear_grad_plan(rows, n, k, epilogue, plan) ? (int)ZO_OK : linear_grad_too_large(rows, n, k);
+}
+
+extern "C" int zo_kernel_linear_grad(const void *x, const void *w, const void *y, const void *dy, void *dx, void *dw, void *db, void *scratch_mem, int dtype,
+                                     int rows, int n, int k, int epilogue, int relu_x, void *stream)
+{
+    ZO_TRY(check_dtype(dtype));
+    if (epilogue < 0 || epilogue > 3) return fail(ZO_EINVAL, "epilogue %d unknown", epilogue);
+    if (!linear_grad_shape(dtype, rows, n, k, epilogue))
+        return fail(ZO_EINVAL, "bad shape: %d rows, n %d, k %d (up to 2^20, 2^22, 2^22; 2-byte types: n and k multiples of 8)", rows, n, k);
+    if (!dx && !dw && !db) return fail(ZO_EINVAL, "no output asked for");
+    if (!dy || !scratch_mem || (dx && !w) || ((dw || (dx && relu_x)) && !x) || (epilogue == 1 && !y)) return fail(ZO_EINVAL, "NULL argument");
+    if (db && epilogue == 3) return fail(ZO_EINVAL, "epilogue 3 has no bias: db must be NULL");
+    const void *out_of_relu = epilogue == 1 ? y : nullptr;
+    if (dtype != ZO_FP32 && ((uintptr_t)x % 16 || (uintptr_t)w % 16 || (uintptr_t)out_of_relu % 16 || (uintptr_t)dy % 16 || (uintptr_t)dx % 16 ||
+                             (uintptr_t)dw % 16 || (uintptr_t)db % 16))
+        return fail(ZO_EINVAL, "buffers must be 16-byte aligned");
+    if ((uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");
+    const size_t n_x = (size_t)rows * k * act_bytes(dtype), n_w = (size_t)n * k * elem_bytes(dtype), n_y = (size_t)rows * n;
+    const Buffer buffers[] = {{"dx", dx, n_x}, {"dw", dw, n_w}, {"db", db, n * elem_bytes(dtype)}, {"x", dw || (dx && relu_x) ? x : nullptr, n_x},
+                              {"w", dx ? w : nullptr, n_w}, {"y", out_of_relu, n_y * act_bytes(dtype)},
+                              {"dy", dy, n_y * (epilogue >= 2 ? resid_bytes(dtype) : act_bytes(dtype))}};
+    ZO_TRY(check_apart(buffers, 3));
+    const hipError_t err = launch_linear_grad(x, w, y, dy, dx, dw, db, scratch_mem, dtype, rows, n, k, epilogue, relu_x != 0, (hipStream_t)stream);
+    if (err == hipErrorNotSupported) return linear_grad_too_large(rows, n, k);
+    ZO_HIP(err);
+    return ZO_OK;
+}
+
 // ------------------------------------------------------------------ AdamW
 // Whether tensors that a call writes overlap each other or ones that it reads: -1 if not, else the number of one that does.  `written` is
 // sorted here.

@@ -44,6 +44,7 @@ template <bool XK, bool WK> struct Product {
         uint64_t ldx, ldw, xz, wz, x_end, w_end;
         int w_row;
         float alpha;                        // epilogue 6: factor of the result
+        const uint16_t *keep;               // 10: a matrix laid out as the result
         // epilogues 5 and 9
         const float2 *stats;                // 5: per row, logsumexp (rounded; infinity in rows that do not count) and what goes on top of the exponent
         float2 *pairs;                      // 9: per row and strip
@@ -53,6 +54,14 @@ template <bool XK, bool WK> struct Product {
     };
 };
 constexpr int kMaxColumns = 1 << 24;        // 16 fp32 rows within 2^30 bytes: what an epilogue pass addresses with 32 bits
+
+// Of the two 16-bit numbers in v, those whose fellows in k are above zero; zeros for the others.
+template <int DT> __device__ __forceinline__ uint32_t above_zero(uint32_t k, uint32_t v)
+{
+    constexpr uint32_t kInf = DT == kBF16 ? 0x7f80u : 0x7c00u;          // 1 .. kInf: the numbers above zero
+    const uint32_t lo = ((k - 1u) & 0xffffu) < kInf ? 0xffffu : 0u, hi = ((k >> 16) - 1u) < kInf ? 0xffff0000u : 0u;
+    return v & (lo | hi);
+}
 
 template <int DT> __device__ __forceinline__ f32x16 mfma32(const uint4 &a, const uint4 &b, const f32x16 &c)
 {
@@ -254,10 +263,10 @@ __device__ __forceinline__ void gradient_row(f32x16 (&a)[TN], float2 st, int rel
     }
 }
 
-// Epilogues 0 - 3 and 5 - 9 of a wave's 32 TM x 32 TN outputs (rows m0 + wm 32 TM .., columns n0 + wn 32 TN .. of sign `sign`).
+// Epilogues 0 - 3 and 5 - 10 of a wave's 32 TM x 32 TN outputs (rows m0 + wm 32 TM .., columns n0 + wn 32 TN .. of sign `sign`).
 // 9: epilogue 4's pairs, and every logit as its distance from the pair's maximum in steps of 32 / 65535 (a distance of 32
 // and more counts as none: e^-32 of the strip's largest; half a step is 2^-12 of a probability, half of fp16's own half step).
-// 5: 16-bit, the values as they are; 6: 16-bit, times alpha; 7: fp32; 8: added to fp32 sums; all without bias.
+// 5: 16-bit, the values as they are; 6: 16-bit, times alpha; 7: fp32; 8: added to fp32 sums; 10: 16-bit, zeros where `keep` is not above zero; all without bias.
 // `stage`: kTileStageBytes<TN> bytes of LDS that are this wave's alone.  NT: non-temporal accesses (see launch_small).
 template <int TN> constexpr int kTileStageBytes = (TN & (TN - 1)) ? 2048 * TN + 512 : 2048 * TN;
 template <int DT, int EPI, int TM, int TN, bool NT, class ARG = Plain::Arg>
@@ -271,7 +280,7 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
     // length is a power of two are XOR-swizzled by the row: the run-wise writes and the row-wise 16-byte reads are free of
     // bank conflicts (16-bit rows of one tile apart, see chunk16 below).  Others have 16 bytes of padding, which leaves two
     // lanes per bank in the writes (15 % of the LDS cycles of a 12-slab launch of 256 x 192 tiles).
-    constexpr bool kOut16 = (EPI == 0 || EPI == 1 || EPI == 5 || EPI == 6 || EPI == 9);              // 2-byte outputs; else fp32
+    constexpr bool kOut16 = (EPI == 0 || EPI == 1 || EPI == 5 || EPI == 6 || EPI == 9 || EPI == 10);              // 2-byte outputs; else fp32
     constexpr bool kAdd = EPI == 2 || EPI == 8, kBias = EPI < 3;
     constexpr int RP = kOut16 ? 32 : 16;                         // rows per pass
     constexpr int NPASS = 32 * TM / RP;
@@ -358,6 +367,20 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
 #pragma unroll
         for (int i = 0; i < NIO; ++i) h[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, offset(i), 0, kPolicy));
     };
+    // epilogue 10: what the result's elements are kept by, read one pass ahead likewise
+    constexpr bool kKeep = EPI == 10;
+    u32x4 keep[2][kKeep ? NIO : 1];
+    auto load_keep = [&](int pass, u32x4 (&h)[kKeep ? NIO : 1]) {
+        if constexpr (kKeep) {
+            const int left = m_half - row0 - pass * RP, rows = left < RP ? left : RP;
+            const uint32_t bytes = left > 0 && ncol0 < n ? ((uint32_t)(rows - 1) * (uint32_t)n + (uint32_t)(n - ncol0)) * ES : 0u;
+            const uint64_t first = uniform64((uint64_t)(uintptr_t)op.keep + (((uint64_t)sign * m_half + row0 + pass * RP) * n + ncol0) * ES);
+            const auto from = __builtin_amdgcn_make_buffer_rsrc((void *)(uintptr_t)first, 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+#pragma unroll
+            for (int i = 0; i < NIO; ++i) h[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, offset(i), 0, 0));
+        }
+    };
+    load_keep(0, keep[0]);
     float bias4[EPI == 2 ? NBV : 1][4] = {};
     if constexpr (kAdd) load_res(0, hres[0]);
     if constexpr (EPI == 2) {
@@ -422,6 +445,9 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
         if constexpr (kAdd) {
             if (pass + 1 < NPASS) load_res(pass + 1, hres[(pass + 1) & 1]);
         }
+        if constexpr (kKeep) {
+            if (pass + 1 < NPASS) load_keep(pass + 1, keep[(pass + 1) & 1]);
+        }
         // fp32: the pass covers rows 16 (pass % 2) .. + 15 of the block, held by the lanes with that fr / 16
         if (kOut16 || (fr >> 4) == (pass & 1)) {
 #pragma unroll
@@ -460,6 +486,10 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[TN][TM], char *st
                 const int r = (64 * i + lane) / LPR, c = (64 * i + lane) % LPR;
                 u32x4 q = *(const u32x4 *)(stage + r * PITCH + ((kXor ? c ^ chunk16(r) : c) << 4));
                 if (kXor && ((i * 64 / LPR) >> kFlip & 1)) q = u32x4{q.z, q.w, q.x, q.y};
+                if constexpr (kKeep) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q[e] = above_zero<DT>(keep[pass & 1][i][e], q[e]);
+                }
                 if (valid(pass, i)) {
                     if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(f32x4, q), piece(at_store, i));
                     else *piece(at_store, i) = __builtin_bit_cast(f32x4, q);

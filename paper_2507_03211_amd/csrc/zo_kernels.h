@@ -144,6 +144,14 @@ static_assert(sizeof(ClipBatch) + 64 <= 4096, "passed by value: a kernel takes 4
 hipError_t launch_grad_clip(const void *const *src, void *const *dst, const uint64_t *numel, int n_tensors, int dtype, float max_norm, double *norm,
                             void *scratch, hipStream_t s);
 
+// ---- gradient of the linear layers (zo_linear_grad.hip) ----
+// `y`, with epilogue 1 alone, is what the forward call left; any of dx, dw and db may be null.  0 bytes, hipErrorNotSupported (before anything
+// is launched) and no plan where a product has more tiles than a launch holds
+size_t linear_grad_scratch(int dtype, int rows, int n, int k, int epilogue);
+bool linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan);      // 16-bit types; see zo_kernel_linear_grad_plan
+hipError_t launch_linear_grad(const void *x, const void *w, const void *y, const void *dy, void *dx, void *dw, void *db, void *scratch, int dtype, int rows,
+                              int n, int k, int epilogue, bool relu_x, hipStream_t s);
+
 // ---- AdamW (zo_adamw.hip) ----
 constexpr int kAdamBlock = 256;            // elements of a state's block
 template <int BITS> constexpr size_t kAdamBlockBytes = BITS == 32 ? 2 * 4 * kAdamBlock : 2 * kAdamBlock + 8;

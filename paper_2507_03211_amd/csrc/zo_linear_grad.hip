@@ -1,0 +1,383 @@
+// Backward pass of the linear layer y = x W^T + b with the forward call's epilogues: G = dy, or dy [y > 0] behind a ReLU,
+//
+//   dx = G W   (times [x > 0] where x is a ReLU's output),   dW = G^T x,   db = sum_r G
+//
+// 16-bit types: two products of 2 rows n k flop on the tiles of zo_gemm_tiles.hip.h, every operand as it lies (the contraction over G's
+// columns has W with k outside, the one over the rows both).  Where there are few tiles a product's contraction is cut into shares whose
+// fp32 sums a last launch adds up.  G is dy itself where that is 16-bit and its rows are whole slabs, else a copy made on the way of the pass
+// that sums its columns: an fp32 dy is rounded to 16 bits there, because that is what the matrix instructions take (half a step an
+// element; db sums the fp32 numbers).  fp32 parameters: everything in fp64, one launch.
+#include "zo_gemm_products.hip.h"
+
+namespace zo {
+
+namespace {
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------------ the pass over dy
+// G's rows and the sums of its columns, eight columns a lane, a wavefront's 512 to a row; the workgroup's four take every fourth row of the
+// workgroup's share.  WIDE: dy is fp32.  g [rows, width] may be null (dy is G already); so may db and part.  One share: db at once; more:
+// part[share][n].
+template <int DT, bool WIDE, bool RELU>
+__global__ __launch_bounds__(256) void grad_rows_kernel(const void *__restrict__ dy, const uint16_t *__restrict__ y, uint4 *__restrict__ g,
+                                                        float *__restrict__ part, uint16_t *__restrict__ db, int rows, int n, int width, int each)
+{
+    constexpr int AHEAD = 4;
+    __shared__ float sums[4][64][8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = (int)blockIdx.x * 512 + 8 * lane;
+    const int first = (int)blockIdx.y * each, last = first + each < rows ? first + each : rows;
+    const bool live = c < n;
+    float sum[8] = {};
+    for (int r0 = first + wave; r0 < last; r0 += 4 * AHEAD) {
+        float4 wide[AHEAD][2];
+        uint4 in[AHEAD], kept[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int r = r0 + 4 * i;
+            const bool on = live && r < last;
+            const size_t at = (size_t)(on ? r : first) * n + (live ? c : 0);
+            if constexpr (WIDE) {
+                const float4 *p = (const float4 *)((const float *)dy + at);
+                wide[i][0] = on ? p[0] : float4{0, 0, 0, 0};
+                wide[i][1] = on ? p[1] : float4{0, 0, 0, 0};
+            } else {
+                in[i] = on ? *(const uint4 *)((const uint16_t *)dy + at) : uint4{0, 0, 0, 0};
+            }
+            if constexpr (RELU) kept[i] = on ? *(const uint4 *)(y + at) : uint4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int r = r0 + 4 * i;
+            if (r >= last) break;
+            uint32_t out[4];
+            float v[8];
+            if constexpr (WIDE) {
+                const float w[8] = {wide[i][0].x, wide[i][0].y, wide[i][0].z, wide[i][0].w, wide[i][1].x, wide[i][1].y, wide[i][1].z, wide[i][1].w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = w[e];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = pack2<DT>(w[2 * e], w[2 * e + 1]);
+            } else {
+                const uint32_t w[4] = {in[i].x, in[i].y, in[i].z, in[i].w}, k[4] = {kept[i].x, kept[i].y, kept[i].z, kept[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    out[e] = RELU ? above_zero<DT>(k[e], w[e]) : w[e];
+                    v[2 * e] = Prec<DT>::a2acc((uint16_t)(out[e] & 0xffff));
+                    v[2 * e + 1] = Prec<DT>::a2acc((uint16_t)(out[e] >> 16));
+                }
+            }
+            if (g && c < width) g[((size_t)r * width + c) / 8] = uint4{out[0], out[1], out[2], out[3]};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += v[e];
+        }
+    }
+    if (!db && !part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[wave][lane][e] = sum[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 512; i += 256) {
+        const int col = (int)blockIdx.x * 512 + i;
+        if (col >= n) continue;
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) s += sums[w][i / 8][i % 8];
+        if (part) part[(size_t)blockIdx.y * n + col] = s;
+        else db[col] = Prec<DT>::acc2a(s);
+    }
+}
+
+// ------------------------------------------------------------------ sums of shares
+// out = rn(sum_z part[z]), eight elements a thread, zeros where `keep` is not above zero (if there is one); the workgroup's `groups` groups of
+// threads take every groups-th share each and their sums meet in LDS.  Up to three results a launch.
+struct SharesJob { const float4 *part; uint4 *out; const uint4 *keep; size_t n8; int shares, groups, blocks; };
+struct SharesJobs { SharesJob job[3]; };
+template <int DT>
+__global__ __launch_bounds__(256) void shares_sum_kernel(SharesJobs jobs)
+{
+    __shared__ float4 sums[256][2];
+    int block = (int)blockIdx.x, j = 0;
+    while (j < 2 && block >= jobs.job[j].blocks) block -= jobs.job[j++].blocks;
+    const SharesJob job = jobs.job[j];
+    const int per = 256 / job.groups, group = threadIdx.x / per, t = threadIdx.x % per;
+    for (size_t i0 = (size_t)block * per; i0 < job.n8; i0 += (size_t)job.blocks * per) {
+        const size_t i = i0 + t < job.n8 ? i0 + t : job.n8 - 1;
+        float4 a{0, 0, 0, 0}, b{0, 0, 0, 0};
+        auto add = [&](const float4 &p, const float4 &q) {
+            a = float4{a.x + p.x, a.y + p.y, a.z + p.z, a.w + p.w};
+            b = float4{b.x + q.x, b.y + q.y, b.z + q.z, b.w + q.w};
+        };
+#pragma unroll 4
+        for (int z = group; z < job.shares; z += job.groups) add(job.part[2 * (z * job.n8 + i)], job.part[2 * (z * job.n8 + i) + 1]);
+        if (job.groups > 1) {
+            __syncthreads();
+            sums[threadIdx.x][0] = a;
+            sums[threadIdx.x][1] = b;
+            __syncthreads();
+            if (group == 0)
+                for (int g = 1; g < job.groups; ++g) add(sums[g * per + t][0], sums[g * per + t][1]);
+        }
+        if (group != 0 || i0 + t >= job.n8) continue;
+        uint4 o{pack2<DT>(a.x, a.y), pack2<DT>(a.z, a.w), pack2<DT>(b.x, b.y), pack2<DT>(b.z, b.w)};
+        if (job.keep) {
+            const uint4 k = job.keep[i];
+            o = uint4{above_zero<DT>(k.x, o.x), above_zero<DT>(k.y, o.y), above_zero<DT>(k.z, o.z), above_zero<DT>(k.w, o.w)};
+        }
+        job.out[i] = o;
+    }
+}
+
+// ------------------------------------------------------------------ the plan of a call
+struct LinearPlan {
+    int width;                              // of G's copy; 0: dy is G
+    int x_shares, x_share;                  // shares of dx's contraction over n, and the columns of one
+    int w_shares, w_share;                  // of dW's over the rows
+    int sum_shares, sum_each;               // of the column sums, and the rows of one
+    Tile x_tile, w_tile;
+    bool both, fits;                        // one launch for both products; every launch's tiles fit one
+    size_t g, x_part, w_part, sums, total;
+};
+LinearPlan linear_plan(int rows, int n, int k, int epilogue)
+{
+    LinearPlan p{};
+    const bool copy = epilogue != 0 || n % BK != 0;
+    const int n_slabs = (n + BK - 1) / BK, r_slabs = (rows + BK - 1) / BK;
+    float best = 0.0f;
+    for (int z = 1; z <= 64 && z <= n_slabs; z += z < 8 ? 1 : z < 16 ? 2 : 4) {
+        if (!copy && n_slabs % z) continue;                      // (a share's slabs past dy's rows would be the next rows')
+        float us;
+        const Tile t = pick_product(kByWords, z, rows, k, (n_slabs + z - 1) / z, &us);
+        if (z > 1) us += shares_us(z, rows, k);
+        if (best == 0.0f || us < best) { best = us; p.x_shares = z; p.x_tile = t; }
+    }
+    p.x_share = (n_slabs + p.x_shares - 1) / p.x_shares * BK;
+    p.width = copy ? p.x_share * p.x_shares : 0;
+    best = 0.0f;
+    for (int z = 1; z <= 64 && z <= r_slabs; z += z < 8 ? 1 : z < 16 ? 2 : 4) {
+        float us;
+        const Tile t = pick_product(kByRows, z, n, k, (r_slabs + z - 1) / z, &us);
+        if (z > 1) us += shares_us(z, n, k);
+        if (best == 0.0f || us < best) { best = us; p.w_shares = z; p.w_tile = t; }
+    }
+    p.w_share = (r_slabs + p.w_shares - 1) / p.w_shares * BK;
+    p.both = p.x_tile == T64x64 && p.w_tile == T64x64 && p.x_shares > 1 && p.w_shares == 1 && p.x_share <= kBothSlabs * BK && r_slabs * BK <= kBothRows;
+    const int64_t dx = small_blocks(p.x_tile, p.x_shares, rows, k), dw = small_blocks(p.w_tile, p.w_shares, n, k);
+    p.fits = dx <= kMostBlocks && dw <= kMostBlocks && (!p.both || dx + dw <= kMostBlocks);
+    const int columns = ((copy ? p.width : n) + 511) / 512, most = 2048 / columns > 1 ? 2048 / columns : 1;
+    p.sum_shares = rows <= 64 ? 1 : (rows + 15) / 16 < most ? (rows + 15) / 16 : most;
+    p.sum_each = ((rows + p.sum_shares - 1) / p.sum_shares + 3) / 4 * 4;
+    p.sum_shares = (rows + p.sum_each - 1) / p.sum_each;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o = up(o + bytes); return at; };
+    p.g = take(2 * (size_t)rows * p.width);
+    p.x_part = take(p.x_shares > 1 ? 4 * (size_t)p.x_shares * rows * k : 0);
+    p.w_part = take(p.w_shares > 1 ? 4 * (size_t)p.w_shares * n * k : 0);
+    p.sums = take(p.sum_shares > 1 ? 4 * (size_t)p.sum_shares * n : 0);
+    p.total = o > 256 ? o : 256;
+    return p;
+}
+
+template <int DT>
+hipError_t linear_grad(const uint16_t *x, const uint16_t *w, const uint16_t *y, const void *dy, uint16_t *dx, uint16_t *dw, uint16_t *db, char *ws, int rows,
+                       int n, int k, int epilogue, bool relu_x, hipStream_t s)
+{
+    const LinearPlan p = linear_plan(rows, n, k, epilogue);
+    if (!p.fits) return hipErrorNotSupported;
+    hipError_t err = hipSuccess;
+    const bool copy = p.width != 0 && (dx || dw);
+    float *sums = db && p.sum_shares > 1 ? (float *)(ws + p.sums) : nullptr;
+    if (copy || db) {
+        auto kern = epilogue >= 2 ? grad_rows_kernel<DT, true, false> : epilogue == 1 ? grad_rows_kernel<DT, false, true> : grad_rows_kernel<DT, false, false>;
+        const int width = copy ? p.width : n;
+        kern<<<dim3((width + 511) / 512, p.sum_shares), dim3(256), 0, s>>>(dy, y, copy ? (uint4 *)(ws + p.g) : nullptr, sums, sums ? nullptr : db, rows, n,
+                                                                           width, p.sum_each);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
+    const uint16_t *g = copy ? (const uint16_t *)(ws + p.g) : (const uint16_t *)dy;
+    const int ldg = copy ? p.width : n;
+    ByWords::Arg op_x{};
+    op_x.ldx = ldg; op_x.ldw = k;
+    op_x.xz = p.x_share; op_x.wz = (uint64_t)p.x_share * k;
+    op_x.w_end = (uint64_t)(uintptr_t)(w + (size_t)n * k);
+    op_x.alpha = 1.0f;
+    op_x.keep = x;
+    const Args a{g, w, nullptr, nullptr, nullptr, p.x_shares > 1 ? (void *)(ws + p.x_part) : dx, p.x_shares, rows, k, p.x_share, s};
+    ByRows::Arg op_w{};
+    op_w.ldx = ldg; op_w.ldw = k;
+    op_w.xz = (uint64_t)p.w_share * ldg; op_w.wz = (uint64_t)p.w_share * k;
+    op_w.x_end = (uint64_t)(uintptr_t)(g + (size_t)rows * ldg);
+    op_w.w_end = (uint64_t)(uintptr_t)(x + (size_t)rows * k);
+    op_w.alpha = 1.0f;
+    const Args b{g, x, nullptr, nullptr, nullptr, p.w_shares > 1 ? (void *)(ws + p.w_part) : dw, p.w_shares, n, k, p.w_share, s};
+    if (dx && dw && p.both) {
+        if ((err = launch_both<DT>(a, op_x, b, op_w)) != hipSuccess) return err;
+    } else {
+        if (dx) {
+            err = p.x_shares > 1 ? launch_product<DT, 7, ByWords>(p.x_tile, a, op_x) : relu_x ? launch_product<DT, 10, ByWords>(p.x_tile, a, op_x)
+                                                                                             : launch_product<DT, 6, ByWords>(p.x_tile, a, op_x);
+            if (err != hipSuccess) return err;
+        }
+        if (dw) {
+            err = p.w_shares > 1 ? launch_product<DT, 7, ByRows>(p.w_tile, b, op_w) : launch_product<DT, 6, ByRows>(p.w_tile, b, op_w);
+            if (err != hipSuccess) return err;
+        }
+    }
+    SharesJobs jobs{};
+    int count = 0, blocks = 0;
+    auto add = [&](const void *part, int shares, size_t elements, uint16_t *out, const uint16_t *keep) {
+        SharesJob &j = jobs.job[count++];
+        j.part = (const float4 *)part; j.out = (uint4 *)out; j.keep = (const uint4 *)keep;
+        j.n8 = elements / 8;
+        j.shares = shares;
+        // groups of threads: enough for every CU to have a workgroup, as long as each has two shares
+        j.groups = 1;
+        while (j.groups < 32 && 4 * j.groups <= shares && j.n8 * j.groups < 256 * 512) j.groups *= 2;
+        const size_t need = (j.n8 * j.groups + 255) / 256;
+        j.blocks = (int)(need < 4096 ? need : 4096);
+        blocks += j.blocks;
+    };
+    if (dx && p.x_shares > 1) add(ws + p.x_part, p.x_shares, (size_t)rows * k, dx, relu_x ? x : nullptr);
+    if (dw && p.w_shares > 1) add(ws + p.w_part, p.w_shares, (size_t)n * k, dw, nullptr);
+    if (sums) add(sums, p.sum_shares, n, db, nullptr);
+    if (!blocks) return hipSuccess;
+    shares_sum_kernel<DT><<<dim3(blocks), dim3(256), 0, s>>>(jobs);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ fp64
+// All three results in one launch: the first x_tiles workgroups have tiles of dx, the next w_tiles of dW, the others 64 columns of db each.  A
+// workgroup owns 16 TB x 16 TB outputs, its W wavefronts take every W-th 16-deep piece of the contraction straight from memory into
+// v_mfma_f64_16x16x4 operands, and the partial sums meet in LDS, in a fixed order.
+template <int TB, int W>
+__global__ __launch_bounds__(64 * W) void linear_grad_f64_kernel(const double *__restrict__ x, const float *__restrict__ w, const double *__restrict__ y,
+                                                                 const double *__restrict__ dy, double *__restrict__ dx, float *__restrict__ dw, float *__restrict__ db,
+                                                                 int rows, int n, int k, bool relu_x, int x_tiles, int w_tiles)
+{
+    constexpr int BT = 16 * TB;
+    __shared__ double part[W][BT][BT + 1];
+    const int block = (int)blockIdx.x;
+    auto grad = [&](int r, int c) {
+        const size_t at = (size_t)r * n + c;
+        return y && !(y[at] > 0.0) ? 0.0 : dy[at];
+    };
+    if (block >= x_tiles + w_tiles) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (block - x_tiles - w_tiles) * 64 + lane;
+        double s = 0.0;
+        if (c < n)
+            for (int r = wave; r < rows; r += W) s += grad(r, c);
+        double *sums = &part[0][0][0];
+        sums[threadIdx.x] = s;
+        __syncthreads();
+        if (wave == 0 && c < n) {
+#pragma unroll
+            for (int v = 1; v < W; ++v) s += sums[64 * v + lane];
+            db[c] = (float)s;
+        }
+        return;
+    }
+    const bool of_x = block < x_tiles;
+    const int tile = of_x ? block : block - x_tiles;
+    const int tiles_k = (k + BT - 1) / BT, i0 = tile / tiles_k * BT, j0 = tile % tiles_k * BT;
+    const int m = of_x ? rows : n, depth = of_x ? n : rows;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+    f64x4 acc[TB][TB] = {};
+#pragma unroll 2
+    for (int k0 = 16 * wave; k0 < depth; k0 += 16 * W) {
+        f64x4 av[TB], bv[TB];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int kk = k0 + 4 * g + q, kc = kk < depth ? kk : depth - 1;
+#pragma unroll
+            for (int t = 0; t < TB; ++t) {
+                const int i = i0 + 16 * t + r16 < m ? i0 + 16 * t + r16 : m - 1, j = j0 + 16 * t + r16 < k ? j0 + 16 * t + r16 : k - 1;   // clamped: never stored
+                const double a = of_x ? grad(i, kc) : grad(kc, i);
+                const double b = of_x ? (double)w[(size_t)kc * k + j] : x[(size_t)kc * k + j];
+                av[t][q] = kk < depth ? a : 0.0;
+                bv[t][q] = kk < depth ? b : 0.0;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < TB; ++i)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f64_16x16x4f64(av[i][q], bv[j][q], acc[i][j], 0, 0, 0);
+    }
+    // element e of a lane's result: row 4 e + lane / 16, column lane % 16 of the 16 x 16 block
+#pragma unroll
+    for (int i = 0; i < TB; ++i)
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) part[wave][16 * i + 4 * q + g][16 * j + r16] = acc[i][j][q];
+    __syncthreads();
+    for (int o = threadIdx.x; o < BT * BT; o += 64 * W) {
+        const int i = i0 + o / BT, j = j0 + o % BT;
+        if (i >= m || j >= k) continue;
+        double v = 0.0;
+#pragma unroll
+        for (int z = 0; z < W; ++z) v += part[z][o / BT][o % BT];
+        const size_t at = (size_t)i * k + j;
+        if (of_x) dx[at] = relu_x && !(x[at] > 0.0) ? 0.0 : v;
+        else dw[at] = (float)v;
+    }
+}
+
+long f64_blocks(int rows, int n, int k, int bt)
+{
+    const long tiles_k = (k + bt - 1) / bt;
+    return ((rows + bt - 1) / bt + (n + bt - 1) / bt) * tiles_k + (n + 63) / 64;
+}
+// 32 x 32 outputs a workgroup where these are enough for every CU
+bool f64_many(int rows, int n, int k) { return f64_blocks(rows, n, k, 32) >= 512; }
+
+hipError_t linear_grad_f64(const double *x, const float *w, const double *y, const double *dy, double *dx, float *dw, float *db, int rows, int n, int k,
+                           bool relu_x, hipStream_t s)
+{
+    auto go = [&](auto kern, int bt, int waves) {
+        const int tiles_k = (k + bt - 1) / bt, x_tiles = dx ? (rows + bt - 1) / bt * tiles_k : 0, w_tiles = dw ? (n + bt - 1) / bt * tiles_k : 0;
+        kern<<<dim3(x_tiles + w_tiles + (db ? (n + 63) / 64 : 0)), dim3(64 * waves), 0, s>>>(x, w, y, dy, dx, dw, db, rows, n, k, relu_x, x_tiles, w_tiles);
+        return hipGetLastError();
+    };
+    return f64_many(rows, n, k) ? go(linear_grad_f64_kernel<2, 4>, 32, 4) : go(linear_grad_f64_kernel<1, 8>, 16, 8);
+}
+
+}  // namespace
+
+size_t linear_grad_scratch(int dtype, int rows, int n, int k, int epilogue)
+{
+    if (dtype == kFP32) return f64_blocks(rows, n, k, 32) < 1l << 24 ? 256 : 0;
+    const LinearPlan p = linear_plan(rows, n, k, epilogue);
+    return p.fits ? p.total : 0;
+}
+
+bool linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan)
+{
+    const LinearPlan p = linear_plan(rows, n, k, epilogue);
+    if (!p.fits) return false;
+    auto tile = [](Tile t) { return kTileRows[t] << 16 | kTileColumns[t]; };
+    plan[0] = tile(p.x_tile);
+    plan[1] = tile(p.w_tile);
+    plan[2] = p.x_shares;
+    plan[3] = p.w_shares;
+    plan[4] = p.width;
+    plan[5] = p.sum_shares;
+    return true;
+}
+
+hipError_t launch_linear_grad(const void *x, const void *w, const void *y, const void *dy, void *dx, void *dw, void *db, void *scratch, int dtype, int rows,
+                              int n, int k, int epilogue, bool relu_x, hipStream_t s)
+{
+    if (epilogue != 1) y = nullptr;
+    if (dtype == kFP32) {
+        if (f64_blocks(rows, n, k, 32) >= 1l << 24) return hipErrorNotSupported;
+        return linear_grad_f64((const double *)x, (const float *)w, (const double *)y, (const double *)dy, (double *)dx, (float *)dw, (float *)db, rows, n, k,
+                               relu_x, s);
+    }
+    auto f = dtype == kBF16 ? linear_grad<kBF16> : linear_grad<kFP16>;
+    return f((const uint16_t *)x, (const uint16_t *)w, (const uint16_t *)y, dy, (uint16_t *)dx, (uint16_t *)dw, (uint16_t *)db, (char *)scratch, rows, n, k,
+             epilogue, relu_x, s);
+}
+
+}  // namespace zo

@@ -59,3 +59,54 @@ def test_adamw_state_bytes():
     f = zo_amd.zo_kernel_adamw_state_bytes
     assert [f(n, 32) for n in (0, 1, 256, 257)] == [0, 2048, 2048, 4096] and [f(n, 8) for n in (0, 1, 256, 257)] == [0, 520, 520, 1040]
     assert f(10, 16) == 0 and f(1 << 44, 8) == 0 and f((1 << 44) - 1, 32) == 1 << 47
+
+
+def test_linear_grad():
+    #       0 x   1 w   2 y   3 dy  4 dx  5 dw  6 db  7 scratch 8 dtype 9 rows 10 n 11 k 12 epilogue 13 relu_x
+    good = A[:8] + [ZO_BF16, 4, 64, 128, 1, False]
+    f = zo_amd.zo_kernel_linear_grad
+    for at in (0, 1, 2, 3, 7):
+        assert "NULL" in refused(f, *changed(good, at, None))
+    assert "no output" in refused(f, *(good[:4] + [None] * 3 + good[7:]))
+    assert "NULL" in refused(f, None, *good[1:5], None, None, *good[7:13], True)       # relu_x asks for x, dw or not
+    assert "no bias" in refused(f, *changed(good, 12, 3))
+    for at, value in ((8, 3), (8, -1), (9, 0), (9, -4), (10, 0), (11, 0), (10, 60), (11, 60), (12, 4), (12, -1), (0, A[0] + 2), (1, A[1] + 8), (2, A[2] + 2), (3, A[3] + 2),
+                      (4, A[4] + 8), (5, A[5] + 2), (6, A[6] + 2), (7, A[7] + 128), (9, 1 << 21), (10, 1 << 23), (11, 1 << 23)):
+        refused(f, *changed(good, at, value))
+        if 8 <= at <= 12:
+            assert zo_amd.zo_kernel_linear_grad_scratch_bytes(*changed(good, at, value)[8:13]) == 0
+    assert zo_amd.zo_kernel_linear_grad_scratch_bytes(ZO_FP32, 1, 1, 1, 0) > 0
+
+
+@pytest.mark.parametrize("dtype,wide,narrow,weight", [(ZO_FP32, 8, 8, 4), (ZO_BF16, 4, 2, 2), (ZO_FP16, 4, 2, 2)])
+def test_linear_gradients_lie_apart(dtype, wide, narrow, weight):
+    f = zo_amd.zo_kernel_linear_grad
+    x, w, y, dy, dx, dw, db = A[:7]
+    for epilogue, each in ((0, narrow), (1, narrow), (2, wide)):
+        args = A[:8] + [dtype, 4, 64, 128, epilogue, True]
+        moves = [(4, x, "dx overlaps x"), (4, x + 512 * narrow - 16, "dx overlaps x"), (4, w, "dx overlaps w"), (4, dy, "dx overlaps dy"), (4, dy + 256 * each - 16, "dx overlaps dy"),
+                 (5, dx + 16, "dx overlaps dw"), (5, w, "dw overlaps w"), (5, x - 64 * 128 * weight + 16, "dw overlaps x"), (6, dw + 64 * 128 * weight - 16, "dw overlaps db"),
+                 (6, dy, "db overlaps dy"), (6, w, "db overlaps w")]
+        if epilogue == 1:
+            moves += [(4, y, "dx overlaps y"), (5, y + 16, "dw overlaps y")]
+        for at, address, words in moves:
+            assert words in refused(f, *changed(args, at, address))
+
+
+def test_linear_grad_plan():
+    p = zo_amd.zo_kernel_linear_grad_plan(8192, 20480, 5120, 0)
+    assert p["dx"] == p["dw"] == (256, 256) and p["copy_columns"] == 0
+    assert zo_amd.zo_kernel_linear_grad_plan(8192, 768, 768, 2)["dw_shares"] > 1
+    assert zo_amd.zo_kernel_linear_grad_plan(20, 8192, 2048, 1)["dx_shares"] > 1
+    for n, epilogue in ((72, 0), (64, 1), (64, 2)):
+        assert zo_amd.zo_kernel_linear_grad_plan(100, n, 64, epilogue)["copy_columns"] >= n
+    for bad in ((0, 64, 64, 0), (4, 60, 64, 0), (4, 64, 60, 0), (4, 64, 64, 4)):
+        refused(zo_amd.zo_kernel_linear_grad_plan, *bad)
+    assert zo_amd.lib().zo_kernel_linear_grad_plan(4, 64, 64, 0, None) == zo_amd.ZO_EINVAL
+
+
+@pytest.mark.parametrize("dtype,rows,n,k", [(ZO_BF16, 64, 1 << 22, 1 << 18), (ZO_FP16, 1 << 20, 64, 1 << 22), (ZO_FP32, 1 << 20, 64, 1 << 17)])
+def test_linear_grad_of_more_tiles_than_a_launch_holds(dtype, rows, n, k):
+    assert zo_amd.zo_kernel_linear_grad_scratch_bytes(dtype, rows, n, k, 0) == 0
+    assert "tiles" in refused(zo_amd.zo_kernel_linear_grad, *[(i + 1) << 44 for i in range(8)], dtype, rows, n, k, 0, False)
+    assert zo_amd.zo_kernel_linear_grad_scratch_bytes(dtype, rows >> 4, max(n >> 4, 8), k >> 4, 0) > 0
