@@ -441,6 +441,20 @@ int zo_kernel_linear_grad(const void *x, const void *w, const void *y, const voi
  * G (0: none), plan[5] the shares of db's sums.  plan holds 6 numbers.  Host only. */
 int zo_kernel_linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan);
 
+/* Backward pass of zo_kernel_attention: `out` is what the forward call left, dout its gradient [n_seq seq, d]; dqkv [n_seq seq, 3 d] gets
+ * the gradients of q | k | v, heads contiguous inside each:  with P = softmax(q k^T / sqrt(d_head)) over the keys up to the query's own and
+ * D = sum_c dout out,
+ *     dv = P^T dout,   dS = P (dout v^T - D),   dq = dS k / sqrt(d_head),   dk = dS^T q / sqrt(d_head).
+ * dqkv overlaps no input (ZO_EINVAL if it does).  Probabilities are worked again from q and k, nothing of the forward call's but `out` is
+ * needed.  2-byte dtypes: d_head a multiple of 8, buffers 16-byte aligned (ZO_EINVAL otherwise); heads of 64, 80, 96, 112 and 128 run on the matrix
+ * cores, which take P and dS rounded to the type (ZO_FP16: scaled so that no finite P or dS leaves the type's range), others on a slower kernel.  An
+ * element of qkv, out or dout that is not finite makes gradients of its sequence and head that are none, those of earlier queries that do not
+ * see it among them; other sequences and heads do not see it.  Any length up to 2^20 positions; up to 2^20 channels and 2^30 rows, and no more
+ * workgroups than a launch holds (2^24 tiles of 64 rows of one head; 2^25 rows on the slower kernel): ZO_EINVAL, and 0 scratch bytes, beyond. */
+size_t zo_kernel_attention_grad_scratch_bytes(int dtype, int n_seq, int seq, int n_heads, int d_head);
+int zo_kernel_attention_grad(const void *qkv, const void *out, const void *dout, void *dqkv, void *scratch, int dtype, int n_seq, int seq,
+                             int n_heads, int d_head, void *stream);
+
 /* One AdamW step over n_tensors tensors.  With t = step, for every element:
  *     g = c grad,   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
  *     p <- p - (lr weight_decay p + lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)).

@@ -29,6 +29,7 @@ EXPORTS = (
     "zo_kernel_layernorm", "zo_kernel_layernorm_grad_scratch_bytes", "zo_kernel_layernorm_grad", "zo_kernel_lmhead_grad_scratch_bytes",
     "zo_kernel_lmhead_grad_plan", "zo_kernel_lmhead_grad", "zo_kernel_grad_clip_scratch_bytes", "zo_kernel_grad_clip",
     "zo_kernel_linear_grad_scratch_bytes", "zo_kernel_linear_grad_plan", "zo_kernel_linear_grad",
+    "zo_kernel_attention_grad_scratch_bytes", "zo_kernel_attention_grad",
     "zo_kernel_adamw_state_bytes", "zo_kernel_adamw",
 )
 
@@ -108,6 +109,9 @@ def lib():
         L.zo_kernel_linear_grad_scratch_bytes.argtypes = [i32, i32, i32, i32, i32]
         L.zo_kernel_linear_grad_plan.argtypes = [i32, i32, i32, i32, vp]
         L.zo_kernel_linear_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
+        L.zo_kernel_attention_grad_scratch_bytes.restype = sz
+        L.zo_kernel_attention_grad_scratch_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.zo_kernel_attention_grad.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]
         f64 = ctypes.c_double
         L.zo_kernel_adamw_state_bytes.restype = sz
         L.zo_kernel_adamw_state_bytes.argtypes = [u64, i32]
@@ -386,6 +390,14 @@ def zo_kernel_linear_grad_plan(rows, n, k, epilogue):
 def zo_kernel_linear_grad(x, w, y, dy, dx, dw, db, scratch, dtype, rows, n, k, epilogue, relu_x=False, stream=None):
     _check(lib().zo_kernel_linear_grad(_ptr(x), _ptr(w), _ptr(y), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(db), _ptr(scratch), dtype, rows, n, k, epilogue,
                                        int(relu_x), _stream(stream)))
+
+
+def zo_kernel_attention_grad_scratch_bytes(dtype, n_seq, seq, n_heads, d_head):
+    return int(lib().zo_kernel_attention_grad_scratch_bytes(dtype, n_seq, seq, n_heads, d_head))
+
+
+def zo_kernel_attention_grad(qkv, out, dout, dqkv, scratch, dtype, n_seq, seq, n_heads, d_head, stream=None):
+    _check(lib().zo_kernel_attention_grad(_ptr(qkv), _ptr(out), _ptr(dout), _ptr(dqkv), _ptr(scratch), dtype, n_seq, seq, n_heads, d_head, _stream(stream)))
 
 
 def zo_kernel_adamw_state_bytes(numel, state_bits):

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(CSRC, "libzo.so")
 SOURCES = ["zo_api.hip", "zo_stream_kernels.hip", "zo_forward_kernels.hip", "zo_gemm_mfma.hip", "zo_attn_mfma.hip",
            "zo_grad_kernels.hip", "zo_gemm_grad.hip",
-           "zo_linear_grad.hip", "zo_adamw.hip"]
+           "zo_linear_grad.hip", "zo_attn_grad.hip", "zo_adamw.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 

@@ -1547,6 +1547,38 @@ extern "C" int zo_kernel_linear_grad(const void *x, const void *w, const void *y
     return ZO_OK;
 }
 
+static bool attention_grad_shape(int dtype, int n_seq, int seq, int n_heads, int d_head)
+{
+    return n_seq >= 1 && seq >= 1 && n_heads >= 1 && d_head >= 1 && d_head <= 128 && (dtype == ZO_FP32 || d_head % 8 == 0) && seq <= kMaxGradRows &&
+           (int64_t)n_seq * seq <= 1ll << 30 && (int64_t)n_heads * d_head <= kMaxGradRows;
+}
+
+extern "C" size_t zo_kernel_attention_grad_scratch_bytes(int dtype, int n_seq, int seq, int n_heads, int d_head)
+{
+    return dtype < 0 || dtype > 2 || !attention_grad_shape(dtype, n_seq, seq, n_heads, d_head) ? 0 : attention_grad_scratch(dtype, n_seq, seq, n_heads, d_head);
+}
+
+extern "C" int zo_kernel_attention_grad(const void *qkv, const void *out, const void *dout, void *dqkv, void *scratch_mem, int dtype, int n_seq, int seq,
+                                        int n_heads, int d_head, void *stream)
+{
+    ZO_TRY(check_dtype(dtype));
+    if (!qkv || !out || !dout || !dqkv || !scratch_mem) return fail(ZO_EINVAL, "NULL argument");
+    if (!attention_grad_shape(dtype, n_seq, seq, n_heads, d_head))
+        return fail(ZO_EINVAL, "bad shape: %d sequences of %d, %d heads of %d (up to 2^20 positions and channels, 2^30 rows, heads of 128; 2-byte types: of a multiple of 8)",
+                    n_seq, seq, n_heads, d_head);
+    if (dtype != ZO_FP32 && ((uintptr_t)qkv % 16 || (uintptr_t)out % 16 || (uintptr_t)dout % 16 || (uintptr_t)dqkv % 16))
+        return fail(ZO_EINVAL, "buffers must be 16-byte aligned");
+    if ((uintptr_t)scratch_mem % 256) return fail(ZO_EINVAL, "scratch must be 256-byte aligned");
+    const size_t n = (size_t)n_seq * seq * n_heads * d_head * act_bytes(dtype);
+    const Buffer buffers[] = {{"dqkv", dqkv, 3 * n}, {"qkv", qkv, 3 * n}, {"out", out, n}, {"dout", dout, n}};
+    ZO_TRY(check_apart(buffers, 1));
+    const hipError_t err = launch_attention_grad(qkv, out, dout, dqkv, scratch_mem, dtype, n_seq, seq, n_heads, d_head, (hipStream_t)stream);
+    if (err == hipErrorNotSupported)
+        return fail(ZO_EINVAL, "%d sequences of %d, %d heads: more workgroups than one launch holds", n_seq, seq, n_heads);
+    ZO_HIP(err);
+    return ZO_OK;
+}
+
 // ------------------------------------------------------------------ AdamW
 // Whether tensors that a call writes overlap each other or ones that it reads: -1 if not, else the number of one that does.  `written` is
 // sorted here.

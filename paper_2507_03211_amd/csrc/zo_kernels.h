@@ -152,6 +152,12 @@ bool linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan);     
 hipError_t launch_linear_grad(const void *x, const void *w, const void *y, const void *dy, void *dx, void *dw, void *db, void *scratch, int dtype, int rows,
                               int n, int k, int epilogue, bool relu_x, hipStream_t s);
 
+// ---- gradient of the attention (zo_attn_grad.hip) ----
+// 0 bytes and hipErrorNotSupported where a launch would not hold the workgroups
+size_t attention_grad_scratch(int dtype, int n_seq, int seq, int n_heads, int d_head);
+hipError_t launch_attention_grad(const void *qkv, const void *out, const void *dout, void *dqkv, void *scratch, int dtype, int n_seq, int seq, int n_heads,
+                                 int d_head, hipStream_t s);
+
 // ---- AdamW (zo_adamw.hip) ----
 constexpr int kAdamBlock = 256;            // elements of a state's block
 template <int BITS> constexpr size_t kAdamBlockBytes = BITS == 32 ? 2 * 4 * kAdamBlock : 2 * kAdamBlock + 8;

@@ -110,3 +110,29 @@ def test_linear_grad_of_more_tiles_than_a_launch_holds(dtype, rows, n, k):
     assert zo_amd.zo_kernel_linear_grad_scratch_bytes(dtype, rows, n, k, 0) == 0
     assert "tiles" in refused(zo_amd.zo_kernel_linear_grad, *[(i + 1) << 44 for i in range(8)], dtype, rows, n, k, 0, False)
     assert zo_amd.zo_kernel_linear_grad_scratch_bytes(dtype, rows >> 4, max(n >> 4, 8), k >> 4, 0) > 0
+
+
+def test_attention_grad():
+    #       0 qkv 1 out 2 dout 3 dqkv 4 scratch 5 dtype 6 n_seq 7 seq 8 heads 9 d_head
+    good = A[:5] + [ZO_BF16, 2, 5, 3, 64]
+    f = zo_amd.zo_kernel_attention_grad
+    for at in range(5):
+        assert "NULL" in refused(f, *changed(good, at, None))
+    for at, value in ((5, 3), (5, -1), (6, 0), (7, 0), (8, 0), (9, 0), (9, 136), (9, 60), (7, 1 << 21), (8, 1 << 15), (0, A[0] + 2), (1, A[1] + 8), (2, A[2] + 2), (3, A[3] + 8),
+                      (4, A[4] + 128), (6, 1 << 29)):
+        refused(f, *changed(good, at, value))
+        if at >= 5:
+            assert zo_amd.zo_kernel_attention_grad_scratch_bytes(*changed(good, at, value)[5:]) == 0
+    assert zo_amd.zo_kernel_attention_grad_scratch_bytes(ZO_FP32, 1, 1, 1, 1) > 0
+    for shape in ((ZO_BF16, 1 << 22, 64, 8, 64), (ZO_FP32, 1 << 25, 1, 1, 16), (ZO_FP16, 1 << 21, 16, 2, 40), (ZO_FP32, 1, 1, 1 << 16, 4)):
+        assert zo_amd.zo_kernel_attention_grad_scratch_bytes(*shape) == 0
+        assert "launch" in refused(f, *[(i + 1) << 44 for i in range(5)], *shape)
+    assert zo_amd.zo_kernel_attention_grad_scratch_bytes(ZO_BF16, (1 << 21) - 8, 64, 8, 64) > 0
+
+
+@pytest.mark.parametrize("dtype,each", [(ZO_FP32, 8), (ZO_BF16, 2), (ZO_FP16, 2)])
+def test_attention_gradients_lie_apart(dtype, each):
+    qkv, out, dout, dqkv = A[:4]
+    n = 10 * 3 * 64 * each
+    for address, words in ((qkv, "qkv"), (qkv + 3 * n - 16, "qkv"), (qkv - 3 * n + 16, "qkv"), (out, "out"), (out + n - 16, "out"), (dout - 3 * n + 16, "dout"), (dout + n - 16, "dout")):
+        assert "dqkv overlaps " + words in refused(zo_amd.zo_kernel_attention_grad, qkv, out, dout, address, A[4], dtype, 2, 5, 3, 64)
