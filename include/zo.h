@@ -460,7 +460,7 @@ int zo_kernel_attention_grad(const void *qkv, const void *out, const void *dout,
  *     p <- p - (lr weight_decay p + lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)).
  * Each scalar is worked in fp64 and rounded to fp32 once, each operation between tensors is one fp32 rounding: the same bits every time.
  *   param, grad, state, numel  host arrays of n_tensors device pointers and counts, read before the call returns; param and grad of dtype's
- *                    storage type; all 16-byte aligned.  numel 0: skipped.  No tensor's parameters or state overlap anything else
+ *                    storage type; all 16-byte aligned (an 8-bit state: 8).  numel 0: skipped.  No tensor's parameters or state overlap anything else
  *                    (ZO_EINVAL if they do); gradients may lie as they like.
  *   state            a tensor's moments, zo_kernel_adamw_state_bytes(numel, state_bits) bytes, all zero before step 1: blocks of 256
  *                    elements (the last one whole, zeros behind the tensor's end).  state_bits 32: a block is 256 fp32 m, then 256 fp32 v.

@@ -1634,7 +1634,7 @@ extern "C" int zo_kernel_adamw(void *const *param, const void *const *grad, void
             if (numel[i] == 0) continue;
             if (!param[i] || !grad[i] || !state[i]) return fail(ZO_EINVAL, "tensor %d is NULL", i);
             const uintptr_t p = (uintptr_t)param[i], g = (uintptr_t)grad[i], s = (uintptr_t)state[i];
-            if (p % 16 || g % 16 || s % 16) return fail(ZO_EINVAL, "tensor %d is not 16-byte aligned", i);
+            if (p % 16 || g % 16 || s % (state_bits == 8 ? 8 : 16)) return fail(ZO_EINVAL, "tensor %d is not 16-byte aligned (an 8-bit state: 8)", i);
             if ((p | g | s) >> 48) return fail(ZO_EINVAL, "tensor %d: not a device address", i);
             if (numel[i] >= 1ull << 44) return fail(ZO_EINVAL, "tensor %d has %llu elements", i, (unsigned long long)numel[i]);
             r[n++] = Range{p, p + numel[i] * each, i};

@@ -34,6 +34,8 @@ def test_adamw():
                       (14, -1.0), (15, 2)):
         refused(f, *changed(good, at, value))
     assert "stochastic" in refused(f, *changed(changed(good, 5, ZO_FP32), 15, 1))
+    # a block of an 8-bit state is 520 bytes: states side by side lie on 8
+    assert "aligned" in refused(f, *changed(changed(good, 6, 8), 2, [A[4] + 4, A[5]]))
     L = zo_amd.lib()
     assert L.zo_kernel_adamw(None, None, None, None, 1, ZO_BF16, 8, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1, None, 1.0, 0, 0, None) == zo_amd.ZO_EINVAL
     with pytest.raises(ValueError):

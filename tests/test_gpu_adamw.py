@@ -323,6 +323,21 @@ def test_more_elements_than_32_bits_count():
     assert not bool(param[:1 << 20].any()) and not bool(state[:1 << 20].any())
 
 
+def test_8_bit_states_side_by_side():
+    """Blocks of 520 bytes, tensor behind tensor: states on odd multiples of 8."""
+    ts = Tensors(zi.BF16, 8, [256, 700, 5, 300], 12)
+    flat = torch.cat([s.t for s in ts.state])
+    sizes = [s.t.numel() for s in ts.state]
+    views = list(flat.split(sizes))
+    assert any(v.data_ptr() % 16 for v in views)
+    before = ts.host()
+    zo_amd.zo_kernel_adamw([p.t for p in ts.param], ts.grad, views, ts.numels, 4, zi.BF16, 8, LR, B1, B2, EPS, WD, 6)
+    torch.cuda.synchronize()
+    for s, v in zip(ts.state, views):
+        s.t.copy_(v)
+    same(ts, expect(ts, *before, 6))
+
+
 def test_nothing_to_do():
     zo_amd.zo_kernel_adamw([], [], [], [], 0, zi.BF16, 32, LR, B1, B2, EPS, WD, 1)
     zo_amd.zo_kernel_adamw([None], [None], [None], [0], 1, zi.BF16, 8, LR, B1, B2, EPS, WD, 1)
