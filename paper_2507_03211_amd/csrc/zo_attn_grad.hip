@@ -3,10 +3,9 @@
 //
 //   dV = P^T dO,   dP = dO V^T,   dS = P (dP - D),   dQ = dS K / sqrt(d_head),   dK = dS^T Q / sqrt(d_head)
 //
-// Matrix path (16-bit types, heads of 64, 80, 96, 112, 128), three launches:
-//   rows     D, and in fp16 what bounds dS (below)
-//   queries  a wavefront's 32 queries against the keys they see: S, dP, dQ.  The softmax runs along (one pass, a reference that is raised
-//            as scores pass it), so that logsumexp comes out at the end, for the third launch
+// Matrix path (16-bit types, heads of 64, 80, 96, 112, 128), two launches, and in fp16 one before them that finds what bounds dS (below):
+//   queries  a wavefront's 32 queries against the keys they see: D, S, dP, dQ.  The softmax runs along (one pass, a reference that is raised
+//            as scores pass it), so that logsumexp comes out at the end, for the other launch
 //   keys     a wavefront's 32 keys against the queries that see them: S, dP, dV, dK
 // Seven products instead of five: with dQ from the launch over the keys it would take sums of other workgroups', in memory and in an order
 // that changes.  Both are computed so that a lane owns a column of the scores (a query there, a key here), and the contraction of the second
@@ -50,7 +49,8 @@ __device__ __forceinline__ void swap_halves(float x, float &a, float &b)
     b = __uint_as_float(r[1]);
 }
 
-constexpr int kOwn = 128, kTile = 64;      // rows of a workgroup's own (32 a wavefront), rows of a tile that streams through LDS
+constexpr int kOwn = 128, kUnit = 32;      // rows of a workgroup's own (32 a wavefront), rows of a tile that streams through LDS
+constexpr int kRows = 64;                  // rows of a workgroup of the first launch
 
 // fp16: dS = P (dP - D) may lie anywhere: |dP| and |D| are at most A B, with A the largest norm of a row of dO and B of a row of V in the
 // sequence and head, so 2^e dS with 2^e = 2^14 / (2 A B) rounded down is within the type whatever P is, and numbers 2^28 below that bound are still
@@ -68,105 +68,100 @@ __device__ __forceinline__ int scale_exponent(const RowTops *tops, int tiles)
     return ab > 0.0f && ab < 0x1p100f ? 12 - (int)((__float_as_uint(ab) >> 23) & 0xff) + 127 : 0;
 }
 
-// D of 64 rows of one head of one sequence; 16 lanes a row and head (8 where it has 8 pieces of 16 bytes).
-template <int DT, int DH>
-__global__ __launch_bounds__(256) void attn_grad_rows_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ out, const uint16_t *__restrict__ dout,
-                                                             float *__restrict__ delta, RowTops *__restrict__ tops, int seq, int n_heads, int tiles)
+// The largest |dO|^2 and |V|^2 of 64 rows of one head of one sequence; 16 lanes a row (8 where it has 8 pieces of 16 bytes).
+template <int DH>
+__global__ __launch_bounds__(256) void attn_grad_tops_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, RowTops *__restrict__ tops, int seq,
+                                                             int n_heads, int tiles)
 {
-    constexpr int PIECES = DH / 8, LANES = PIECES <= 8 ? 8 : 16, ROWS = 256 / LANES;
+    constexpr int PIECES = DH / 8, LANES = PIECES <= 8 ? 8 : 16, ROWS = 256 / LANES, TURNS = kRows / ROWS;
     __shared__ float top[2][4];
     const int tile = (int)blockIdx.x % tiles, pair = (int)blockIdx.x / tiles, s = pair / n_heads, head = pair % n_heads, d = n_heads * DH;
     const int piece = threadIdx.x % LANES;
-    float most_out = 0.0f, most_value = 0.0f;
-    for (int r0 = 0; r0 < kTile; r0 += ROWS) {
-        const int r = tile * kTile + r0 + (int)threadIdx.x / LANES;
+    uint4 x[TURNS][2];                                          // all under way together
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const int r = tile * kRows + i * ROWS + (int)threadIdx.x / LANES;
         const bool live = r < seq && piece < PIECES;
         const size_t row = (size_t)s * seq + (r < seq ? r : 0), at = row * d + head * DH + (piece < PIECES ? 8 * piece : 0);
-        const uint4 zero{0, 0, 0, 0};
-        const uint4 o = live ? *(const uint4 *)(out + at) : zero, g = live ? *(const uint4 *)(dout + at) : zero;
-        const uint4 v = live && DT == kFP16 ? *(const uint4 *)(qkv + at + row * 2 * d + 2 * d) : zero;
-        float sum = 0.0f, out2 = 0.0f, value2 = 0.0f;
-        auto two = [&](uint32_t a, uint32_t b, uint32_t c) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 16) {
-                const float fa = Prec<DT>::a2acc((uint16_t)(a >> e)), fb = Prec<DT>::a2acc((uint16_t)(b >> e));
-                sum = __builtin_fmaf(fa, fb, sum);
-                if constexpr (DT == kFP16) {
-                    const float fc = Prec<DT>::a2acc((uint16_t)(c >> e));
-                    out2 = __builtin_fmaf(fb, fb, out2);
-                    value2 = __builtin_fmaf(fc, fc, value2);
-                }
-            }
-        };
-        two(o.x, g.x, v.x); two(o.y, g.y, v.y); two(o.z, g.z, v.z); two(o.w, g.w, v.w);
-#pragma unroll
-        for (int m = LANES / 2; m > 0; m >>= 1) {
-            sum += __shfl_xor(sum, m, 64);
-            if constexpr (DT == kFP16) {
-                out2 += __shfl_xor(out2, m, 64);
-                value2 += __shfl_xor(value2, m, 64);
-            }
-        }
-        if (piece == 0 && r < seq) delta[(size_t)pair * seq + r] = sum;
-        if constexpr (DT == kFP16) {
-            most_out = out2 > most_out ? out2 : most_out;
-            most_value = value2 > most_value ? value2 : most_value;
-        }
+        x[i][0] = live ? *(const uint4 *)(dout + at) : uint4{0, 0, 0, 0};
+        x[i][1] = live ? *(const uint4 *)(qkv + at + row * 2 * d + 2 * d) : uint4{0, 0, 0, 0};
     }
-    if constexpr (DT == kFP16) {
-        most_out = wave_max(most_out);
-        most_value = wave_max(most_value);
-        if ((threadIdx.x & 63) == 0) { top[0][threadIdx.x >> 6] = most_out; top[1][threadIdx.x >> 6] = most_value; }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            RowTops t{};
-            for (int w = 0; w < 4; ++w) {
-                t.out2 = top[0][w] > t.out2 ? top[0][w] : t.out2;
-                t.value2 = top[1][w] > t.value2 ? top[1][w] : t.value2;
+    float most[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const uint32_t w[4] = {x[i][which].x, x[i][which].y, x[i][which].z, x[i][which].w};
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = Prec<kFP16>::a2acc((uint16_t)(w[e / 2] >> (16 * (e & 1))));
+                sum = __builtin_fmaf(v, v, sum);
             }
-            tops[blockIdx.x] = t;
+#pragma unroll
+            for (int m = LANES / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m, 64);
+            most[which] = sum > most[which] ? sum : most[which];
         }
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        const float m = wave_max(most[which]);
+        if ((threadIdx.x & 63) == 0) top[which][threadIdx.x >> 6] = m;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        const float *t = top[threadIdx.x];
+        const float a = t[0] > t[1] ? t[0] : t[1], b = t[2] > t[3] ? t[2] : t[3];
+        (&tops[blockIdx.x].out2)[threadIdx.x] = a > b ? a : b;
     }
 }
 
-// Tiles of 64 rows in LDS, [row][piece of 16 bytes]: read by rows (32 rows, one piece: an operand with its contraction over the channels) and, by the
+// Tiles of 32 rows in LDS, [row][piece of 16 bytes]: read by rows (32 rows, one piece: an operand with its contraction over the channels) and, by the
 // transposing read, by columns (4 rows x 32 bytes per 16 lanes: one with its contraction over the rows).  Pieces are XOR-swizzled by the row so that
 // both are free of bank conflicts: 16 rows of one piece lie on 16 distinct 16-byte places of the 256-byte bank line, four rows on its
 // four quarters.  Rows are padded to 192 or 256 bytes (80 and 112 channels); what lies there is a piece over again, for channels that are not stored.
 template <int DH> struct TileShape {
-    static constexpr int CHD = DH / 8, CH = DH == 64 ? 8 : DH <= 96 ? 12 : 16, KS = DH / 16, CT = (DH + 31) / 32, PIECES = kTile * CH;
+    static constexpr int CHD = DH / 8, CH = DH == 64 ? 8 : DH <= 96 ? 12 : 16, KS = DH / 16, CT = (DH + 31) / 32, PIECES = kUnit * CH;
     static __device__ __forceinline__ int swizzle(int r) { return CH == 16 ? (r & 3) << 2 | ((r >> 2) & 3) : CH == 12 ? (r >> 2) & 3 : ((r >> 1) & 1) << 2 | ((r >> 2) & 3); }
     static constexpr int in_row(int piece) { return piece < CHD ? piece : piece - 2; }
 };
+// A stage's tiles begin at multiples of 4 KiB, and the pieces of a row and of four rows differ in address bits that nothing else sets, so that an exclusive
+// or with a constant leads from one piece's address to another's: a register for the rows, two for the columns, instead of one for each piece.
 template <int DH> struct TileReader : TileShape<DH> {
     using T = TileShape<DH>;
-    int row[T::KS], column[T::CT][2];       // u32x4 index of (row lane % 32, k-step s); element offset of a column fragment, row base 0 or 8 mod 16
+    static constexpr bool kXor = T::CH != 12;                   // (192-byte rows: pieces within aligned groups of four only)
+    uint32_t row[kXor ? 1 : 2], column[2];  // byte offset of (row lane % 32, k-step 0 (1)); of a column fragment, row base 0 or 8 mod 16
     __device__ __forceinline__ TileReader(int lane)
     {
         const int fr = lane & 31, fh = lane >> 5, j = lane & 15;
 #pragma unroll
-        for (int s = 0; s < T::KS; ++s) row[s] = fr * T::CH + ((2 * s + fh) ^ T::swizzle(fr));
+        for (int s = 0; s < (kXor ? 1 : 2); ++s) row[s] = (fr * T::CH + ((2 * s + fh) ^ T::swizzle(fr))) * 16;
 #pragma unroll
-        for (int c = 0; c < T::CT; ++c)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int r = 8 * b + 4 * fh + (j >> 2), chan = c * 32 + 16 * ((lane >> 4) & 1) + 4 * (j & 3);
-                column[c][b] = (r * T::CH + ((chan >> 3) ^ T::swizzle(r))) * 8 + (chan & 7);
-            }
+        for (int b = 0; b < 2; ++b) {
+            const int r = 8 * b + 4 * fh + (j >> 2), chan = 16 * ((lane >> 4) & 1) + 4 * (j & 3);
+            column[b] = (r * T::CH + ((chan >> 3) ^ T::swizzle(r))) * 16 + 2 * (chan & 7);
+        }
     }
-    // rows half * 32 + lane % 32, channels of k-step s
-    __device__ __forceinline__ uint4 by_row(const u32x4 *tile, int half, int s) const { return __builtin_bit_cast(uint4, tile[half * 32 * T::CH + row[s]]); }
+    static __device__ __forceinline__ uint32_t address(const u32x4 *tile) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const u32x4 *)tile; }
+    // rows lane % 32, channels of k-step s
+    __device__ __forceinline__ uint4 by_row(const u32x4 *tile, int s) const
+    {
+        const uint32_t at = kXor ? (address(tile) + row[0]) ^ (uint32_t)(32 * s) : address(tile) + row[s % (kXor ? 1 : 2)] + (s / 2) * 64;
+        return __builtin_bit_cast(uint4, *(__attribute__((address_space(3))) const u32x4 *)(uintptr_t)at);
+    }
     // channels of tile c, rows first + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}, first a multiple of 16
     __device__ __forceinline__ uint4 by_column(const u32x4 *tile, int first, int c) const
     {
         typedef __attribute__((address_space(3))) v4i16 *lds;
-        const uint16_t *p = (const uint16_t *)tile + first * T::CH * 8;
-        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + column[c][0])));
-        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + column[c][1])));
+        auto at = [&](int b) {
+            const uint32_t base = address(tile) + column[b];
+            return (kXor ? base ^ (uint32_t)(64 * c) : base + 64 * c) + (uint32_t)(first * T::CH * 16);
+        };
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(uintptr_t)at(0)));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(uintptr_t)at(1)));
         return uint4{lo.x, lo.y, hi.x, hi.y};
     }
 };
-// 64 rows of a matrix, straight into LDS; rows past the end of the sequence come as zeros (the buffer ends there).
+// 32 rows of a matrix, straight into LDS; rows past the end of the sequence come as zeros (the buffer ends there).
 __device__ __forceinline__ void dma16(u32x4 rows, uint32_t lane_off, uint32_t lds_off)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(lane_off), "s"(rows), "s"(lds_off) : "memory", "m0");
@@ -180,137 +175,244 @@ __device__ __forceinline__ u32x4 buffer_of(uint64_t first, uint32_t bytes)
     return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(first >> 32)),
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
-template <int DH> struct TileLoader : TileShape<DH> {
+// Every wavefront of the workgroup's WAVES has LOADS loads: where a tile's do not deal out evenly, some come twice.
+template <int DH, int WAVES> struct TileLoader : TileShape<DH> {
     using T = TileShape<DH>;
-    static constexpr int LOADS = T::PIECES / 256;               // of a wavefront
+    static constexpr int ALL = T::PIECES / 64, LOADS = (ALL + WAVES - 1) / WAVES;
     uint32_t off[LOADS];
-    uint64_t base;
     uint32_t ld;
     int wave;
-    // `first`: the sequence's first row, this head's first channel
-    __device__ __forceinline__ TileLoader(const uint16_t *first, int ld_, int lane, int wave_) : base((uint64_t)(uintptr_t)first), ld((uint32_t)ld_ * 2u), wave(wave_)
+    __device__ __forceinline__ TileLoader(int ld_, int lane, int wave_) : ld((uint32_t)ld_ * 2u), wave(wave_)
     {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int p = 64 * (LOADS * wave + i) + lane, r = p / T::CH;
+            const int p = 64 * number(i) + lane, r = p / T::CH;
             off[i] = (uint32_t)r * ld + (uint32_t)T::in_row((p % T::CH) ^ T::swizzle(r)) * 16u;
         }
     }
-    __device__ __forceinline__ void load(u32x4 *tile, int row0, int seq) const
+    __device__ __forceinline__ int number(int i) const { return ALL % WAVES == 0 ? WAVES * i + wave : (WAVES * i + wave) % ALL; }
+    // `first`: the sequence's first row, this head's first channel
+    __device__ __forceinline__ void load(u32x4 *tile, const uint16_t *first, int row0, int seq) const
     {
-        const int left = seq - row0 < kTile ? seq - row0 : kTile;
-        const u32x4 rows = buffer_of(base + (uint64_t)row0 * ld, (uint32_t)(left - 1) * ld + DH * 2);
+        const int left = seq - row0 < kUnit ? seq - row0 : kUnit;
+        const u32x4 rows = buffer_of((uint64_t)(uintptr_t)first + (uint64_t)row0 * ld, (uint32_t)(left - 1) * ld + DH * 2);
         const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4 *)tile;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) dma16(rows, off[i], lds + (uint32_t)(LOADS * wave + i) * 1024u);
+        for (int i = 0; i < LOADS; ++i) dma16(rows, off[i], lds + (uint32_t)number(i) * 1024u);
     }
 };
 
-// Which workgroup has which rows of which (sequence, head): consecutive workgroups go round-robin to the 8 XCDs, all tiles of a pair to one of
-// them, whose L2 then holds what they share.
+// Which workgroup has which rows of which (sequence, head): the longest tiles of all pairs first, so that what is left at a launch's end is
+// short; consecutive workgroups go round-robin to the 8 XCDs, all tiles of a pair to one of them.  All tiles of a pair, then the next one's:
+// queries and keys of 4 x 2048, 40 heads of 128 441 and 553 us, here 318 and 452; 16 x 512, 12 of 64 29.0 and 42.0, here 22.8 and 34.7.
 struct Item { int pair, tile; };
-__device__ __forceinline__ Item item_of(int block, int tiles) { return {block / 8 / tiles * 8 + block % 8, block / 8 % tiles}; }
+__device__ __forceinline__ Item item_of(int block, int pairs)
+{
+    const int row = (pairs + 7) / 8 * 8;
+    return {block % row, block / row};
+}
+
+// Both launches work their rows in units of 32 against 32, software-pipelined, since the one or two wavefronts of a SIMD leave little else to
+// hide an instruction's wait behind.  Step u, with S of unit u there:
+//     dP of unit u                  |  P of unit u
+//     S of unit u + 1               |  dS of unit u
+//     the second products of unit u |  what the next products start from
+// Row fragments run through rings that are refilled as they drain, column fragments are read ahead; the sched_barriers pin the order written
+// here.  LDS answers a wavefront in order, so that what is needed soon must not be asked for behind what is not: minus logsumexp and minus D, which
+// S and dP start from, are read into their registers while these have nothing else to hold.  Four stages of tiles in LDS, a tile a unit, one barrier a
+// step: behind it tiles up to u + 1 have landed for everybody, u + 2 may be under way, and u + 3 goes out into the stage that everybody has left.
+constexpr int kStages = 4;
+// until all but a wavefront's last N loads have landed, or all
+template <int N> __device__ __forceinline__ void wait_loads(bool all)
+{
+    if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // word i of two fragments
+{
+    uint4 &f = w[i >> 2];
+    if ((i & 3) == 0) f.x = v;
+    else if ((i & 3) == 1) f.y = v;
+    else if ((i & 3) == 2) f.z = v;
+    else f.w = v;
+}
 
 // ------------------------------------------------------------------ queries
 template <int DT, int DH>
-__global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
-                                                                   const float *__restrict__ delta, float *__restrict__ lse, const RowTops *__restrict__ tops,
+__global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ out, const uint16_t *__restrict__ dout,
+                                                                   uint16_t *__restrict__ dqkv, float *__restrict__ delta, float *__restrict__ lse, const RowTops *__restrict__ tops,
                                                                    int seq, int n_heads, int pairs, int tiles)
 {
     using T = TileShape<DH>;
-    constexpr int KS = T::KS, CT = T::CT;
+    constexpr int KS = T::KS, CT = T::CT, R = 2;
     // the reference is raised when a scaled score passes it by this much: unnormalised probabilities are 2^kRaise at most
     constexpr int kRaise = 4;
-    __shared__ u32x4 ks[2][T::PIECES], vs[2][T::PIECES];
-    const Item item = item_of((int)blockIdx.x, tiles);
+    __shared__ __attribute__((aligned(256))) u32x4 ks[kStages][T::PIECES], vs[kStages][T::PIECES];
+    const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
     const int s = item.pair / n_heads, head = item.pair % n_heads, d = n_heads * DH, ld = 3 * d;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 31, fh = lane >> 5;
     const int q0 = (tiles - 1 - item.tile) * kOwn, w0 = q0 + 32 * wave, q = w0 + fr;          // the longest first
     const uint16_t *base = qkv + (size_t)s * seq * ld + head * DH;
     const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
-    const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * ((seq + kTile - 1) / kTile), (seq + kTile - 1) / kTile) - kRaise : 0;
+    const int row_tiles = (seq + kRows - 1) / kRows;
+    const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) - kRaise : 0;
     const float factor = DT == kFP16 ? ldexpf(1.0f, e) : 1.0f;
 
     uint4 qf[KS], of[KS];
+    float minus_d = 0.0f;
     {
-        const uint16_t *qp = base + (size_t)(q < seq ? q : 0) * ld + 8 * fh, *op = dout + ((size_t)s * seq + (q < seq ? q : 0)) * d + head * DH + 8 * fh;
+        const size_t at = ((size_t)s * seq + (q < seq ? q : 0)) * d + head * DH + 8 * fh;
+        const uint16_t *qp = base + (size_t)(q < seq ? q : 0) * ld + 8 * fh, *gp = dout + at, *op = out + at;
+        uint4 o[KS];
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
+            o[i] = q < seq ? *(const uint4 *)(op + 16 * i) : uint4{0, 0, 0, 0};
+            of[i] = q < seq ? *(const uint4 *)(gp + 16 * i) : uint4{0, 0, 0, 0};
             qf[i] = q < seq ? *(const uint4 *)(qp + 16 * i) : uint4{0, 0, 0, 0};
-            of[i] = q < seq ? *(const uint4 *)(op + 16 * i) : uint4{0, 0, 0, 0};
         }
+        auto two = [&](uint32_t a, uint32_t b) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 16) minus_d = __builtin_fmaf(-Prec<DT>::a2acc((uint16_t)(a >> e)), Prec<DT>::a2acc((uint16_t)(b >> e)), minus_d);
+        };
+#pragma unroll
+        for (int i = 0; i < KS; ++i) { two(o[i].x, of[i].x); two(o[i].y, of[i].y); two(o[i].z, of[i].z); two(o[i].w, of[i].w); }
+        float a, b;
+        swap_halves(minus_d, a, b);
+        minus_d = a + b;
+        if (fh == 0 && q < seq) delta[(size_t)item.pair * seq + q] = minus_d;
     }
-    const float dl = (q < seq ? delta[(size_t)item.pair * seq + q] : 0.0f) * factor;
     const TileReader<DH> read(lane);
-    const TileLoader<DH> load_k(base + d, ld, lane, wave), load_v(base + 2 * d, ld, lane, wave);
-    f32x16 acc[CT] = {};
-    float m_run = -INFINITY, moff = 0.0f, thr = -INFINITY, l_lane = 0.0f;
-    const int last = q0 + kOwn <= seq ? q0 + kOwn : seq, n_tiles = (last + kTile - 1) / kTile;
-    load_k.load(ks[0], 0, seq);
-    load_v.load(vs[0], 0, seq);
-    for (int t = 0; t < n_tiles; ++t) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const TileLoader<DH, 4> loader(ld, lane, wave);
+    const int last = q0 + kOwn <= seq ? q0 + kOwn : seq, n_units = (last + kUnit - 1) / kUnit, u_last = w0 / 32 < n_units ? w0 / 32 : n_units - 1;
+    auto load = [&](int u) {
+        if (u >= n_units) return;
+        loader.load(ks[u % kStages], base + d, u * kUnit, seq);
+        loader.load(vs[u % kStages], base + 2 * d, u * kUnit, seq);
+    };
+    f32x16 acc[CT] = {}, S[2], dP;
+    uint4 kr[R], vr[R], kc[CT], ds[2];
+    float m_run = -INFINITY, moff = 0.0f, thr = -INFINITY, l_lane = 0.0f, top = -INFINITY;
+    auto k_row = [&](int u, int i) { kr[i % R] = read.by_row(ks[u % kStages], i); };
+    auto v_row = [&](int u, int i) { vr[i % R] = read.by_row(vs[u % kStages], i); };
+    auto start = [&] {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) dP[j] = minus_d;
+    };
+    auto mask = [&](f32x16 &x) {                                // of the unit on the diagonal
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (8 * (i >> 2) + 4 * fh + (i & 3) > fr) x[i] = -INFINITY;
+    };
+    auto maximum = [&](const f32x16 &x) {
+        float t = __builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), x[2]);
+#pragma unroll
+        for (int i = 3; i < 15; i += 2) t = __builtin_fmaxf(__builtin_fmaxf(x[i], x[i + 1]), t);
+        return __builtin_fmaxf(t, x[15]);
+    };
+    auto sync = [&](int u) {
+        wait_loads<2 * TileLoader<DH, 4>::LOADS>(u + 2 >= n_units);
         __syncthreads();
-        if (t + 1 < n_tiles) {
-            load_k.load(ks[(t + 1) & 1], (t + 1) * kTile, seq);
-            load_v.load(vs[(t + 1) & 1], (t + 1) * kTile, seq);
+        load(u + 3);
+    };
+    auto step = [&](auto hc, int u) {
+        constexpr int H = decltype(hc)::value;                  // u & 1
+        f32x16 &Sc = S[H], &Sn = S[H ^ 1];
+        const u32x4 *kt = ks[u % kStages];
+        if (__builtin_amdgcn_ballot_w64(top > thr) != 0) {
+            float a, b;
+            swap_halves(top, a, b);
+            const float m_new = __builtin_fmaxf(__builtin_fmaxf(a, b), m_run), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
+            l_lane *= alpha;
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
+            m_run = m_new;
+            moff = -m_new * sc;
+            thr = m_new + (float)kRaise / sc;
         }
-        const u32x4 *kt = ks[t & 1], *vt = vs[t & 1];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int first = t * kTile + 32 * h;
-            if (first > w0) continue;                           // keys that none of the wavefront's queries sees
-            f32x16 S = {}, dP = {};
+        for (int i = 0; i < KS; ++i) {
+            dP = mfma32<DT>(vr[i % R], of[i], dP);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + R < KS) v_row(u, i + R);
+            if (i + R >= KS) k_row(u + 1, i + R - KS);          // (the last unit's successor is multiplied too, from whatever lies there: nothing reads it)
 #pragma unroll
-            for (int i = 0; i < KS; ++i) S = mfma32<DT>(read.by_row(kt, h, i), qf[i], S);
-#pragma unroll
-            for (int i = 0; i < KS; ++i) dP = mfma32<DT>(read.by_row(vt, h, i), of[i], dP);
-            if (first == w0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (8 * (i >> 2) + 4 * fh + (i & 3) > fr) S[i] = -INFINITY;
+            for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) {
+                Sc[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sc[j], sc, moff));
+                l_lane += Sc[j];
             }
-            float top = S[0];
+            asm volatile("" : "+v"(l_lane));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const f32x16 zero = {};
 #pragma unroll
-            for (int i = 1; i < 16; ++i) top = __builtin_fmaxf(top, S[i]);
-            if (__builtin_amdgcn_ballot_w64(top > thr) != 0) {
-                float a, b;
-                swap_halves(top, a, b);
-                const float m_new = __builtin_fmaxf(__builtin_fmaxf(a, b), m_run), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
-                l_lane *= alpha;
+        for (int i = 0; i < KS; ++i) {
+            Sn = mfma32<DT>(kr[i % R], qf[i], i == 0 ? zero : Sn);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + R < KS) k_row(u + 1, i + R);
+            if (i < CT) kc[i] = read.by_column(kt, 0, i);
 #pragma unroll
-                for (int c = 0; c < CT; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
-                m_run = m_new;
-                moff = -m_new * sc;
-                thr = m_new + (float)kRaise / sc;
+            for (int j = 8 * i / KS; j < 8 * (i + 1) / KS; ++j) {
+                auto scaled = [&](float v) { return DT == kFP16 ? v * factor : v; };
+                put(ds, j, pack2<DT>(Sc[2 * j] * scaled(dP[2 * j]), Sc[2 * j + 1] * scaled(dP[2 * j + 1])));
             }
-            uint4 ds[2];
-            uint32_t *w = &ds[0].x;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        start();
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                float v[2];
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i + j], sc, moff));
-                    l_lane += p;
-                    v[j] = p * (DT == kFP16 ? __builtin_fmaf(dP[i + j], factor, -dl) : dP[i + j] - dl);
+            for (int c = 0; c < CT; ++c) {
+                acc[c] = mfma32<DT>(kc[c], ds[k], acc[c]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (k == 0) {
+                    kc[c] = read.by_column(kt, 16, c);
+                } else {
+#pragma unroll
+                    for (int i = R * c / CT; i < R * (c + 1) / CT; ++i) v_row(u + 1, i);
                 }
-                w[i / 2] = pack2<DT>(v[0], v[1]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        if (u + 1 == u_last) mask(Sn);
+        top = maximum(Sn);
+    };
+    load(0);
+    load(1);
+    load(2);
+    sync(0);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) acc[c] = mfma32<DT>(read.by_column(kt, 32 * h + 16 * k, c), ds[k], acc[c]);
-        }
+    for (int i = 0; i < KS; ++i) {
+        const f32x16 zero = {};
+        k_row(0, i);
+        S[0] = mfma32<DT>(kr[i % R], qf[i], i == 0 ? zero : S[0]);
     }
+#pragma unroll
+    for (int i = 0; i < R; ++i) v_row(0, i);
+    start();
+    if (u_last == 0) mask(S[0]);
+    top = maximum(S[0]);
+    int u = 0;
+    for (; u < u_last; u += 2) {
+        step(std::integral_constant<int, 0>{}, u);
+        sync(u + 1);
+        step(std::integral_constant<int, 1>{}, u + 1);
+        if (u + 2 < n_units) sync(u + 2);
+    }
+    if (u == u_last) {
+        step(std::integral_constant<int, 0>{}, u);
+        ++u;
+        if (u < n_units) sync(u);
+    }
+    for (++u; u < n_units; ++u) sync(u);                        // for the other wavefronts
     if (q >= seq) return;
     float a, b;
     swap_halves(l_lane, a, b);
     const float l = a + b;
-    if (fh == 0) lse[(size_t)item.pair * seq + q] = m_run * sc + __builtin_amdgcn_logf(l);
+    // as the third launch's scores start from it: minus logsumexp, before the scaling
+    if (fh == 0) lse[(size_t)item.pair * seq + q] = -(m_run + __builtin_amdgcn_logf(l) / sc);
     const float scale = 1.0f / (l * __builtin_sqrtf((float)DH)) * (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f);
     uint16_t *dq = dqkv + ((size_t)s * seq + q) * ld + head * DH + 4 * fh;
 #pragma unroll
@@ -322,117 +424,239 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 }
 
 // ------------------------------------------------------------------ keys
+// Eight wavefronts, two to a slice of 32 keys, on one SIMD: the first has S, P and dV, the second dP, dS and dK.  A wavefront with all of it would hold
+// 128 accumulators and 64 registers of keys and values at 128 channels and have its SIMD to itself.  P passes from the first to the second
+// through LDS, as the 16-bit numbers that dV's product takes, a step later; the second works a unit behind.  Five stages: it still reads u - 1.
+constexpr int kKeyStages = 5;
 template <int DT, int DH>
-__global__ __launch_bounds__(256, DH <= 96 ? 2 : 1) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
+__global__ __launch_bounds__(512, 2) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
                                                                 const float *__restrict__ delta, const float *__restrict__ lse, const RowTops *__restrict__ tops,
                                                                 int seq, int n_heads, int pairs, int tiles)
 {
     using T = TileShape<DH>;
-    constexpr int KS = T::KS, CT = T::CT;
+    constexpr int KS = T::KS, CT = T::CT, R = KS < 4 ? KS : 4;
     constexpr int kShift = DT == kFP16 ? 14 : 0;               // probabilities carry 2^kShift: down to 2^-28 they are normal numbers
-    __shared__ u32x4 qs[2][T::PIECES], os[2][T::PIECES];
-    __shared__ float rows[2][2][kTile];                         // logsumexp and D of a tile's queries
-    const Item item = item_of((int)blockIdx.x, tiles);
+    __shared__ __attribute__((aligned(256))) u32x4 qs[kKeyStages][T::PIECES], os[kKeyStages][T::PIECES];
+    __shared__ u32x4 mail[2][4][2][64];                         // P of units of either parity, by slice
+    __shared__ float rows[kKeyStages][2][64];                   // minus logsumexp and minus D of a tile's queries, zeros behind them
+    const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
     const int s = item.pair / n_heads, head = item.pair % n_heads, d = n_heads * DH, ld = 3 * d;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 31, fh = lane >> 5;
-    const int k0 = item.tile * kOwn, w0 = k0 + 32 * wave, key = w0 + fr;                      // the longest first
-    const uint16_t *base = qkv + (size_t)s * seq * ld + head * DH;
-    const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
-    const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * ((seq + kTile - 1) / kTile), (seq + kTile - 1) / kTile) : 0;
-    const float factor = DT == kFP16 ? ldexpf(1.0f, e - kShift) : 1.0f;
-    uint4 kf[KS], vf[KS];
-    {
-        const uint16_t *kp = base + d + (size_t)(key < seq ? key : 0) * ld + 8 * fh;
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            kf[i] = key < seq ? *(const uint4 *)(kp + 16 * i) : uint4{0, 0, 0, 0};
-            vf[i] = key < seq ? *(const uint4 *)(kp + d + 16 * i) : uint4{0, 0, 0, 0};
-        }
-    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slice = wave & 3, fr = lane & 31, fh = lane >> 5;
+    const int k0 = item.tile * kOwn, w0 = k0 + 32 * slice, key = w0 + fr;                     // the longest first
+    const uint16_t *base = qkv + (size_t)s * seq * ld + head * DH, *obase = dout + (size_t)s * seq * d + head * DH;
     const TileReader<DH> read(lane);
-    const TileLoader<DH> load_q(base, ld, lane, wave), load_o(dout + (size_t)s * seq * d + head * DH, d, lane, wave);
-    auto load = [&](int t) {
-        load_q.load(qs[t & 1], t * kTile, seq);
-        load_o.load(os[t & 1], t * kTile, seq);
-        if (wave < 2) {                                          // (queries past the end get zeros: their dO is, too)
-            const int left = seq - t * kTile < kTile ? seq - t * kTile : kTile;
-            const float *from = (wave ? delta : lse) + (size_t)item.pair * seq + t * kTile;
-            dma4(buffer_of((uint64_t)(uintptr_t)from, (uint32_t)left * 4), 4 * lane, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&rows[t & 1][wave][0]);
-        }
+    const TileLoader<DH, 8> load_q(ld, lane, wave), load_o(d, lane, wave);
+    const int u0 = k0 / kUnit, n_units = (seq + kUnit - 1) / kUnit, u_first = w0 / kUnit;
+    auto load = [&](int u, int stage) {
+        if (u >= n_units) return;
+        load_q.load(qs[stage], base, u * kUnit, seq);
+        load_o.load(os[stage], obase, u * kUnit, seq);
+        // every wavefront one of the two (queries past the end get zeros: their dO is, too)
+        const int left = seq - u * kUnit < kUnit ? seq - u * kUnit : kUnit, which = wave & 1;
+        const float *from = (which ? delta : lse) + (size_t)item.pair * seq + u * kUnit;
+        dma4(buffer_of((uint64_t)(uintptr_t)from, (uint32_t)left * 4), 4 * lane, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&rows[stage][which][0]);
     };
-    f32x16 dk[CT] = {}, dv[CT] = {};
-    const int t0 = k0 / kTile, n_tiles = (seq + kTile - 1) / kTile;
-    load(t0);
-    for (int t = t0; t < n_tiles; ++t) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // stages of units u - 1, u, u + 1
+    int st_last = 3, st = 4, st_next = 0;
+    auto sync = [&](int u) {
+        wait_loads<2 * TileLoader<DH, 8>::LOADS + 1>(u + 2 >= n_units);
         __syncthreads();
-        if (t + 1 < n_tiles) load(t + 1);
-        const u32x4 *qt = qs[t & 1], *ot = os[t & 1];
+        st_last = st;
+        st = st_next;
+        st_next = st == kKeyStages - 1 ? 0 : st + 1;
+        load(u + 3, st >= 2 ? st - 2 : st + 3);
+    };
+    // what S (0) or dP (1) of a unit start from, four of its queries at a time
+    auto start = [&](int which, int stage, int g, f32x16 &x) {
+        const float4 v = *(const float4 *)&rows[stage][which][8 * g + 4 * fh];
+        x[4 * g] = v.x; x[4 * g + 1] = v.y; x[4 * g + 2] = v.z; x[4 * g + 3] = v.w;
+    };
+    // this slice's keys (part 1) or values (2)
+    uint4 own[KS];
+    const bool second = wave >= 4;
+    {
+        const uint16_t *p = base + (second ? 2 : 1) * d + (size_t)(key < seq ? key : 0) * ld + 8 * fh;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int first = t * kTile + 32 * h;
-            if (first < w0) continue;                           // queries that see none of the wavefront's keys
-            f32x16 S = {}, dP = {};
+        for (int i = 0; i < KS; ++i) own[i] = key < seq ? *(const uint4 *)(p + 16 * i) : uint4{0, 0, 0, 0};
+    }
+    f32x16 acc[CT] = {}, X[2];                                  // X: S, then P; or dP
+    uint4 row[R], col[CT], w[2];
+    auto store = [&](int part, float scale) {
+        if (key >= seq) return;
+        uint16_t *to = dqkv + ((size_t)s * seq + key) * ld + part * d + head * DH + 4 * fh;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) S = mfma32<DT>(read.by_row(qt, h, i), kf[i], S);
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int i = 0; i < KS; ++i) dP = mfma32<DT>(read.by_row(ot, h, i), vf[i], dP);
-            uint4 ps[2], ds[2];
-            uint32_t *pw = &ps[0].x, *dw = &ds[0].x;
+            for (int i = 0; i < 16; i += 4)
+                if (32 * c + 2 * i < DH)
+                    *(uint2 *)(to + 32 * c + 2 * i) = uint2{pack2<DT>(acc[c][i] * scale, acc[c][i + 1] * scale), pack2<DT>(acc[c][i + 2] * scale, acc[c][i + 3] * scale)};
+    };
+    using H0 = std::integral_constant<int, 0>;
+    using H1 = std::integral_constant<int, 1>;
+    load(u0, 0);
+    load(u0 + 1, 1);
+    load(u0 + 2, 2);
+    int u = u0;
+    for (; u < u_first && u <= n_units; ++u) sync(u);           // for the other wavefronts
+    if (u_first >= n_units) {
+        for (; u <= n_units; ++u) sync(u);
+        return;
+    }
+    sync(u);
+    if (!second) {
+        const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
+        auto products = [&](int stage, f32x16 &x, auto &&between) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 ls = *(const float4 *)&rows[t & 1][0][32 * h + 8 * g + 4 * fh], dl = *(const float4 *)&rows[t & 1][1][32 * h + 8 * g + 4 * fh];
-                const float lr[4] = {ls.x, ls.y, ls.z, ls.w}, dr[4] = {dl.x, dl.y, dl.z, dl.w};
-                float p[4], v[4];
+            for (int i = 0; i < R; ++i) row[i] = read.by_row(qs[stage], i);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[4 * g + j], sc, (float)kShift - lr[j]));
-                    if (first == w0 && 8 * g + 4 * fh + j < fr) p[j] = 0.0f;
-                    v[j] = p[j] * (DT == kFP16 ? (dP[4 * g + j] - dr[j]) * factor : dP[4 * g + j] - dr[j]);
-                }
+            for (int g = 0; g < 4; ++g) start(0, stage, g, x);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    pw[2 * g + j] = pack2<DT>(p[2 * j], p[2 * j + 1]);
-                    dw[2 * g + j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
-                }
+            for (int i = 0; i < KS; ++i) {
+                between(i);
+                __builtin_amdgcn_sched_barrier(0);
+                x = mfma32<DT>(row[i % R], own[i], x);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i + R < KS) row[i % R] = read.by_row(qs[stage], i + R);
             }
+        };
+        // P and dV of unit u, S of unit u + 1 (of the last unit's successor too, from whatever lies there: nothing reads it)
+        auto step = [&](auto hc) {
+            constexpr int H = decltype(hc)::value;
+            f32x16 &x = X[H];
+            const u32x4 *ot = os[st];
+            __builtin_amdgcn_sched_barrier(0);
+            products(st_next, X[H ^ 1], [&](int i) {
+                if (i < CT) col[i] = read.by_column(ot, 0, i);
+#pragma unroll
+                for (int j = 8 * i / KS; j < 8 * (i + 1) / KS; ++j) {
+                    auto exponent = [&](float v) { return DT == kFP16 ? __builtin_fmaf(v, sc, (float)kShift) : v * sc; };
+                    put(w, j, pack2<DT>(__builtin_amdgcn_exp2f(exponent(x[2 * j])), __builtin_amdgcn_exp2f(exponent(x[2 * j + 1]))));
+                }
+            });
+#pragma unroll
+            for (int k = 0; k < 2; ++k) mail[H][slice][k][lane] = __builtin_bit_cast(u32x4, w[k]);
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int c = 0; c < CT; ++c) {
-                    dv[c] = mfma32<DT>(read.by_column(ot, 32 * h + 16 * k, c), ps[k], dv[c]);
-                    dk[c] = mfma32<DT>(read.by_column(qt, 32 * h + 16 * k, c), ds[k], dk[c]);
+                    acc[c] = mfma32<DT>(col[c], w[k], acc[c]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (k == 0) col[c] = read.by_column(ot, 16, c);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+        };
+        products(st, X[0], [](int) {});
+#pragma unroll
+        for (int i = 0; i < 16; ++i)                            // the unit on the diagonal: queries that do not see the key
+            if (8 * (i >> 2) + 4 * fh + (i & 3) < fr) X[0][i] = -INFINITY;
+        for (; u + 1 < n_units; u += 2) {
+            step(H0{});
+            sync(u + 1);
+            step(H1{});
+            sync(u + 2);
         }
-    }
-    if (key >= seq) return;
-    const float k_scale = (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f) / __builtin_sqrtf((float)DH), v_scale = DT == kFP16 ? 0x1p-14f : 1.0f;
-    uint16_t *to = dqkv + ((size_t)s * seq + key) * ld + d + head * DH + 4 * fh;
+        if (u < n_units) {
+            step(H0{});
+            sync(u + 1);
+        }
+        store(2, DT == kFP16 ? 0x1p-14f : 1.0f);
+    } else {
+        const int row_tiles = (seq + kRows - 1) / kRows;
+        const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) : 0;
+        const float factor = DT == kFP16 ? ldexpf(1.0f, e - kShift) : 1.0f;
+        auto products = [&](f32x16 &x, auto &&between) {        // dP of unit u
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
+            for (int i = 0; i < R; ++i) row[i] = read.by_row(os[st], i);
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-            if (32 * c + 2 * i < DH) {
-                auto four = [&](const f32x16 &a, float f) { return uint2{pack2<DT>(a[i] * f, a[i + 1] * f), pack2<DT>(a[i + 2] * f, a[i + 3] * f)}; };
-                *(uint2 *)(to + 32 * c + 2 * i) = four(dk[c], k_scale);
-                *(uint2 *)(to + d + 32 * c + 2 * i) = four(dv[c], v_scale);
+            for (int g = 0; g < 4; ++g) start(1, st, g, x);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                between(i);
+                __builtin_amdgcn_sched_barrier(0);
+                x = mfma32<DT>(row[i % R], own[i], x);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i + R < KS) row[i % R] = read.by_row(os[st], i + R);
             }
+        };
+        // dS of unit u - 1, eight 32-bit words, from its dP in x and the first wavefront's P
+        uint4 ps[2];
+        auto collect = [&](auto hc) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) ps[k] = __builtin_bit_cast(uint4, mail[decltype(hc)::value][slice][k][lane]);
+        };
+        auto centred = [&](const f32x16 &x, int j) {
+            const uint4 &f = ps[j >> 2];
+            const uint32_t p = (j & 3) == 0 ? f.x : (j & 3) == 1 ? f.y : (j & 3) == 2 ? f.z : f.w;
+            auto scaled = [&](float v) { return DT == kFP16 ? v * factor : v; };
+            put(w, j, pack2<DT>(Prec<DT>::a2acc((uint16_t)(p & 0xffff)) * scaled(x[2 * j]), Prec<DT>::a2acc((uint16_t)(p >> 16)) * scaled(x[2 * j + 1])));
+        };
+        auto second_products = [&] {                            // dK of unit u - 1
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    acc[c] = mfma32<DT>(col[c], w[k], acc[c]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (k == 0) col[c] = read.by_column(qs[st_last], 16, c);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        };
+        // H: the parity, by the wavefront's count, of the unit before
+        auto step = [&](auto hc) {
+            constexpr int H = decltype(hc)::value;
+            collect(hc);
+            __builtin_amdgcn_sched_barrier(0);
+            products(X[H ^ 1], [&](int i) {
+                if (i < CT) col[i] = read.by_column(qs[st_last], 0, i);
+#pragma unroll
+                for (int j = 8 * i / KS; j < 8 * (i + 1) / KS; ++j) centred(X[H], j);
+            });
+            second_products();
+        };
+        auto last = [&](auto hc) {
+            collect(hc);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) col[c] = read.by_column(qs[st_last], 0, c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) centred(X[decltype(hc)::value], j);
+            second_products();
+        };
+        products(X[0], [](int) {});
+        for (++u; u + 1 < n_units; u += 2) {
+            sync(u);
+            step(H0{});
+            sync(u + 1);
+            step(H1{});
+        }
+        if (u < n_units) {
+            sync(u);
+            step(H0{});
+            sync(u + 1);
+            last(H1{});
+        } else {
+            sync(u);
+            last(H0{});
+        }
+        store(1, (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f) / __builtin_sqrtf((float)DH));
+    }
 }
 
 template <int DT, int DH>
 hipError_t attn_grad(const uint16_t *qkv, const uint16_t *out, const uint16_t *dout, uint16_t *dqkv, char *ws, int n_seq, int seq, int n_heads, hipStream_t s)
 {
-    const int pairs = n_seq * n_heads, row_tiles = (seq + kTile - 1) / kTile, tiles = (seq + kOwn - 1) / kOwn;
+    const int pairs = n_seq * n_heads, row_tiles = (seq + kRows - 1) / kRows, tiles = (seq + kOwn - 1) / kOwn;
     float *delta = (float *)ws, *lse = delta + (size_t)pairs * seq;
     RowTops *tops = (RowTops *)(lse + (size_t)pairs * seq);
-    attn_grad_rows_kernel<DT, DH><<<dim3(pairs * row_tiles), dim3(256), 0, s>>>(qkv, out, dout, delta, tops, seq, n_heads, row_tiles);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
+    hipError_t err = hipSuccess;
+    if constexpr (DT == kFP16) {
+        attn_grad_tops_kernel<DH><<<dim3(pairs * row_tiles), dim3(256), 0, s>>>(qkv, dout, tops, seq, n_heads, row_tiles);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
     const dim3 grid((pairs + 7) / 8 * 8 * tiles);
-    attn_grad_queries_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
+    attn_grad_queries_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, out, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
     if ((err = hipGetLastError()) != hipSuccess) return err;
-    attn_grad_keys_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
+    attn_grad_keys_kernel<DT, DH><<<grid, dim3(512), 0, s>>>(qkv, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
     return hipGetLastError();
 }
 
@@ -546,7 +770,7 @@ bool on_matrix_cores(int dtype, int d_head) { return dtype != kFP32 && (d_head =
 
 size_t attention_grad_scratch(int dtype, int n_seq, int seq, int n_heads, int d_head)
 {
-    const size_t pairs = (size_t)n_seq * n_heads, row_tiles = ((size_t)seq + kTile - 1) / kTile;
+    const size_t pairs = (size_t)n_seq * n_heads, row_tiles = ((size_t)seq + kRows - 1) / kRows;
     // a launch's size is counted in threads, by 32 bits, and in workgroups of the second dimension by 16
     if (on_matrix_cores(dtype, d_head)) {
         if ((pairs + 7) / 8 * 8 * row_tiles >= (size_t)1 << 24) return 0;
