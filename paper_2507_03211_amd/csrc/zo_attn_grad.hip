@@ -25,6 +25,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 namespace {
 
@@ -49,8 +50,7 @@ __device__ __forceinline__ void swap_halves(float x, float &a, float &b)
     b = __uint_as_float(r[1]);
 }
 
-constexpr int kOwn = 128, kUnit = 32;      // rows of a workgroup's own (32 a wavefront), rows of a tile that streams through LDS
-constexpr int kRows = 64;                  // rows of a workgroup of the first launch
+constexpr int kOwn = 128, kTile = 64;      // rows of a workgroup's own (32 a wavefront), rows of a tile that streams through LDS
 
 // fp16: dS = P (dP - D) may lie anywhere: |dP| and |D| are at most A B, with A the largest norm of a row of dO and B of a row of V in the
 // sequence and head, so 2^e dS with 2^e = 2^14 / (2 A B) rounded down is within the type whatever P is, and numbers 2^28 below that bound are still
@@ -73,14 +73,14 @@ template <int DH>
 __global__ __launch_bounds__(256) void attn_grad_tops_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, RowTops *__restrict__ tops, int seq,
                                                              int n_heads, int tiles)
 {
-    constexpr int PIECES = DH / 8, LANES = PIECES <= 8 ? 8 : 16, ROWS = 256 / LANES, TURNS = kRows / ROWS;
+    constexpr int PIECES = DH / 8, LANES = PIECES <= 8 ? 8 : 16, ROWS = 256 / LANES, TURNS = kTile / ROWS;
     __shared__ float top[2][4];
     const int tile = (int)blockIdx.x % tiles, pair = (int)blockIdx.x / tiles, s = pair / n_heads, head = pair % n_heads, d = n_heads * DH;
     const int piece = threadIdx.x % LANES;
     uint4 x[TURNS][2];                                          // all under way together
 #pragma unroll
     for (int i = 0; i < TURNS; ++i) {
-        const int r = tile * kRows + i * ROWS + (int)threadIdx.x / LANES;
+        const int r = tile * kTile + i * ROWS + (int)threadIdx.x / LANES;
         const bool live = r < seq && piece < PIECES;
         const size_t row = (size_t)s * seq + (r < seq ? r : 0), at = row * d + head * DH + (piece < PIECES ? 8 * piece : 0);
         x[i][0] = live ? *(const uint4 *)(dout + at) : uint4{0, 0, 0, 0};
@@ -115,12 +115,12 @@ __global__ __launch_bounds__(256) void attn_grad_tops_kernel(const uint16_t *__r
     }
 }
 
-// Tiles of 32 rows in LDS, [row][piece of 16 bytes]: read by rows (32 rows, one piece: an operand with its contraction over the channels) and, by the
+// Tiles of 64 rows in LDS, [row][piece of 16 bytes]: read by rows (32 rows, one piece: an operand with its contraction over the channels) and, by the
 // transposing read, by columns (4 rows x 32 bytes per 16 lanes: one with its contraction over the rows).  Pieces are XOR-swizzled by the row so that
 // both are free of bank conflicts: 16 rows of one piece lie on 16 distinct 16-byte places of the 256-byte bank line, four rows on its
 // four quarters.  Rows are padded to 192 or 256 bytes (80 and 112 channels); what lies there is a piece over again, for channels that are not stored.
 template <int DH> struct TileShape {
-    static constexpr int CHD = DH / 8, CH = DH == 64 ? 8 : DH <= 96 ? 12 : 16, KS = DH / 16, CT = (DH + 31) / 32, PIECES = kUnit * CH;
+    static constexpr int CHD = DH / 8, CH = DH == 64 ? 8 : DH <= 96 ? 12 : 16, KS = DH / 16, CT = (DH + 31) / 32, PIECES = kTile * CH;
     static __device__ __forceinline__ int swizzle(int r) { return CH == 16 ? (r & 3) << 2 | ((r >> 2) & 3) : CH == 12 ? (r >> 2) & 3 : ((r >> 1) & 1) << 2 | ((r >> 2) & 3); }
     static constexpr int in_row(int piece) { return piece < CHD ? piece : piece - 2; }
 };
@@ -142,7 +142,7 @@ template <int DH> struct TileReader : TileShape<DH> {
         }
     }
     static __device__ __forceinline__ uint32_t address(const u32x4 *tile) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const u32x4 *)tile; }
-    // rows lane % 32, channels of k-step s
+    // rows lane % 32, channels of k-step s; `tile`: the first row
     __device__ __forceinline__ uint4 by_row(const u32x4 *tile, int s) const
     {
         const uint32_t at = kXor ? (address(tile) + row[0]) ^ (uint32_t)(32 * s) : address(tile) + row[s % (kXor ? 1 : 2)] + (s / 2) * 64;
@@ -161,7 +161,7 @@ template <int DH> struct TileReader : TileShape<DH> {
         return uint4{lo.x, lo.y, hi.x, hi.y};
     }
 };
-// 32 rows of a matrix, straight into LDS; rows past the end of the sequence come as zeros (the buffer ends there).
+// 64 rows of a matrix, straight into LDS; rows past the end of the sequence come as zeros (the buffer ends there).
 __device__ __forceinline__ void dma16(u32x4 rows, uint32_t lane_off, uint32_t lds_off)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(lane_off), "s"(rows), "s"(lds_off) : "memory", "m0");
@@ -175,10 +175,9 @@ __device__ __forceinline__ u32x4 buffer_of(uint64_t first, uint32_t bytes)
     return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(first >> 32)),
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
-// Every wavefront of the workgroup's WAVES has LOADS loads: where a tile's do not deal out evenly, some come twice.
-template <int DH, int WAVES> struct TileLoader : TileShape<DH> {
+template <int DH> struct TileLoader : TileShape<DH> {
     using T = TileShape<DH>;
-    static constexpr int ALL = T::PIECES / 64, LOADS = (ALL + WAVES - 1) / WAVES;
+    static constexpr int LOADS = T::PIECES / 256;               // of a wavefront
     uint32_t off[LOADS];
     uint32_t ld;
     int wave;
@@ -186,19 +185,18 @@ template <int DH, int WAVES> struct TileLoader : TileShape<DH> {
     {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int p = 64 * number(i) + lane, r = p / T::CH;
+            const int p = 64 * (LOADS * wave + i) + lane, r = p / T::CH;
             off[i] = (uint32_t)r * ld + (uint32_t)T::in_row((p % T::CH) ^ T::swizzle(r)) * 16u;
         }
     }
-    __device__ __forceinline__ int number(int i) const { return ALL % WAVES == 0 ? WAVES * i + wave : (WAVES * i + wave) % ALL; }
     // `first`: the sequence's first row, this head's first channel
     __device__ __forceinline__ void load(u32x4 *tile, const uint16_t *first, int row0, int seq) const
     {
-        const int left = seq - row0 < kUnit ? seq - row0 : kUnit;
+        const int left = seq - row0 < kTile ? seq - row0 : kTile;
         const u32x4 rows = buffer_of((uint64_t)(uintptr_t)first + (uint64_t)row0 * ld, (uint32_t)(left - 1) * ld + DH * 2);
         const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4 *)tile;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) dma16(rows, off[i], lds + (uint32_t)number(i) * 1024u);
+        for (int i = 0; i < LOADS; ++i) dma16(rows, off[i], lds + (uint32_t)(LOADS * wave + i) * 1024u);
     }
 };
 
@@ -213,21 +211,10 @@ __device__ __forceinline__ Item item_of(int block, int pairs)
 }
 
 // Both launches work their rows in units of 32 against 32, software-pipelined, since the one or two wavefronts of a SIMD leave little else to
-// hide an instruction's wait behind.  Step u, with S of unit u there:
-//     dP of unit u                  |  P of unit u
-//     S of unit u + 1               |  dS of unit u
-//     the second products of unit u |  what the next products start from
-// Row fragments run through rings that are refilled as they drain, column fragments are read ahead; the sched_barriers pin the order written
-// here.  LDS answers a wavefront in order, so that what is needed soon must not be asked for behind what is not: minus logsumexp and minus D, which
-// S and dP start from, are read into their registers while these have nothing else to hold.  Four stages of tiles in LDS, a tile a unit, one barrier a
-// step: behind it tiles up to u + 1 have landed for everybody, u + 2 may be under way, and u + 3 goes out into the stage that everybody has left.
-constexpr int kStages = 4;
-// until all but a wavefront's last N loads have landed, or all
-template <int N> __device__ __forceinline__ void wait_loads(bool all)
-{
-    if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
+// hide an instruction's wait behind: between two multiplies stand a share of the vector arithmetic of a unit whose products are there and the
+// LDS reads of fragments some multiplies ahead (the sched_barriers pin that order).  LDS answers a wavefront in order, so that what is needed soon must
+// not be asked for behind what is not: minus logsumexp and minus D, which S and dP start from, are read a unit ahead, straight into their registers.
+// A barrier for every two units (for each: queries and keys of 4 x 2048, 40 heads of 128 318 and 452 us, without any 260 and 395).
 __device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // word i of two fragments
 {
     uint4 &f = w[i >> 2];
@@ -247,7 +234,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     constexpr int KS = T::KS, CT = T::CT, R = 2;
     // the reference is raised when a scaled score passes it by this much: unnormalised probabilities are 2^kRaise at most
     constexpr int kRaise = 4;
-    __shared__ __attribute__((aligned(256))) u32x4 ks[kStages][T::PIECES], vs[kStages][T::PIECES];
+    // keys of tiles T and T + 1 and values of T are read while T + 2's and T + 1's arrive
+    __shared__ __attribute__((aligned(256))) u32x4 ks[3][T::PIECES], vs[2][T::PIECES];
     const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
     const int s = item.pair / n_heads, head = item.pair % n_heads, d = n_heads * DH, ld = 3 * d;
@@ -255,7 +243,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     const int q0 = (tiles - 1 - item.tile) * kOwn, w0 = q0 + 32 * wave, q = w0 + fr;          // the longest first
     const uint16_t *base = qkv + (size_t)s * seq * ld + head * DH;
     const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
-    const int row_tiles = (seq + kRows - 1) / kRows;
+    const int row_tiles = (seq + kTile - 1) / kTile;
     const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) - kRaise : 0;
     const float factor = DT == kFP16 ? ldexpf(1.0f, e) : 1.0f;
 
@@ -283,21 +271,23 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
         if (fh == 0 && q < seq) delta[(size_t)item.pair * seq + q] = minus_d;
     }
     const TileReader<DH> read(lane);
-    const TileLoader<DH, 4> loader(ld, lane, wave);
-    const int last = q0 + kOwn <= seq ? q0 + kOwn : seq, n_units = (last + kUnit - 1) / kUnit, u_last = w0 / 32 < n_units ? w0 / 32 : n_units - 1;
-    auto load = [&](int u) {
-        if (u >= n_units) return;
-        loader.load(ks[u % kStages], base + d, u * kUnit, seq);
-        loader.load(vs[u % kStages], base + 2 * d, u * kUnit, seq);
-    };
+    const TileLoader<DH> loader(ld, lane, wave);
+    const int last = q0 + kOwn <= seq ? q0 + kOwn : seq, n_tiles = (last + kTile - 1) / kTile, u_last = w0 / 32 < 2 * n_tiles ? w0 / 32 : 2 * n_tiles - 1;
+    auto load_k = [&](int t, int stage) { if (t < n_tiles) loader.load(ks[stage], base + d, t * kTile, seq); };
+    auto load_v = [&](int t) { if (t < n_tiles) loader.load(vs[t & 1], base + 2 * d, t * kTile, seq); };
     f32x16 acc[CT] = {}, S[2], dP;
     uint4 kr[R], vr[R], kc[CT], ds[2];
     float m_run = -INFINITY, moff = 0.0f, thr = -INFINITY, l_lane = 0.0f, top = -INFINITY;
-    auto k_row = [&](int u, int i) { kr[i % R] = read.by_row(ks[u % kStages], i); };
-    auto v_row = [&](int u, int i) { vr[i % R] = read.by_row(vs[u % kStages], i); };
-    auto start = [&] {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) dP[j] = minus_d;
+    // stages of tile T's keys and T + 1's and T + 2's
+    int tile = -1, st0 = 2, st1 = 0, st2 = 1;
+    auto sync = [&] {                                           // on to the next tile
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        ++tile;
+        const int left = st0;
+        st0 = st1; st1 = st2; st2 = left;
+        load_k(tile + 2, st2);
+        load_v(tile + 1);
     };
     auto mask = [&](f32x16 &x) {                                // of the unit on the diagonal
 #pragma unroll
@@ -310,15 +300,19 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
         for (int i = 3; i < 15; i += 2) t = __builtin_fmaxf(__builtin_fmaxf(x[i], x[i + 1]), t);
         return __builtin_fmaxf(t, x[15]);
     };
-    auto sync = [&](int u) {
-        wait_loads<2 * TileLoader<DH, 4>::LOADS>(u + 2 >= n_units);
-        __syncthreads();
-        load(u + 3);
+    auto start = [&] {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) dP[j] = minus_d;
     };
+    // Step u, with S of unit u there:  dP of unit u | P of unit u;  S of unit u + 1 | dS of unit u;  dQ's products of unit u | the maximum of S
     auto step = [&](auto hc, int u) {
-        constexpr int H = decltype(hc)::value;                  // u & 1
+        constexpr int H = decltype(hc)::value;                  // u & 1: unit u is half H of its tile
         f32x16 &Sc = S[H], &Sn = S[H ^ 1];
-        const u32x4 *kt = ks[u % kStages];
+        const u32x4 *kt = ks[st0] + H * 32 * T::CH, *vt = vs[tile & 1] + H * 32 * T::CH, *kn = H ? ks[st1] : ks[st0] + 32 * T::CH;
+        if constexpr (H == 0) {                                 // (the other half's were read a unit ago)
+#pragma unroll
+            for (int i = 0; i < R; ++i) vr[i] = read.by_row(vt, i);
+        }
         if (__builtin_amdgcn_ballot_w64(top > thr) != 0) {
             float a, b;
             swap_halves(top, a, b);
@@ -335,10 +329,6 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
-            dP = mfma32<DT>(vr[i % R], of[i], dP);
-            __builtin_amdgcn_sched_barrier(0);
-            if (i + R < KS) v_row(u, i + R);
-            if (i + R >= KS) k_row(u + 1, i + R - KS);          // (the last unit's successor is multiplied too, from whatever lies there: nothing reads it)
 #pragma unroll
             for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) {
                 Sc[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sc[j], sc, moff));
@@ -346,13 +336,18 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
             }
             asm volatile("" : "+v"(l_lane));
             __builtin_amdgcn_sched_barrier(0);
+            dP = mfma32<DT>(vr[i % R], of[i], dP);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + R < KS) vr[i % R] = read.by_row(vt, i + R);
+            // (the last unit's successor is multiplied too, from whatever lies there: nothing reads it)
+            if (i + R >= KS) kr[i + R - KS] = read.by_row(kn, i + R - KS);
         }
         const f32x16 zero = {};
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             Sn = mfma32<DT>(kr[i % R], qf[i], i == 0 ? zero : Sn);
             __builtin_amdgcn_sched_barrier(0);
-            if (i + R < KS) k_row(u + 1, i + R);
+            if (i + R < KS) kr[i % R] = read.by_row(kn, i + R);
             if (i < CT) kc[i] = read.by_column(kt, 0, i);
 #pragma unroll
             for (int j = 8 * i / KS; j < 8 * (i + 1) / KS; ++j) {
@@ -368,45 +363,38 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
             for (int c = 0; c < CT; ++c) {
                 acc[c] = mfma32<DT>(kc[c], ds[k], acc[c]);
                 __builtin_amdgcn_sched_barrier(0);
-                if (k == 0) {
-                    kc[c] = read.by_column(kt, 16, c);
-                } else {
+                if (k == 0) kc[c] = read.by_column(kt, 16, c);
+                if constexpr (H == 0) {
+                    if (k == 1) {
 #pragma unroll
-                    for (int i = R * c / CT; i < R * (c + 1) / CT; ++i) v_row(u + 1, i);
+                        for (int i = R * c / CT; i < R * (c + 1) / CT; ++i) vr[i] = read.by_row(vt + 32 * T::CH, i);
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         if (u + 1 == u_last) mask(Sn);
         top = maximum(Sn);
     };
-    load(0);
-    load(1);
-    load(2);
-    sync(0);
+    load_k(0, 0);
+    load_v(0);
+    load_k(1, 1);
+    sync();
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
         const f32x16 zero = {};
-        k_row(0, i);
-        S[0] = mfma32<DT>(kr[i % R], qf[i], i == 0 ? zero : S[0]);
+        S[0] = mfma32<DT>(read.by_row(ks[0], i), qf[i], i == 0 ? zero : S[0]);
     }
-#pragma unroll
-    for (int i = 0; i < R; ++i) v_row(0, i);
     start();
     if (u_last == 0) mask(S[0]);
     top = maximum(S[0]);
     int u = 0;
     for (; u < u_last; u += 2) {
         step(std::integral_constant<int, 0>{}, u);
-        sync(u + 1);
         step(std::integral_constant<int, 1>{}, u + 1);
-        if (u + 2 < n_units) sync(u + 2);
+        if (tile + 1 < n_tiles) sync();
     }
-    if (u == u_last) {
-        step(std::integral_constant<int, 0>{}, u);
-        ++u;
-        if (u < n_units) sync(u);
-    }
-    for (++u; u < n_units; ++u) sync(u);                        // for the other wavefronts
+    if (u == u_last) step(std::integral_constant<int, 0>{}, u);
+    while (tile + 1 < n_tiles) sync();                          // for the other wavefronts
     if (q >= seq) return;
     float a, b;
     swap_halves(l_lane, a, b);
@@ -424,228 +412,174 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 }
 
 // ------------------------------------------------------------------ keys
-// Eight wavefronts, two to a slice of 32 keys, on one SIMD: the first has S, P and dV, the second dP, dS and dK.  A wavefront with all of it would hold
-// 128 accumulators and 64 registers of keys and values at 128 channels and have its SIMD to itself.  P passes from the first to the second
-// through LDS, as the 16-bit numbers that dV's product takes, a step later; the second works a unit behind.  Five stages: it still reads u - 1.
-constexpr int kKeyStages = 5;
 template <int DT, int DH>
-__global__ __launch_bounds__(512, 2) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
+__global__ __launch_bounds__(256, DH <= 96 ? 2 : 1) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
                                                                 const float *__restrict__ delta, const float *__restrict__ lse, const RowTops *__restrict__ tops,
                                                                 int seq, int n_heads, int pairs, int tiles)
 {
     using T = TileShape<DH>;
-    constexpr int KS = T::KS, CT = T::CT, R = KS < 4 ? KS : 4;
+    constexpr int KS = T::KS, CT = T::CT, R = DH == 80 || DH == 96 ? 2 : 4;
     constexpr int kShift = DT == kFP16 ? 14 : 0;               // probabilities carry 2^kShift: down to 2^-28 they are normal numbers
-    __shared__ __attribute__((aligned(256))) u32x4 qs[kKeyStages][T::PIECES], os[kKeyStages][T::PIECES];
-    __shared__ u32x4 mail[2][4][2][64];                         // P of units of either parity, by slice
-    __shared__ float rows[kKeyStages][2][64];                   // minus logsumexp and minus D of a tile's queries, zeros behind them
+    __shared__ __attribute__((aligned(256))) u32x4 qs[3][T::PIECES], os[3][T::PIECES];
+    __shared__ float rows[3][2][kTile];                   // logsumexp and D of a tile's queries
     const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
     const int s = item.pair / n_heads, head = item.pair % n_heads, d = n_heads * DH, ld = 3 * d;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slice = wave & 3, fr = lane & 31, fh = lane >> 5;
-    const int k0 = item.tile * kOwn, w0 = k0 + 32 * slice, key = w0 + fr;                     // the longest first
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 31, fh = lane >> 5;
+    const int k0 = item.tile * kOwn, w0 = k0 + 32 * wave, key = w0 + fr;                      // the longest first
     const uint16_t *base = qkv + (size_t)s * seq * ld + head * DH, *obase = dout + (size_t)s * seq * d + head * DH;
-    const TileReader<DH> read(lane);
-    const TileLoader<DH, 8> load_q(ld, lane, wave), load_o(d, lane, wave);
-    const int u0 = k0 / kUnit, n_units = (seq + kUnit - 1) / kUnit, u_first = w0 / kUnit;
-    auto load = [&](int u, int stage) {
-        if (u >= n_units) return;
-        load_q.load(qs[stage], base, u * kUnit, seq);
-        load_o.load(os[stage], obase, u * kUnit, seq);
-        // every wavefront one of the two (queries past the end get zeros: their dO is, too)
-        const int left = seq - u * kUnit < kUnit ? seq - u * kUnit : kUnit, which = wave & 1;
-        const float *from = (which ? delta : lse) + (size_t)item.pair * seq + u * kUnit;
-        dma4(buffer_of((uint64_t)(uintptr_t)from, (uint32_t)left * 4), 4 * lane, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&rows[stage][which][0]);
-    };
-    // stages of units u - 1, u, u + 1
-    int st_last = 3, st = 4, st_next = 0;
-    auto sync = [&](int u) {
-        wait_loads<2 * TileLoader<DH, 8>::LOADS + 1>(u + 2 >= n_units);
-        __syncthreads();
-        st_last = st;
-        st = st_next;
-        st_next = st == kKeyStages - 1 ? 0 : st + 1;
-        load(u + 3, st >= 2 ? st - 2 : st + 3);
-    };
-    // what S (0) or dP (1) of a unit start from, four of its queries at a time
-    auto start = [&](int which, int stage, int g, f32x16 &x) {
-        const float4 v = *(const float4 *)&rows[stage][which][8 * g + 4 * fh];
-        x[4 * g] = v.x; x[4 * g + 1] = v.y; x[4 * g + 2] = v.z; x[4 * g + 3] = v.w;
-    };
-    // this slice's keys (part 1) or values (2)
-    uint4 own[KS];
-    const bool second = wave >= 4;
+    const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
+    const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * ((seq + kTile - 1) / kTile), (seq + kTile - 1) / kTile) : 0;
+    const float factor = DT == kFP16 ? ldexpf(1.0f, e - kShift) : 1.0f;
+    uint4 kf[KS], vf[KS];
     {
-        const uint16_t *p = base + (second ? 2 : 1) * d + (size_t)(key < seq ? key : 0) * ld + 8 * fh;
+        const uint16_t *kp = base + d + (size_t)(key < seq ? key : 0) * ld + 8 * fh;
 #pragma unroll
-        for (int i = 0; i < KS; ++i) own[i] = key < seq ? *(const uint4 *)(p + 16 * i) : uint4{0, 0, 0, 0};
+        for (int i = 0; i < KS; ++i) {
+            kf[i] = key < seq ? *(const uint4 *)(kp + 16 * i) : uint4{0, 0, 0, 0};
+            vf[i] = key < seq ? *(const uint4 *)(kp + d + 16 * i) : uint4{0, 0, 0, 0};
+        }
     }
-    f32x16 acc[CT] = {}, X[2];                                  // X: S, then P; or dP
-    uint4 row[R], col[CT], w[2];
-    auto store = [&](int part, float scale) {
-        if (key >= seq) return;
-        uint16_t *to = dqkv + ((size_t)s * seq + key) * ld + part * d + head * DH + 4 * fh;
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                if (32 * c + 2 * i < DH)
-                    *(uint2 *)(to + 32 * c + 2 * i) = uint2{pack2<DT>(acc[c][i] * scale, acc[c][i + 1] * scale), pack2<DT>(acc[c][i + 2] * scale, acc[c][i + 3] * scale)};
+    const TileReader<DH> read(lane);
+    const TileLoader<DH> load_q(ld, lane, wave), load_o(d, lane, wave);
+    const int t0 = k0 / kTile, n_tiles = (seq + kTile - 1) / kTile, n_units = (seq + 31) / 32, u_first = w0 / 32;
+    auto load = [&](int t, int stage) {
+        if (t >= n_tiles) return;
+        load_q.load(qs[stage], base, t * kTile, seq);
+        load_o.load(os[stage], obase, t * kTile, seq);
+        if (wave < 2) {                                          // (queries past the end get zeros: their dO is, too)
+            const int left = seq - t * kTile < kTile ? seq - t * kTile : kTile;
+            const float *from = (wave ? delta : lse) + (size_t)item.pair * seq + t * kTile;
+            dma4(buffer_of((uint64_t)(uintptr_t)from, (uint32_t)left * 4), 4 * lane, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&rows[stage][wave][0]);
+        }
     };
-    using H0 = std::integral_constant<int, 0>;
-    using H1 = std::integral_constant<int, 1>;
-    load(u0, 0);
-    load(u0 + 1, 1);
-    load(u0 + 2, 2);
-    int u = u0;
-    for (; u < u_first && u <= n_units; ++u) sync(u);           // for the other wavefronts
-    if (u_first >= n_units) {
-        for (; u <= n_units; ++u) sync(u);
-        return;
-    }
-    sync(u);
-    if (!second) {
-        const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
-        auto products = [&](int stage, f32x16 &x, auto &&between) {
-#pragma unroll
-            for (int i = 0; i < R; ++i) row[i] = read.by_row(qs[stage], i);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) start(0, stage, g, x);
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                between(i);
-                __builtin_amdgcn_sched_barrier(0);
-                x = mfma32<DT>(row[i % R], own[i], x);
-                __builtin_amdgcn_sched_barrier(0);
-                if (i + R < KS) row[i % R] = read.by_row(qs[stage], i + R);
-            }
+    f32x16 dk[CT] = {}, dv[CT] = {}, S[2], dP[2];
+    uint4 qr[R], orow[R], qc[CT], oc[CT], ps[2], ds[2];
+    auto ring = [&](const u32x4 *qt, const u32x4 *ot, int i) {
+        qr[i % R] = read.by_row(qt, i);
+        orow[i % R] = read.by_row(ot, i);
+    };
+    auto multiply = [&](int i, f32x16 &Sn, f32x16 &dPn) {
+        Sn = mfma32<DT>(qr[i % R], kf[i], Sn);
+        dPn = mfma32<DT>(orow[i % R], vf[i], dPn);
+    };
+    // what S and dP of a unit start from: minus logsumexp (over the scaling) and minus D of its queries, four rows at a time
+    auto start = [&](const float (&row)[2][kTile], int half, int g, f32x16 &Sn, f32x16 &dPn) {
+        const float4 l = *(const float4 *)&row[0][32 * half + 8 * g + 4 * fh], v = *(const float4 *)&row[1][32 * half + 8 * g + 4 * fh];
+        Sn[4 * g] = l.x; Sn[4 * g + 1] = l.y; Sn[4 * g + 2] = l.z; Sn[4 * g + 3] = l.w;
+        dPn[4 * g] = v.x; dPn[4 * g + 1] = v.y; dPn[4 * g + 2] = v.z; dPn[4 * g + 3] = v.w;
+    };
+    int tile = t0 - 1, st0 = 2, st1 = 0, st2 = 1;               // as above
+    auto sync = [&] {
+        ++tile;
+        const int left = st0;
+        st0 = st1; st1 = st2; st2 = left;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        load(tile + 2, st2);
+    };
+    // H: the wavefront's j-th unit's lowest bit; which half of its tile unit u is goes by the wavefront
+    auto step = [&](auto hc, int u) {
+        constexpr int H = decltype(hc)::value;
+        f32x16 &Sc = S[H], &dPc = dP[H], &Sn = S[H ^ 1], &dPn = dP[H ^ 1];
+        if (tile < u / 2) sync();
+        const int half = u & 1;
+        const u32x4 *qt = qs[st0] + half * 32 * T::CH, *ot = os[st0] + half * 32 * T::CH;
+        const u32x4 *qt1 = half ? qs[st1] : qs[st0] + 32 * T::CH, *ot1 = half ? os[st1] : os[st0] + 32 * T::CH;
+        const u32x4 *qt2 = qs[st1] + half * 32 * T::CH, *ot2 = os[st1] + half * 32 * T::CH;      // unit u + 2
+        auto pair = [&](int i) {                                // elements i and i + 1
+            auto exponent = [&](float v) { return DT == kFP16 ? __builtin_fmaf(v, sc, (float)kShift) : v * sc; };
+            const float p0 = __builtin_amdgcn_exp2f(exponent(Sc[i])), p1 = __builtin_amdgcn_exp2f(exponent(Sc[i + 1]));
+            auto scaled = [&](float v) { return DT == kFP16 ? v * factor : v; };
+            put(ps, i / 2, pack2<DT>(p0, p1));
+            put(ds, i / 2, pack2<DT>(p0 * scaled(dPc[i]), p1 * scaled(dPc[i + 1])));
         };
-        // P and dV of unit u, S of unit u + 1 (of the last unit's successor too, from whatever lies there: nothing reads it)
-        auto step = [&](auto hc) {
-            constexpr int H = decltype(hc)::value;
-            f32x16 &x = X[H];
-            const u32x4 *ot = os[st];
+        // (the last unit's successor is multiplied too, from whatever lies there: nothing reads it)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            multiply(i, Sn, dPn);
             __builtin_amdgcn_sched_barrier(0);
-            products(st_next, X[H ^ 1], [&](int i) {
-                if (i < CT) col[i] = read.by_column(ot, 0, i);
+            if (i + R < KS) ring(qt1, ot1, i + R);
+            if (i < CT) {
+                oc[i] = read.by_column(ot, 0, i);
+                qc[i] = read.by_column(qt, 0, i);
+            }
 #pragma unroll
-                for (int j = 8 * i / KS; j < 8 * (i + 1) / KS; ++j) {
-                    auto exponent = [&](float v) { return DT == kFP16 ? __builtin_fmaf(v, sc, (float)kShift) : v * sc; };
-                    put(w, j, pack2<DT>(__builtin_amdgcn_exp2f(exponent(x[2 * j])), __builtin_amdgcn_exp2f(exponent(x[2 * j + 1]))));
+            for (int p = 4 * i / KS; p < 4 * (i + 1) / KS; ++p) pair(2 * p);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                dv[c] = mfma32<DT>(oc[c], ps[k], dv[c]);
+                dk[c] = mfma32<DT>(qc[c], ds[k], dk[c]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (k == 0) {
+                    oc[c] = read.by_column(ot, 16, c);
+                    qc[c] = read.by_column(qt, 16, c);
+#pragma unroll
+                    for (int p = 4 + 4 * c / CT; p < 4 + 4 * (c + 1) / CT; ++p) pair(2 * p);
+                } else {                                        // what unit u + 2 starts from, and its first fragments
+#pragma unroll
+                    for (int g = 4 * c / CT; g < 4 * (c + 1) / CT; ++g) start(rows[st1], half, g, Sc, dPc);
+#pragma unroll
+                    for (int i = R * c / CT; i < R * (c + 1) / CT; ++i) ring(qt2, ot2, i);
                 }
-            });
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    load(t0, 0);
+    load(t0 + 1, 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    {
+        const int stage = u_first / 2 - t0, half = u_first & 1;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) mail[H][slice][k][lane] = __builtin_bit_cast(u32x4, w[k]);
+        for (int g = 0; g < 4; ++g) start(rows[stage], half, g, S[0], dP[0]);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    acc[c] = mfma32<DT>(col[c], w[k], acc[c]);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (k == 0) col[c] = read.by_column(ot, 16, c);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-        };
-        products(st, X[0], [](int) {});
+        for (int i = 0; i < KS; ++i) {
+            ring(qs[stage] + half * 32 * T::CH, os[stage] + half * 32 * T::CH, i);
+            multiply(i, S[0], dP[0]);
+        }
 #pragma unroll
         for (int i = 0; i < 16; ++i)                            // the unit on the diagonal: queries that do not see the key
-            if (8 * (i >> 2) + 4 * fh + (i & 3) < fr) X[0][i] = -INFINITY;
-        for (; u + 1 < n_units; u += 2) {
-            step(H0{});
-            sync(u + 1);
-            step(H1{});
-            sync(u + 2);
-        }
-        if (u < n_units) {
-            step(H0{});
-            sync(u + 1);
-        }
-        store(2, DT == kFP16 ? 0x1p-14f : 1.0f);
-    } else {
-        const int row_tiles = (seq + kRows - 1) / kRows;
-        const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) : 0;
-        const float factor = DT == kFP16 ? ldexpf(1.0f, e - kShift) : 1.0f;
-        auto products = [&](f32x16 &x, auto &&between) {        // dP of unit u
-#pragma unroll
-            for (int i = 0; i < R; ++i) row[i] = read.by_row(os[st], i);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) start(1, st, g, x);
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                between(i);
-                __builtin_amdgcn_sched_barrier(0);
-                x = mfma32<DT>(row[i % R], own[i], x);
-                __builtin_amdgcn_sched_barrier(0);
-                if (i + R < KS) row[i % R] = read.by_row(os[st], i + R);
-            }
-        };
-        // dS of unit u - 1, eight 32-bit words, from its dP in x and the first wavefront's P
-        uint4 ps[2];
-        auto collect = [&](auto hc) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) ps[k] = __builtin_bit_cast(uint4, mail[decltype(hc)::value][slice][k][lane]);
-        };
-        auto centred = [&](const f32x16 &x, int j) {
-            const uint4 &f = ps[j >> 2];
-            const uint32_t p = (j & 3) == 0 ? f.x : (j & 3) == 1 ? f.y : (j & 3) == 2 ? f.z : f.w;
-            auto scaled = [&](float v) { return DT == kFP16 ? v * factor : v; };
-            put(w, j, pack2<DT>(Prec<DT>::a2acc((uint16_t)(p & 0xffff)) * scaled(x[2 * j]), Prec<DT>::a2acc((uint16_t)(p >> 16)) * scaled(x[2 * j + 1])));
-        };
-        auto second_products = [&] {                            // dK of unit u - 1
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    acc[c] = mfma32<DT>(col[c], w[k], acc[c]);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (k == 0) col[c] = read.by_column(qs[st_last], 16, c);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-        };
-        // H: the parity, by the wavefront's count, of the unit before
-        auto step = [&](auto hc) {
-            constexpr int H = decltype(hc)::value;
-            collect(hc);
-            __builtin_amdgcn_sched_barrier(0);
-            products(X[H ^ 1], [&](int i) {
-                if (i < CT) col[i] = read.by_column(qs[st_last], 0, i);
-#pragma unroll
-                for (int j = 8 * i / KS; j < 8 * (i + 1) / KS; ++j) centred(X[H], j);
-            });
-            second_products();
-        };
-        auto last = [&](auto hc) {
-            collect(hc);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) col[c] = read.by_column(qs[st_last], 0, c);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) centred(X[decltype(hc)::value], j);
-            second_products();
-        };
-        products(X[0], [](int) {});
-        for (++u; u + 1 < n_units; u += 2) {
-            sync(u);
-            step(H0{});
-            sync(u + 1);
-            step(H1{});
-        }
-        if (u < n_units) {
-            sync(u);
-            step(H0{});
-            sync(u + 1);
-            last(H1{});
-        } else {
-            sync(u);
-            last(H0{});
-        }
-        store(1, (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f) / __builtin_sqrtf((float)DH));
+            if (8 * (i >> 2) + 4 * fh + (i & 3) < fr) S[0][i] = -INFINITY;
     }
+    while (tile < u_first / 2 && tile + 1 < n_tiles) sync();
+    {
+        const int stage = u_first & 1 ? st1 : st0, half = (u_first & 1) ^ 1;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) start(rows[stage], half, g, S[1], dP[1]);
+#pragma unroll
+        for (int i = 0; i < R; ++i) ring(qs[stage] + half * 32 * T::CH, os[stage] + half * 32 * T::CH, i);
+    }
+    int u = u_first;
+    for (; u + 1 < n_units; u += 2) {
+        step(std::integral_constant<int, 0>{}, u);
+        step(std::integral_constant<int, 1>{}, u + 1);
+    }
+    if (u < n_units) step(std::integral_constant<int, 0>{}, u);
+    while (tile + 1 < n_tiles) sync();                          // for the other wavefronts
+    if (key >= seq) return;
+    const float k_scale = (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f) / __builtin_sqrtf((float)DH), v_scale = DT == kFP16 ? 0x1p-14f : 1.0f;
+    uint16_t *to = dqkv + ((size_t)s * seq + key) * ld + d + head * DH + 4 * fh;
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            if (32 * c + 2 * i < DH) {
+                auto four = [&](const f32x16 &a, float f) { return uint2{pack2<DT>(a[i] * f, a[i + 1] * f), pack2<DT>(a[i + 2] * f, a[i + 3] * f)}; };
+                *(uint2 *)(to + 32 * c + 2 * i) = four(dk[c], k_scale);
+                *(uint2 *)(to + d + 32 * c + 2 * i) = four(dv[c], v_scale);
+            }
 }
 
 template <int DT, int DH>
 hipError_t attn_grad(const uint16_t *qkv, const uint16_t *out, const uint16_t *dout, uint16_t *dqkv, char *ws, int n_seq, int seq, int n_heads, hipStream_t s)
 {
-    const int pairs = n_seq * n_heads, row_tiles = (seq + kRows - 1) / kRows, tiles = (seq + kOwn - 1) / kOwn;
+    const int pairs = n_seq * n_heads, row_tiles = (seq + kTile - 1) / kTile, tiles = (seq + kOwn - 1) / kOwn;
     float *delta = (float *)ws, *lse = delta + (size_t)pairs * seq;
     RowTops *tops = (RowTops *)(lse + (size_t)pairs * seq);
     hipError_t err = hipSuccess;
@@ -656,7 +590,7 @@ hipError_t attn_grad(const uint16_t *qkv, const uint16_t *out, const uint16_t *d
     const dim3 grid((pairs + 7) / 8 * 8 * tiles);
     attn_grad_queries_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, out, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
     if ((err = hipGetLastError()) != hipSuccess) return err;
-    attn_grad_keys_kernel<DT, DH><<<grid, dim3(512), 0, s>>>(qkv, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
+    attn_grad_keys_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
     return hipGetLastError();
 }
 
@@ -770,7 +704,7 @@ bool on_matrix_cores(int dtype, int d_head) { return dtype != kFP32 && (d_head =
 
 size_t attention_grad_scratch(int dtype, int n_seq, int seq, int n_heads, int d_head)
 {
-    const size_t pairs = (size_t)n_seq * n_heads, row_tiles = ((size_t)seq + kRows - 1) / kRows;
+    const size_t pairs = (size_t)n_seq * n_heads, row_tiles = ((size_t)seq + kTile - 1) / kTile;
     // a launch's size is counted in threads, by 32 bits, and in workgroups of the second dimension by 16
     if (on_matrix_cores(dtype, d_head)) {
         if ((pairs + 7) / 8 * 8 * row_tiles >= (size_t)1 << 24) return 0;
