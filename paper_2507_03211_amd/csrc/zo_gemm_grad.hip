@@ -172,32 +172,9 @@ __global__ __launch_bounds__(256) void head_dx_kernel(const float4 *__restrict__
     }
 }
 
-// ------------------------------------------------------------------ the products' plan
+// ------------------------------------------------------------------ the plan of a call
 using Logits = Product<false, false>;       // x rows, words: both with k inside
 
-// de's words: those of whole rounds of one tile, and what is left in a launch of its own, in tiles of its own, where that is estimated to be
-// faster.  8192 x 768 x 50272: 591 tiles of 256 x 256 are 2.3 rounds on 256 CUs; two rounds and 216 tiles of 192 x 128 take the whole
-// call from 2094 us to 2032.  17 shapes that the rule cuts: 1.018 times as fast on average (0.998 - 1.040), to the same bits.
-constexpr float kCutGain = 0.99f;
-struct Words { Tile tile; int words; Tile rest; };
-Words pick_words(int words, int d, int slabs)
-{
-    float best;
-    const Tile all = pick_product(kByRows, 1, words, d, slabs, &best);
-    Words w{all, words, all};
-    const int n_cu = cu_count() ? cu_count() : 256;
-    for (Tile t : kProductTiles) {
-        if (t == T64x64 || slabs < kLeastSlabs[t]) continue;
-        const int columns = (d + kTileColumns[t] - 1) / kTileColumns[t];
-        const int first = (int)((int64_t)words * columns / kTileRows[t] / n_cu) * n_cu / columns * kTileRows[t];
-        if (first <= 0 || first >= words) continue;
-        float rest_us;
-        const Tile rest = pick_product(kByRows, 1, words - first, d, slabs, &rest_us);
-        const float us = product_us(kByRows, t, 1, first, d, slabs) + rest_us;
-        if (us < kCutGain * best) { best = us; w = Words{t, first, rest}; }
-    }
-    return w;
-}
 // G is held for `width` words at a time: as many as kPieceBytes hold (8192 rows: the whole of 50272 words), in `shares` shares of
 // share_words for the product with e, whose outputs [rows, d] are few tiles where rows are few.
 constexpr size_t kPieceBytes = 1u << 30;

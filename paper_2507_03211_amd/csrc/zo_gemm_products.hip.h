@@ -107,6 +107,29 @@ Tile pick_product(ProductKind kind, int shares, int m, int n, int slabs, float *
     if (us) *us = best_us;
     return best;
 }
+// de's words: those of whole rounds of one tile, and what is left in a launch of its own, in tiles of its own, where that is estimated to be
+// faster.  8192 x 768 x 50272: 591 tiles of 256 x 256 are 2.3 rounds on 256 CUs; two rounds and 216 tiles of 192 x 128 take the whole
+// call from 2094 us to 2032.  17 shapes that the rule cuts: 1.018 times as fast on average (0.998 - 1.040), to the same bits.
+constexpr float kCutGain = 0.99f;
+struct Words { Tile tile; int words; Tile rest; };
+Words pick_words(int words, int d, int slabs)
+{
+    float best;
+    const Tile all = pick_product(kByRows, 1, words, d, slabs, &best);
+    Words w{all, words, all};
+    const int n_cu = cu_count() ? cu_count() : 256;
+    for (Tile t : kProductTiles) {
+        if (t == T64x64 || slabs < kLeastSlabs[t]) continue;
+        const int columns = (d + kTileColumns[t] - 1) / kTileColumns[t];
+        const int first = (int)((int64_t)words * columns / kTileRows[t] / n_cu) * n_cu / columns * kTileRows[t];
+        if (first <= 0 || first >= words) continue;
+        float rest_us;
+        const Tile rest = pick_product(kByRows, 1, words - first, d, slabs, &rest_us);
+        const float us = product_us(kByRows, t, 1, first, d, slabs) + rest_us;
+        if (us < kCutGain * best) { best = us; w = Words{t, first, rest}; }
+    }
+    return w;
+}
 // of the launch that adds up dx's shares
 float shares_us(int shares, int rows, int d) { return 3.1f + (float)shares * (float)rows * (float)d * (4e-6f * 0.117f) + (shares < 8 ? 0.014f * (float)shares : 0.0f); }
 

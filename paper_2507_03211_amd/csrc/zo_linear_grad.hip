@@ -16,26 +16,29 @@ namespace {
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ the pass over dy
-// G's rows and the sums of its columns, eight columns a lane, a wavefront's 512 to a row; the workgroup's four take every fourth row of the
-// workgroup's share.  WIDE: dy is fp32.  g [rows, width] may be null (dy is G already); so may db and part.  One share: db at once; more:
-// part[share][n].
-template <int DT, bool WIDE, bool RELU>
+// G's rows and the sums of its columns, eight columns a thread, LANES threads to a row; the workgroup's 256 / LANES groups of them take every so
+// many-th row of the workgroup's share.  WIDE: dy is fp32.  g [rows, width] may be null (dy is G already); so may db and part.  One share: db at
+// once; more: part[share][n], for the launch that adds up shares.  LANES 64: whole lines of a row.  4: 64 rows at a time, for up to
+// kNarrowRows rows in one share, where no product has shares to add up either and that launch, 4 us, is saved.  us of the whole call, wide / narrow: 300 x
+// 2048 x 2048 23.8 / 21.1, 1048 x 2048 x 8192 81.0 / 79.4, 2000 x 768 x 2304 34.0 / 38.4, 2000 x 5120 x 5120 199.7 / 202.0.
+template <int DT, bool WIDE, bool RELU, int LANES>
 __global__ __launch_bounds__(256) void grad_rows_kernel(const void *__restrict__ dy, const uint16_t *__restrict__ y, uint4 *__restrict__ g,
                                                         float *__restrict__ part, uint16_t *__restrict__ db, int rows, int n, int width, int each)
 {
     constexpr int AHEAD = 4;
-    __shared__ float sums[4][64][8];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = (int)blockIdx.x * 512 + 8 * lane;
+    constexpr int GROUPS = 256 / LANES;
+    __shared__ float sums[GROUPS][LANES][8];
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int c = ((int)blockIdx.x * LANES + lane) * 8;
     const int first = (int)blockIdx.y * each, last = first + each < rows ? first + each : rows;
     const bool live = c < n;
     float sum[8] = {};
-    for (int r0 = first + wave; r0 < last; r0 += 4 * AHEAD) {
+    for (int r0 = first + group; r0 < last; r0 += GROUPS * AHEAD) {
         float4 wide[AHEAD][2];
         uint4 in[AHEAD], kept[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int r = r0 + 4 * i;
+            const int r = r0 + GROUPS * i;
             const bool on = live && r < last;
             const size_t at = (size_t)(on ? r : first) * n + (live ? c : 0);
             if constexpr (WIDE) {
@@ -49,7 +52,7 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const void *__restrict__
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int r = r0 + 4 * i;
+            const int r = r0 + GROUPS * i;
             if (r >= last) break;
             uint32_t out[4];
             float v[8];
@@ -75,18 +78,19 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const void *__restrict__
     }
     if (!db && !part) return;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sums[wave][lane][e] = sum[e];
+    for (int e = 0; e < 8; ++e) sums[group][lane][e] = sum[e];
     __syncthreads();
-    for (int i = threadIdx.x; i < 512; i += 256) {
-        const int col = (int)blockIdx.x * 512 + i;
+    for (int i = threadIdx.x; i < 8 * LANES; i += 256) {
+        const int col = (int)blockIdx.x * LANES * 8 + i;
         if (col >= n) continue;
         float s = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) s += sums[w][i / 8][i % 8];
+#pragma unroll 8
+        for (int w = 0; w < GROUPS; ++w) s += sums[w][i / 8][i % 8];
         if (part) part[(size_t)blockIdx.y * n + col] = s;
         else db[col] = Prec<DT>::acc2a(s);
     }
 }
+constexpr int kNarrowRows = 1024;
 
 // ------------------------------------------------------------------ sums of shares
 // out = rn(sum_z part[z]), eight elements a thread, zeros where `keep` is not above zero (if there is one); the workgroup's `groups` groups of
@@ -134,10 +138,13 @@ struct LinearPlan {
     int x_shares, x_share;                  // shares of dx's contraction over n, and the columns of one
     int w_shares, w_share;                  // of dW's over the rows
     int sum_shares, sum_each;               // of the column sums, and the rows of one
+    bool narrow;                            // one share, by narrow workgroups
     Tile x_tile, w_tile;
+    Words w_rows;                           // dW's rows, where its sum has one share: what whole rounds of a tile hold and the rest
     bool both, fits;                        // one launch for both products; every launch's tiles fit one
     size_t g, x_part, w_part, sums, total;
 };
+constexpr int kSumBlocks = 1024;            // workgroups of the pass over dy, about: four to a CU
 LinearPlan linear_plan(int rows, int n, int k, int epilogue)
 {
     LinearPlan p{};
@@ -161,13 +168,17 @@ LinearPlan linear_plan(int rows, int n, int k, int epilogue)
         if (best == 0.0f || us < best) { best = us; p.w_shares = z; p.w_tile = t; }
     }
     p.w_share = (r_slabs + p.w_shares - 1) / p.w_shares * BK;
-    p.both = p.x_tile == T64x64 && p.w_tile == T64x64 && p.x_shares > 1 && p.w_shares == 1 && p.x_share <= kBothSlabs * BK && r_slabs * BK <= kBothRows;
-    const int64_t dx = small_blocks(p.x_tile, p.x_shares, rows, k), dw = small_blocks(p.w_tile, p.w_shares, n, k);
+    p.w_rows = p.w_shares == 1 ? pick_words(n, k, r_slabs) : Words{p.w_tile, n, p.w_tile};
+    p.w_tile = p.w_rows.tile;
+    p.both = p.x_tile == T64x64 && p.w_tile == T64x64 && p.w_rows.words == n && p.x_shares > 1 && p.w_shares == 1 && p.x_share <= kBothSlabs * BK && r_slabs * BK <= kBothRows;
+    const int64_t dx = small_blocks(p.x_tile, p.x_shares, rows, k), dw = small_blocks(p.w_tile, p.w_shares, p.w_rows.words, k);
     p.fits = dx <= kMostBlocks && dw <= kMostBlocks && (!p.both || dx + dw <= kMostBlocks);
-    const int columns = ((copy ? p.width : n) + 511) / 512, most = 2048 / columns > 1 ? 2048 / columns : 1;
+    const int columns = ((copy ? p.width : n) + 511) / 512, most = kSumBlocks / columns > 1 ? kSumBlocks / columns : 1;
     p.sum_shares = rows <= 64 ? 1 : (rows + 15) / 16 < most ? (rows + 15) / 16 : most;
     p.sum_each = ((rows + p.sum_shares - 1) / p.sum_shares + 3) / 4 * 4;
     p.sum_shares = (rows + p.sum_each - 1) / p.sum_each;
+    p.narrow = p.sum_shares > 1 && rows <= kNarrowRows && p.x_shares == 1 && p.w_shares == 1;
+    if (p.narrow) { p.sum_shares = 1; p.sum_each = rows; }
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up(o + bytes); return at; };
     p.g = take(2 * (size_t)rows * p.width);
@@ -188,9 +199,12 @@ hipError_t linear_grad(const uint16_t *x, const uint16_t *w, const uint16_t *y, 
     const bool copy = p.width != 0 && (dx || dw);
     float *sums = db && p.sum_shares > 1 ? (float *)(ws + p.sums) : nullptr;
     if (copy || db) {
-        auto kern = epilogue >= 2 ? grad_rows_kernel<DT, true, false> : epilogue == 1 ? grad_rows_kernel<DT, false, true> : grad_rows_kernel<DT, false, false>;
-        const int width = copy ? p.width : n;
-        kern<<<dim3((width + 511) / 512, p.sum_shares), dim3(256), 0, s>>>(dy, y, copy ? (uint4 *)(ws + p.g) : nullptr, sums, sums ? nullptr : db, rows, n,
+        auto kern = [&](auto lanes) {
+            constexpr int L = decltype(lanes)::value;
+            return epilogue >= 2 ? grad_rows_kernel<DT, true, false, L> : epilogue == 1 ? grad_rows_kernel<DT, false, true, L> : grad_rows_kernel<DT, false, false, L>;
+        };
+        const int width = copy ? p.width : n, columns = p.narrow ? 32 : 512;
+        (p.narrow ? kern(std::integral_constant<int, 4>{}) : kern(std::integral_constant<int, 64>{}))<<<dim3((width + columns - 1) / columns, p.sum_shares), dim3(256), 0, s>>>(dy, y, copy ? (uint4 *)(ws + p.g) : nullptr, sums, sums ? nullptr : db, rows, n,
                                                                            width, p.sum_each);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
@@ -209,17 +223,22 @@ hipError_t linear_grad(const uint16_t *x, const uint16_t *w, const uint16_t *y, 
     op_w.x_end = (uint64_t)(uintptr_t)(g + (size_t)rows * ldg);
     op_w.w_end = (uint64_t)(uintptr_t)(x + (size_t)rows * k);
     op_w.alpha = 1.0f;
-    const Args b{g, x, nullptr, nullptr, nullptr, p.w_shares > 1 ? (void *)(ws + p.w_part) : dw, p.w_shares, n, k, p.w_share, s};
+    const Args b{g, x, nullptr, nullptr, nullptr, p.w_shares > 1 ? (void *)(ws + p.w_part) : dw, p.w_shares, p.w_rows.words, k, p.w_share, s};
     if (dx && dw && p.both) {
         if ((err = launch_both<DT>(a, op_x, b, op_w)) != hipSuccess) return err;
     } else {
+        // (dW first: what it reads of x is near when dx's results are held against it)
+        if (dw) {
+            err = p.w_shares > 1 ? launch_product<DT, 7, ByRows>(p.w_tile, b, op_w) : launch_product<DT, 6, ByRows>(p.w_tile, b, op_w);
+            if (err != hipSuccess) return err;
+            if (p.w_rows.words < n) {
+                const Args rest{g + p.w_rows.words, x, nullptr, nullptr, nullptr, dw + (size_t)p.w_rows.words * k, 1, n - p.w_rows.words, k, p.w_share, s};
+                if ((err = launch_product<DT, 6, ByRows>(p.w_rows.rest, rest, op_w)) != hipSuccess) return err;
+            }
+        }
         if (dx) {
             err = p.x_shares > 1 ? launch_product<DT, 7, ByWords>(p.x_tile, a, op_x) : relu_x ? launch_product<DT, 10, ByWords>(p.x_tile, a, op_x)
                                                                                              : launch_product<DT, 6, ByWords>(p.x_tile, a, op_x);
-            if (err != hipSuccess) return err;
-        }
-        if (dw) {
-            err = p.w_shares > 1 ? launch_product<DT, 7, ByRows>(p.w_tile, b, op_w) : launch_product<DT, 6, ByRows>(p.w_tile, b, op_w);
             if (err != hipSuccess) return err;
         }
     }
