@@ -15,6 +15,7 @@ namespace zo {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = kAdamBlock;
 constexpr int kBlocksAhead = 4;                                 // of a wavefront: their loads are under way together
@@ -60,22 +61,49 @@ template <bool LOW> __device__ __forceinline__ uint32_t hold8(const float (&x)[4
         const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
         top = b > top ? b : top;
     }
-    top = wave_umax(top);
+    top = (uint32_t)__builtin_amdgcn_readfirstlane((int)wave_umax(top));       // (one for the wavefront: its tests are scalar)
     scale = __uint_as_float(top) * (1.0f / 448.0f);
-    float inverse = 1.0f / scale;
-    if (!(scale >= 0x1p-126f)) scale = inverse = 0.0f;
-    if (top >= 0x7f800000u) { scale = __uint_as_float(0x7fc00000u); inverse = 0.0f; }
-    float y[4];
+    float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (top >= 0x7f800000u) {
+        scale = __uint_as_float(0x7fc00000u);
+    } else if (!(scale >= 0x1p-126f)) {
+        scale = 0.0f;
+    } else {
+        const float inverse = 1.0f / scale;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        y[e] = top >= 0x7f800000u ? 0.0f : x[e] * inverse;
-        if (LOW && x[e] > 0.0f && inverse > 0.0f) y[e] = __builtin_fmaxf(y[e], 0x1p-9f);
+        for (int e = 0; e < 4; ++e) {
+            y[e] = x[e] * inverse;
+            // (2^-9 for what is above zero, as no root of an fp32 number is below 2^-75; zero for zero)
+            if (LOW) y[e] = __builtin_fmaxf(y[e], __builtin_fminf(x[e] * 0x1p100f, 0x1p-9f));
+        }
     }
     return to_e4m3(y);
 }
 
+// The correctly rounded square root of four numbers.  Where all of a wavefront's lie between 2^-90 and 2^120: from the hardware's reciprocal root and
+// one correction with the exact remainder, 6 instructions a number (the compiler's, for the whole range, takes 16).  The two differ for none of the 2^24
+// numbers of two neighbouring powers of two, and a power of four goes through every step unchanged.
+__device__ __forceinline__ float near_root(float v)
+{
+    const float y = __builtin_amdgcn_rsqf(v), s = v * y;
+    return __builtin_fmaf(__builtin_fmaf(-s, s, v), 0.5f * y, s);
+}
+__device__ __forceinline__ void roots(const float (&v)[4], float (&root)[4])
+{
+    const float low = __builtin_fminf(__builtin_fminf(v[0], v[1]), __builtin_fminf(v[2], v[3])), high = __builtin_fmaxf(__builtin_fmaxf(v[0], v[1]), __builtin_fmaxf(v[2], v[3]));
+    const bool plain = low > 0x1p-90f && high < 0x1p120f && v[0] == v[0] && v[1] == v[1] && v[2] == v[2] && v[3] == v[3];
+    if (__builtin_amdgcn_ballot_w64(!plain) == 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) root[e] = near_root(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) root[e] = __builtin_sqrtf(v[e]);       // (rounded to nearest; the intrinsic of that name is a step off at times)
+    }
+}
+
 // Chunk c of a batch: its tensor (found by the lanes side by side), its first element and how many it has.
-struct AdamPlace { char *param, *state; const char *grad; uint64_t at; uint32_t n, tensor; };
+#define ZO_GLOBAL __attribute__((address_space(1)))            // (addresses out of a table would take flat accesses, which go by the LDS too)
+struct AdamPlace { ZO_GLOBAL char *param, *state; const ZO_GLOBAL char *grad; uint64_t at; uint32_t n, tensor; };
 template <int N> __device__ __forceinline__ AdamPlace adam_place(const AdamBatchOf<N> &b, uint32_t c)
 {
     const int lane = threadIdx.x & 63;
@@ -84,114 +112,139 @@ template <int N> __device__ __forceinline__ AdamPlace adam_place(const AdamBatch
     t = __builtin_amdgcn_readfirstlane(t);
     const uint64_t param = b.param[t];
     const uint32_t end = t + 1 < b.n ? b.first[t + 1] : b.chunks;
-    return {(char *)(param & 0xffffffffffffull), (char *)b.state[t], (const char *)b.grad[t], (uint64_t)(c - b.first[t]) * kAdamChunk,
+    return {(ZO_GLOBAL char *)(uintptr_t)(param & 0xffffffffffffull), (ZO_GLOBAL char *)(uintptr_t)b.state[t], (const ZO_GLOBAL char *)(uintptr_t)b.grad[t],
+            (uint64_t)(c - b.first[t]) * kAdamChunk,
             c + 1 == end ? (uint32_t)(param >> 48) + 1 : kAdamChunk, (uint32_t)t};
 }
 
-// four stored numbers of a tensor, `left` of which exist
-template <typename W> struct Four { W w[4]; };
-template <typename W> __device__ __forceinline__ Four<W> load4(const W *p, int left)
+// four stored numbers of a tensor, `left` of which exist (WHOLE: all)
+template <typename W> struct Four { typedef W type __attribute__((ext_vector_type(4))); };
+template <bool WHOLE, typename W> __device__ __forceinline__ typename Four<W>::type load4(const ZO_GLOBAL W *p, int left)
 {
-    Four<W> f;
-    if (left >= 4) {
-        __builtin_memcpy(&f, __builtin_assume_aligned(p, 4 * sizeof(W)), sizeof f);
-    } else {
+    typename Four<W>::type f = {};
+    if (WHOLE || left >= 4) return *(const ZO_GLOBAL typename Four<W>::type *)p;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f.w[e] = e < left ? p[e] : (W)0;
-    }
+    for (int e = 0; e < 4; ++e)
+        if (e < left) f[e] = p[e];
     return f;
 }
-template <typename W> __device__ __forceinline__ void store4(W *p, const Four<W> &f, int left)
+template <bool WHOLE, typename W> __device__ __forceinline__ void store4(ZO_GLOBAL W *p, const typename Four<W>::type &f, int left)
 {
-    if (left >= 4) {
-        __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(W)), &f, sizeof f);
-    } else {
+    if (WHOLE || left >= 4) {
+        *(ZO_GLOBAL typename Four<W>::type *)p = f;
+        return;
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = f.w[e];
+    for (int e = 0; e < 4; ++e)
+        if (e < left) p[e] = f[e];
+}
+
+// kBlocksAhead blocks from block r of a chunk on, as many as the chunk has (WHOLE: all of them and every element).
+template <int DT, int BITS, bool SR, bool WHOLE> __device__ __forceinline__ void adamw_blocks(const AdamPlace &t, int r, const AdamScalars &k, float coef, int power)
+{
+    using P = Prec<DT>;
+    using W = typename P::W;
+    using F = typename Four<W>::type;
+    const int lane = threadIdx.x & 63;
+    F pw[kBlocksAhead], gw[kBlocksAhead];
+    f32x4 m32[BITS == 32 ? kBlocksAhead : 1], v32[BITS == 32 ? kBlocksAhead : 1];
+    uint32_t m8[kBlocksAhead], v8[kBlocksAhead];
+    f32x2 scale[kBlocksAhead];
+    ZO_GLOBAL W *param = (ZO_GLOBAL W *)t.param + t.at + r * kBlock + 4 * lane;
+    const ZO_GLOBAL W *grad = (const ZO_GLOBAL W *)t.grad + t.at + r * kBlock + 4 * lane;
+    ZO_GLOBAL char *state = t.state + (t.at / kBlock + r) * kAdamBlockBytes<BITS>;
+    auto any = [&](int i) { return WHOLE || (r + i) * kBlock < (int)t.n; };          // all of a wavefront's lanes: a state's blocks are whole
+    auto left = [&](int i) { return (int)t.n - (r + i) * kBlock - 4 * lane; };
+#pragma unroll
+    for (int i = 0; i < kBlocksAhead; ++i) {
+        if (!any(i)) continue;
+        pw[i] = load4<WHOLE, W>(param + i * kBlock, left(i));
+        gw[i] = load4<WHOLE, W>(grad + i * kBlock, left(i));
+        const ZO_GLOBAL char *s = state + i * kAdamBlockBytes<BITS>;
+        if constexpr (BITS == 32) {
+            m32[i] = *(const ZO_GLOBAL f32x4 *)(s + 16 * lane);
+            v32[i] = *(const ZO_GLOBAL f32x4 *)(s + 1024 + 16 * lane);
+        } else {
+            m8[i] = *(const ZO_GLOBAL uint32_t *)(s + 4 * lane);
+            v8[i] = *(const ZO_GLOBAL uint32_t *)(s + 256 + 4 * lane);
+            scale[i] = *(const ZO_GLOBAL f32x2 *)(s + 512);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kBlocksAhead; ++i) {
+        if (!any(i)) continue;
+        float m[4], v[4], root[4], g[4];
+        if constexpr (BITS == 32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { m[e] = m32[i][e]; v[e] = v32[i][e]; }
+        } else {
+            from_e4m3(m8[i], scale[i].x, m);
+            from_e4m3(v8[i], scale[i].y, root);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = root[e] * root[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] = coef * P::w2f(gw[i][e]);
+        if (power) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g[e] = ldexpf(g[e], power);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = WHOLE || e < left(i);               // (what lies behind a tensor's end, in its state's last block, is zeros)
+            m[e] = in ? k.b1 * m[e] + k.c1 * g[e] : 0.0f;
+            v[e] = in ? k.b2 * v[e] + (k.c2 * g[e]) * g[e] : 0.0f;
+        }
+        roots(v, root);
+        u32x4 word{};
+        if constexpr (SR) word = philox_block(k.seed, k.first_tensor + t.tensor, (t.at + (uint32_t)((r + i) * kBlock + 4 * lane)) / 4, 3u);
+        const uint32_t words[4] = {word.x, word.y, word.z, word.w};
+        F now;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float p = P::w2f(pw[i][e]), moved = p - (k.decay * p + k.rate * m[e] / (k.root * root[e] + k.eps));
+            if constexpr (SR) now[e] = DT == kBF16 ? sr_to_bf16(moved, words[e]) : sr_to_f16(moved, words[e]);
+            else now[e] = P::f2w(moved);
+        }
+        store4<WHOLE, W>(param + i * kBlock, now, left(i));
+        ZO_GLOBAL char *s = state + i * kAdamBlockBytes<BITS>;
+        if constexpr (BITS == 32) {
+            *(ZO_GLOBAL f32x4 *)(s + 16 * lane) = f32x4{m[0], m[1], m[2], m[3]};
+            *(ZO_GLOBAL f32x4 *)(s + 1024 + 16 * lane) = f32x4{v[0], v[1], v[2], v[3]};
+        } else {
+            float m_scale, v_scale;
+            const uint32_t m_now = hold8<false>(m, m_scale), v_now = hold8<true>(root, v_scale);
+            *(ZO_GLOBAL uint32_t *)(s + 4 * lane) = m_now;
+            *(ZO_GLOBAL uint32_t *)(s + 256 + 4 * lane) = v_now;
+            if (lane == 0) *(ZO_GLOBAL f32x2 *)(s + 512) = f32x2{m_scale, v_scale};
+        }
     }
 }
 
 template <int DT, int BITS, bool SR, int N>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamBatchOf<N> b, AdamScalars k)
 {
-    using P = Prec<DT>;
-    using W = typename P::W;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // the clipping's coefficient, as a fraction from a half to one and a power of two: itself it may lie beyond fp32's range
-    float fraction = 1.0f;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // the clipping's coefficient, as an fp32 number and, where it lies beyond these, a power of two
+    float coef = 1.0f;
     int power = 0;
     if (k.norm) {
         const double norm = *k.norm;
         if (!(norm - norm == 0.0)) return;                      // nothing is written
-        if (norm > (double)k.max_norm) fraction = (float)frexp((double)k.max_norm / norm, &power);
+        if (norm > (double)k.max_norm) {
+            coef = (float)frexp((double)k.max_norm / norm, &power);
+            power = __builtin_amdgcn_readfirstlane(power);
+            if (power > -120) {
+                coef = ldexpf(coef, power);
+                power = 0;
+            }
+        }
     }
     for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
         const AdamPlace t = adam_place(b, c);
         for (int r = wave * kBlocksAhead; r < kChunkBlocks && r * kBlock < (int)t.n; r += 4 * kBlocksAhead) {
-            Four<W> pw[kBlocksAhead], gw[kBlocksAhead];
-            f32x4 m32[BITS == 32 ? kBlocksAhead : 1], v32[BITS == 32 ? kBlocksAhead : 1];
-            uint32_t m8[kBlocksAhead], v8[kBlocksAhead];
-            float2 scale[kBlocksAhead];
-            const uint64_t block0 = t.at / kBlock + r;
-#pragma unroll
-            for (int i = 0; i < kBlocksAhead; ++i) {
-                const int first = (r + i) * kBlock + 4 * lane, left = (int)t.n - first;
-                pw[i] = load4((const W *)t.param + t.at + first, left);
-                gw[i] = load4((const W *)t.grad + t.at + first, left);
-                const bool any = (r + i) * kBlock < (int)t.n;    // a wavefront's all lanes: a state's blocks are whole
-                const char *s = t.state + (block0 + i) * kAdamBlockBytes<BITS>;
-                if constexpr (BITS == 32) {
-                    m32[i] = any ? *(const f32x4 *)(s + 16 * lane) : f32x4{};
-                    v32[i] = any ? *(const f32x4 *)(s + 1024 + 16 * lane) : f32x4{};
-                } else {
-                    m8[i] = any ? *(const uint32_t *)(s + 4 * lane) : 0;
-                    v8[i] = any ? *(const uint32_t *)(s + 256 + 4 * lane) : 0;
-                    scale[i] = any ? *(const float2 *)(s + 512) : float2{0.0f, 0.0f};
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kBlocksAhead; ++i) {
-                const int first = (r + i) * kBlock + 4 * lane, left = (int)t.n - first;
-                if ((r + i) * kBlock >= (int)t.n) break;
-                float m[4], v[4], root[4];
-                if constexpr (BITS == 32) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { m[e] = m32[i][e]; v[e] = v32[i][e]; }
-                } else {
-                    from_e4m3(m8[i], scale[i].x, m);
-                    from_e4m3(v8[i], scale[i].y, root);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = root[e] * root[e];
-                }
-                u32x4 word{};
-                if constexpr (SR) word = philox_block(k.seed, k.first_tensor + t.tensor, (t.at + first) / 4, 3u);
-                const uint32_t words[4] = {word.x, word.y, word.z, word.w};
-                Four<W> out;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool in = e < left;                   // (what lies behind a tensor's end, in its state's last block, is zeros)
-                    const float g = in ? ldexpf(fraction * P::w2f(gw[i].w[e]), power) : 0.0f, p = P::w2f(pw[i].w[e]);
-                    m[e] = in ? k.b1 * m[e] + k.c1 * g : 0.0f;
-                    v[e] = in ? k.b2 * v[e] + (k.c2 * g) * g : 0.0f;
-                    root[e] = __builtin_sqrtf(v[e]);           // (rounded to nearest; the intrinsic of that name here is a step off at times)
-                    const float moved = p - (k.decay * p + k.rate * m[e] / (k.root * root[e] + k.eps));
-                    if constexpr (SR) out.w[e] = DT == kBF16 ? sr_to_bf16(moved, words[e]) : sr_to_f16(moved, words[e]);
-                    else out.w[e] = P::f2w(moved);
-                }
-                store4((W *)t.param + t.at + first, out, left);
-                char *s = t.state + (block0 + i) * kAdamBlockBytes<BITS>;
-                if constexpr (BITS == 32) {
-                    *(f32x4 *)(s + 16 * lane) = f32x4{m[0], m[1], m[2], m[3]};
-                    *(f32x4 *)(s + 1024 + 16 * lane) = f32x4{v[0], v[1], v[2], v[3]};
-                } else {
-                    float2 now;
-                    const uint32_t m_now = hold8<false>(m, now.x), v_now = hold8<true>(root, now.y);
-                    *(uint32_t *)(s + 4 * lane) = m_now;
-                    *(uint32_t *)(s + 256 + 4 * lane) = v_now;
-                    if (lane == 0) *(float2 *)(s + 512) = now;
-                }
-            }
+            if ((r + kBlocksAhead) * kBlock <= (int)t.n) adamw_blocks<DT, BITS, SR, true>(t, r, k, coef, power);
+            else adamw_blocks<DT, BITS, SR, false>(t, r, k, coef, power);
         }
     }
 }
@@ -204,7 +257,7 @@ hipError_t adamw(void *const *param, const void *const *grad, void *const *state
     int first_tensor = 0;
     auto flush = [&](int next) {
         hipError_t e = hipSuccess;
-        if (b.n) {
+        if (b.chunks) {
             k.first_tensor = first_tensor;
             adamw_kernel<DT, BITS, SR, N><<<dim3(b.chunks < kAdamGrid ? b.chunks : kAdamGrid), dim3(256), 0, s>>>(b, k);
             e = hipGetLastError();

@@ -341,3 +341,12 @@ def test_8_bit_states_side_by_side():
 def test_nothing_to_do():
     zo_amd.zo_kernel_adamw([], [], [], [], 0, zi.BF16, 32, LR, B1, B2, EPS, WD, 1)
     zo_amd.zo_kernel_adamw([None], [None], [None], [0], 1, zi.BF16, 8, LR, B1, B2, EPS, WD, 1)
+
+
+@pytest.mark.parametrize("before", [39, 40, 139, 140, 141, 300])
+def test_a_table_of_empty_tensors_in_front(before):
+    """Nothing but empty tensors in a launch's table: no launch, and the numbering goes on."""
+    ts = Tensors(zi.BF16, 32, [0] * before + [5, 700] + [0] * 150)
+    at = ts.host()
+    ts.step(3, rounding=zo_amd.ZO_ROUND_STOCHASTIC, seed=9)
+    same(ts, expect(ts, *at, 3, stochastic=True, seed=9))
