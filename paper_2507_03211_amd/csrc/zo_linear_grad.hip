@@ -382,6 +382,8 @@ bool linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan)
     plan[3] = p.w_shares;
     plan[4] = p.width;
     plan[5] = p.sum_shares;
+    plan[6] = p.w_rows.words;
+    plan[7] = tile(p.w_rows.rest);
     return true;
 }
 

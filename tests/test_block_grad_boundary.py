@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 import paper_2507_03211_amd as zo_amd
 from paper_2507_03211_amd import ZO_BF16, ZO_FP16, ZO_FP32
@@ -105,6 +106,20 @@ def test_linear_grad_plan():
     for bad in ((0, 64, 64, 0), (4, 60, 64, 0), (4, 64, 60, 0), (4, 64, 64, 4)):
         refused(zo_amd.zo_kernel_linear_grad_plan, *bad)
     assert zo_amd.lib().zo_kernel_linear_grad_plan(4, 64, 64, 0, None) == zo_amd.ZO_EINVAL
+
+
+@pytest.mark.parametrize("rows,n,k", [(1048, 5000, 4096), (2050, 13000, 1288), (700, 13000, 3000), (8192, 20480, 5120), (300, 512, 512), (8192, 768, 768)])
+def test_linear_grad_plan_of_the_rows_behind_whole_rounds(rows, n, k):
+    """dw's launch is whole rounds of tiles over the compute units (256 where there is no device) or has all rows."""
+    p = zo_amd.zo_kernel_linear_grad_plan(rows, n, k, 0)
+    tall, wide = p["dw"]
+    assert 0 < p["dw_rows"] <= n and (p["dw_rows"] == n or p["dw_rows"] % tall == 0)
+    assert (p["dw_rows"] < n) == (n >= 5000)
+    if p["dw_rows"] < n:
+        assert p["dw_shares"] == 1
+    if p["dw_rows"] < n and not torch.cuda.is_available():
+        tiles = (p["dw_rows"] // tall) * ((k + wide - 1) // wide)
+        assert -tiles % 256 < (k + wide - 1) // wide         # (what a last row of tiles would pass the rounds by)
 
 
 @pytest.mark.parametrize("dtype,rows,n,k", [(ZO_BF16, 64, 1 << 22, 1 << 18), (ZO_FP16, 1 << 20, 64, 1 << 22), (ZO_FP32, 1 << 20, 64, 1 << 17)])

@@ -117,6 +117,28 @@ def test_tiles(dtype, rows, n, k, epilogue, relu_x):
     l.check(step(min(rows, n)))
 
 
+@pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows,n,k,epilogue", [(1048, 5000, 4096, 0), (2050, 13000, 1288, 2), (700, 13000, 3000, 1)])
+def test_rows_behind_whole_rounds_of_tiles(dtype, rows, n, k, epilogue):
+    p = zo_amd.zo_kernel_linear_grad_plan(rows, n, k, epilogue)
+    assert p["dw_rows"] < n
+    l = Layer(dtype, rows, n, k, epilogue, False)
+    l.run()
+    torch.cuda.synchronize()
+    assert l.whole()
+    step = max(1, rows // 300)
+    l.check(slice(None, rows, step))                           # (dx's rows, and as many of dw's first)
+    cut = p["dw_rows"]
+    last = torch.cat([torch.arange(cut - 40, min(cut + 300, n)), torch.arange(n - 40, n)])
+    grad = l.dy.double() if l.y is None else torch.where(l.y > 0, l.dy.double(), 0.0)
+    left, right = grad.t()[last.to(DEV)], l.x.double()
+    want, size = left @ right, left.abs() @ right.abs()
+    off = ((rows + 64) * 2.0**-24 + (half(param_dtype(dtype)) if epilogue >= 2 else 0.0)) * size
+    own = half(param_dtype(dtype))
+    tiny = least(param_dtype(dtype)) * (1.0 + (right.abs().sum(0) if epilogue >= 2 else 0.0))
+    assert bool(((l.dw.t[last.to(DEV)].double() - want).abs() <= off + own * (want.abs() + off) + tiny).all())
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows,n,k", [(65, 136, 72), (20, 768, 768), (700, 520, 256)])
 def test_subsets_of_the_outputs(dtype, rows, n, k):
