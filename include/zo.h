@@ -438,8 +438,9 @@ int zo_kernel_linear_grad(const void *x, const void *w, const void *y, const voi
 
 /* How such a call of 2-byte types works on the current device (on 256 compute units where there is none): plan[0], plan[1] the output tiles
  * of dx and dw (rows << 16 | columns), plan[2], plan[3] the shares their sums are cut into, plan[4] the columns of the copy it makes of
- * G (0: none), plan[5] the shares of db's sums, plan[6] dw's rows that plan[1]'s tiles work, plan[7] the tile of those behind them, if any.
- * plan holds 8 numbers.  Host only. */
+ * G (0: none), plan[5] the shares of db's sums, plan[6] dw's rows that plan[1]'s tiles work, plan[7] the tile of those behind them, if any;
+ * where a call that wants both dx and dw has them in one launch, plan[8] its tile and plan[9] dw's workgroups in it, else 0.  plan holds 10 numbers.
+ * Host only. */
 int zo_kernel_linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan);
 
 /* Backward pass of zo_kernel_attention: `out` is what the forward call left, dout its gradient [n_seq seq, d]; dqkv [n_seq seq, 3 d] gets

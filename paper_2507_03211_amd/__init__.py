@@ -381,12 +381,12 @@ def zo_kernel_linear_grad_scratch_bytes(dtype, rows, n, k, epilogue):
 
 def zo_kernel_linear_grad_plan(rows, n, k, epilogue):
     """Of 2-byte types: {"dx", "dw": (rows, columns) of the output tiles, "dx_shares", "dw_shares", "copy_columns", "db_shares", "dw_rows" (of dw's
-    tiles), "dw_rest" (the tiles of the rows behind them)}."""
-    plan = (ctypes.c_int32 * 8)()
+    tiles), "dw_rest" (the tiles of the rows behind them), "both" (the tile where one launch has both products, else None), "both_dw" (dw's workgroups in it)}."""
+    plan = (ctypes.c_int32 * 10)()
     _check(lib().zo_kernel_linear_grad_plan(rows, n, k, epilogue, plan))
     tile = lambda t: (t >> 16, t & 0xffff)  # noqa: E731
     return dict(dx=tile(plan[0]), dw=tile(plan[1]), dx_shares=plan[2], dw_shares=plan[3], copy_columns=plan[4], db_shares=plan[5], dw_rows=plan[6],
-                dw_rest=tile(plan[7]))
+                dw_rest=tile(plan[7]), both=tile(plan[8]) if plan[8] else None, both_dw=plan[9])
 
 
 def zo_kernel_linear_grad(x, w, y, dy, dx, dw, db, scratch, dtype, rows, n, k, epilogue, relu_x=False, stream=None):

@@ -399,7 +399,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     float a, b;
     swap_halves(l_lane, a, b);
     const float l = a + b;
-    // as the third launch's scores start from it: minus logsumexp, before the scaling
+    // as the other launch's scores start from it: minus logsumexp, before the scaling
     if (fh == 0) lse[(size_t)item.pair * seq + q] = -(m_run + __builtin_amdgcn_logf(l) / sc);
     const float scale = 1.0f / (l * __builtin_sqrtf((float)DH)) * (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f);
     uint16_t *dq = dqkv + ((size_t)s * seq + q) * ld + head * DH + 4 * fh;

@@ -552,11 +552,11 @@ template <int TM_, int TN_, int A_> struct Shape {
     static_assert(xloads(0) == 0 && xloads(2 * NM + NM / 2) == LX && wloads(0) == 0 && wloads(NM / 2 + NM) == LW, "");
 };
 
-template <int DT, int EPI, class SH, class OP = Plain>
-__global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *__restrict__ x, const uint16_t *__restrict__ wt_p,
-                                                             const uint16_t *__restrict__ wt_m, const uint16_t *__restrict__ b_p,
-                                                             const uint16_t *__restrict__ b_m, void *__restrict__ y, int m_half,
-                                                             int n, int k, int tiles_m, int tiles_n, int total, typename OP::Arg op)
+// The tiles of workgroup `block` of `blocks`, a multiple of 8 that starts at one.
+template <int DT, int EPI, class SH, class OP>
+__device__ __forceinline__ void pipe_tiles(const uint16_t *__restrict__ x, const uint16_t *__restrict__ wt_p, const uint16_t *__restrict__ wt_m,
+                                           const uint16_t *__restrict__ b_p, const uint16_t *__restrict__ b_m, void *__restrict__ y, int m_half, int n, int k,
+                                           int tiles_m, int tiles_n, int total, const typename OP::Arg &op, int block, int blocks)
 {
     constexpr bool XK = OP::kXK, WK = OP::kWK;
     constexpr int CHX = SH::BM / 8, CHW = SH::BN / 8;           // chunks of a k row, where k lies outside
@@ -567,8 +567,8 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
     // tile list, slot, slot + slots, ...  The software pipeline does not stop between tiles: while the last two
     // slabs of a tile are multiplied the first two slabs of the next tile are already being loaded, and they land
     // during the epilogue.
-    const int per_xcd = (total + 7) / 8, slots = (int)gridDim.x / 8;
-    const int xcd = (int)blockIdx.x % 8, slot0 = (int)blockIdx.x / 8;
+    const int per_xcd = (total + 7) / 8, slots = blocks / 8;
+    const int xcd = block % 8, slot0 = block / 8;
     auto tile_lin = [&](int it) {                                   // -1: no such tile
         const int sl = slot0 + slots * it, lin = xcd * per_xcd + sl;
         return (sl < per_xcd && lin < total) ? lin : -1;
@@ -848,6 +848,14 @@ __global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *_
         ++it;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // the tail loads land before LDS is released
+}
+template <int DT, int EPI, class SH, class OP = Plain>
+__global__ __launch_bounds__(256) void linear_mfma_pipe_kernel(const uint16_t *__restrict__ x, const uint16_t *__restrict__ wt_p,
+                                                             const uint16_t *__restrict__ wt_m, const uint16_t *__restrict__ b_p,
+                                                             const uint16_t *__restrict__ b_m, void *__restrict__ y, int m_half,
+                                                             int n, int k, int tiles_m, int tiles_n, int total, typename OP::Arg op)
+{
+    pipe_tiles<DT, EPI, SH, OP>(x, wt_p, wt_m, b_p, b_m, y, m_half, n, k, tiles_m, tiles_n, total, op, (int)blockIdx.x, (int)gridDim.x);
 }
 
 

@@ -132,6 +132,44 @@ __global__ __launch_bounds__(256) void shares_sum_kernel(SharesJobs jobs)
     }
 }
 
+// ------------------------------------------------------------------ both products in one launch
+// Where neither product fills the chip for long: dW's tiles on some CUs (workgroups 0 .. blocks_w - 1, persistent, one a CU), dx's on the others, tiles of
+// one shape.  What bounds such a call is not the multiplies but rounds of tiles that leave CUs empty, each launch's first loads and last stores, and the
+// sums of shares that a product needs to fill the chip by itself.  us of the whole call, bf16, two launches / one: 8192 x 768 x 768 45.7 / 39.5, 8192 x
+// 2304 x 768 75.0 / 68.7, 2000 x 2304 x 768 37.1 / 26.6, 2000 x 768 x 768 25.3 / 18.6, 1500 x 1536 x 1536 35.5 / 28.9, 4096 x 4096 x 1024 80.4 / 69.3,
+// 8192 x 4096 x 1024 173 / 158, 32768 x 512 x 512 75.8 / 70.6, 400 x 1024 x 4096 19.9 / 15.8, 300 x 512 x 512 14.6 / 11.3; of 34 sizes the worst pick is 4096 x 2048 x 2048, 78.9 / 80.1.
+struct PairTiles { const uint16_t *x, *w; void *y; int m, n, k, tiles_m, tiles_n, total; };
+template <int DT, int EPIW, int EPIX, class SH>
+__global__ __launch_bounds__(256) void linear_pair_kernel(PairTiles dw, PairTiles dx, ByRows::Arg op_w, ByWords::Arg op_x, int blocks_w)
+{
+    const int block = (int)blockIdx.x;
+    if (block < blocks_w)
+        pipe_tiles<DT, EPIW, SH, ByRows>(dw.x, dw.w, nullptr, nullptr, nullptr, dw.y, dw.m, dw.n, dw.k, dw.tiles_m, dw.tiles_n, dw.total, op_w, block, blocks_w);
+    else
+        pipe_tiles<DT, EPIX, SH, ByWords>(dx.x, dx.w, nullptr, nullptr, nullptr, dx.y, dx.m, dx.n, dx.k, dx.tiles_m, dx.tiles_n, dx.total, op_x, block - blocks_w,
+                                          (int)gridDim.x - blocks_w);
+}
+template <int DT, int EPIW, int EPIX, class SH> hipError_t launch_pair_of(const Args &dw, const ByRows::Arg &op_w, const Args &dx, const ByWords::Arg &op_x, int blocks_w, int blocks_x)
+{
+    auto tiles = [](const Args &a) {
+        const int tm = (a.m_half + SH::BM - 1) / SH::BM, tn = (a.n + SH::BN - 1) / SH::BN;
+        return PairTiles{(const uint16_t *)a.x, (const uint16_t *)a.wt_p, a.y, a.m_half, a.n, a.k, tm, tn, a.n_sign * tm * tn};
+    };
+    if (cu_count() == 0 || dw.k / BK <= SH::A || dx.k / BK <= SH::A) return hipErrorInvalidValue;
+    auto kern = linear_pair_kernel<DT, EPIW, EPIX, SH>;
+    static std::atomic<uint64_t> lds_allowed{0};
+    const hipError_t e = once_per_device(lds_allowed, [&] { return hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, SH::kLdsBytes); });
+    if (e != hipSuccess) return e;
+    kern<<<dim3(blocks_w + blocks_x), dim3(256), SH::kLdsBytes, dw.s>>>(tiles(dw), tiles(dx), op_w, op_x, blocks_w);
+    return hipGetLastError();
+}
+template <int DT, int EPIW, int EPIX> hipError_t launch_pair(Tile t, const Args &dw, const ByRows::Arg &op_w, const Args &dx, const ByWords::Arg &op_x, int blocks_w, int blocks_x)
+{
+    return t == T256x256   ? launch_pair_of<DT, EPIW, EPIX, Shape<4, 4, 2>>(dw, op_w, dx, op_x, blocks_w, blocks_x)
+           : t == T256x128 ? launch_pair_of<DT, EPIW, EPIX, Shape<4, 2, 2>>(dw, op_w, dx, op_x, blocks_w, blocks_x)
+                           : launch_pair_of<DT, EPIW, EPIX, Shape<2, 2, 4>>(dw, op_w, dx, op_x, blocks_w, blocks_x);
+}
+
 // ------------------------------------------------------------------ the plan of a call
 struct LinearPlan {
     int width;                              // of G's copy; 0: dy is G
@@ -139,13 +177,54 @@ struct LinearPlan {
     int w_shares, w_share;                  // of dW's over the rows
     int sum_shares, sum_each;               // of the column sums, and the rows of one
     bool narrow;                            // one share, by narrow workgroups
+    int pair_w, pair_x;                     // workgroups of dW and of dx where one launch has both; 0: launches of their own
+    Tile pair_tile;
     Tile x_tile, w_tile;
     Words w_rows;                           // dW's rows, where its sum has one share: what whole rounds of a tile hold and the rest
     bool both, fits;                        // one launch for both products; every launch's tiles fit one
     size_t g, x_part, w_part, sums, total;
 };
+constexpr float kPairMost = 250.0f, kPairGain = 0.95f;         // (longer calls have many rounds: nothing to gain; estimates nearer than that are a toss-up)
 constexpr int kSumBlocks = 1024;            // workgroups of the pass over dy, about: four to a CU
-LinearPlan linear_plan(int rows, int n, int k, int epilogue)
+// One launch of both products, dx in one share: the tile, dW's shares and the CUs of each of least estimated time, if that is below `limit`.  By the
+// costs of launches of their own, with what the faster clock of a chip that is not full saves counted for both together.
+void pick_pair(LinearPlan &p, int rows, int n, int k, int n_slabs, int r_slabs, float limit)
+{
+    const int n_cu = cu_count() ? cu_count() : 256;
+    for (Tile t : {T256x256, T256x128, T128x128}) {
+        if (n_slabs < kLeastSlabs[t]) continue;
+        auto tiles = [&](int m) { return (m + kTileRows[t] - 1) / kTileRows[t] * ((k + kTileColumns[t] - 1) / kTileColumns[t]); };
+        const auto &cx = kProductCost[kByWords][t], &cw = kProductCost[kByRows][t];
+        const int tx = tiles(rows), sx = n_slabs;
+        const float x_mb = (float)(rows + k) * (float)sx * (BK * 2e-6f) * cx.operand + (float)rows * (float)k * 4e-6f * cx.output;
+        for (int z = 1; z <= 64 && z <= r_slabs; z += z < 8 ? 1 : z < 16 ? 2 : 4) {
+            const int sw = (r_slabs + z - 1) / z, tw = z * tiles(n);
+            if (sw < kLeastSlabs[t]) break;
+            const float w_mb = (float)(n + k) * (float)(sw * z) * (BK * 2e-6f) * cw.operand + (float)n * (float)k * (float)z * 2e-6f * cw.output;
+            const float fixed = (cx.start > cw.start ? cx.start : cw.start) + x_mb + w_mb + (z > 1 ? shares_us(z, n, k) : 0.0f);
+            const float work_w = (float)tw * (float)sw, work_x = (float)tx * (float)sx, part = work_w / (work_w + work_x);
+            for (int i = -1; i < 3; ++i) {
+                const int bw = ((int)(part * (float)n_cu) / 8 + i) * 8, bx = n_cu - bw;
+                if (bw < 8 || bx < 8) continue;
+                const float rw = (float)(((tw + 7) / 8 + bw / 8 - 1) / (bw / 8)), rx = (float)(((tx + 7) / 8 + bx / 8 - 1) / (bx / 8));
+                // (how busy the chip is while the longer one lasts)
+                const float longest = rw * (float)sw > rx * (float)sx ? rw * (float)sw : rx * (float)sx, full = (work_w + work_x) / ((float)n_cu * longest);
+                const float busy = full > 0.5f ? 2 * full - 1 : 0.0f;
+                const float uw = rw * ((float)sw * (cw.slab + busy * cw.busy) + cw.round), ux = rx * ((float)sx * (cx.slab + busy * cx.busy) + cx.round);
+                const float us = fixed + (uw > ux ? uw : ux);
+                if (us >= limit) continue;
+                limit = us;
+                p.pair_w = bw; p.pair_x = bx;
+                p.pair_tile = t;
+                p.x_shares = 1; p.w_shares = z;
+            }
+        }
+    }
+    if (!p.pair_w) return;
+    p.x_tile = pick_product(kByWords, 1, rows, k, n_slabs);         // (for calls that want one of the two)
+    p.w_tile = pick_product(kByRows, p.w_shares, n, k, (r_slabs + p.w_shares - 1) / p.w_shares);
+}
+LinearPlan work_out(int rows, int n, int k, int epilogue)
 {
     LinearPlan p{};
     const bool copy = epilogue != 0 || n % BK != 0;
@@ -158,8 +237,7 @@ LinearPlan linear_plan(int rows, int n, int k, int epilogue)
         if (z > 1) us += shares_us(z, rows, k);
         if (best == 0.0f || us < best) { best = us; p.x_shares = z; p.x_tile = t; }
     }
-    p.x_share = (n_slabs + p.x_shares - 1) / p.x_shares * BK;
-    p.width = copy ? p.x_share * p.x_shares : 0;
+    const float x_us = best;
     best = 0.0f;
     for (int z = 1; z <= 64 && z <= r_slabs; z += z < 8 ? 1 : z < 16 ? 2 : 4) {
         float us;
@@ -167,10 +245,13 @@ LinearPlan linear_plan(int rows, int n, int k, int epilogue)
         if (z > 1) us += shares_us(z, n, k);
         if (best == 0.0f || us < best) { best = us; p.w_shares = z; p.w_tile = t; }
     }
+    if (best + x_us < kPairMost) pick_pair(p, rows, n, k, n_slabs, r_slabs, kPairGain * (best + x_us));
+    p.x_share = (n_slabs + p.x_shares - 1) / p.x_shares * BK;
+    p.width = copy ? p.x_share * p.x_shares : 0;
     p.w_share = (r_slabs + p.w_shares - 1) / p.w_shares * BK;
-    p.w_rows = p.w_shares == 1 ? pick_words(n, k, r_slabs) : Words{p.w_tile, n, p.w_tile};
+    p.w_rows = p.w_shares == 1 && !p.pair_w ? pick_words(n, k, r_slabs) : Words{p.w_tile, n, p.w_tile};
     p.w_tile = p.w_rows.tile;
-    p.both = p.x_tile == T64x64 && p.w_tile == T64x64 && p.w_rows.words == n && p.x_shares > 1 && p.w_shares == 1 && p.x_share <= kBothSlabs * BK && r_slabs * BK <= kBothRows;
+    p.both = !p.pair_w && p.x_tile == T64x64 && p.w_tile == T64x64 && p.w_rows.words == n && p.x_shares > 1 && p.w_shares == 1 && p.x_share <= kBothSlabs * BK && r_slabs * BK <= kBothRows;
     const int64_t dx = small_blocks(p.x_tile, p.x_shares, rows, k), dw = small_blocks(p.w_tile, p.w_shares, p.w_rows.words, k);
     p.fits = dx <= kMostBlocks && dw <= kMostBlocks && (!p.both || dx + dw <= kMostBlocks);
     const int columns = ((copy ? p.width : n) + 511) / 512, most = kSumBlocks / columns > 1 ? kSumBlocks / columns : 1;
@@ -188,12 +269,22 @@ LinearPlan linear_plan(int rows, int n, int k, int epilogue)
     p.total = o > 256 ? o : 256;
     return p;
 }
+// A thread's plans of late, by their sizes: a program goes through the same few over and over, and to work one out takes the host up to 25 us, as long
+// as the device needs for a small call.
+const LinearPlan &linear_plan(int rows, int n, int k, int epilogue)
+{
+    struct Kept { int rows, n, k, epilogue, n_cu; LinearPlan plan; };
+    static thread_local Kept kept[32];                         // (rows 0: none)
+    Kept &at = kept[(((((uint32_t)rows * 31u + (uint32_t)n) * 31u + (uint32_t)k) * 31u + (uint32_t)epilogue) * 0x9e3779b1u) >> 27];
+    if (at.rows != rows || at.n != n || at.k != k || at.epilogue != epilogue || at.n_cu != cu_count()) at = Kept{rows, n, k, epilogue, cu_count(), work_out(rows, n, k, epilogue)};
+    return at.plan;
+}
 
 template <int DT>
 hipError_t linear_grad(const uint16_t *x, const uint16_t *w, const uint16_t *y, const void *dy, uint16_t *dx, uint16_t *dw, uint16_t *db, char *ws, int rows,
                        int n, int k, int epilogue, bool relu_x, hipStream_t s)
 {
-    const LinearPlan p = linear_plan(rows, n, k, epilogue);
+    const LinearPlan &p = linear_plan(rows, n, k, epilogue);
     if (!p.fits) return hipErrorNotSupported;
     hipError_t err = hipSuccess;
     const bool copy = p.width != 0 && (dx || dw);
@@ -224,7 +315,12 @@ hipError_t linear_grad(const uint16_t *x, const uint16_t *w, const uint16_t *y, 
     op_w.w_end = (uint64_t)(uintptr_t)(x + (size_t)rows * k);
     op_w.alpha = 1.0f;
     const Args b{g, x, nullptr, nullptr, nullptr, p.w_shares > 1 ? (void *)(ws + p.w_part) : dw, p.w_shares, p.w_rows.words, k, p.w_share, s};
-    if (dx && dw && p.both) {
+    if (dx && dw && p.pair_w) {
+        auto pair = [&](auto epi_w, auto epi_x) { return launch_pair<DT, decltype(epi_w)::value, decltype(epi_x)::value>(p.pair_tile, b, op_w, a, op_x, p.pair_w, p.pair_x); };
+        auto with = [&](auto epi_w) { return relu_x ? pair(epi_w, std::integral_constant<int, 10>{}) : pair(epi_w, std::integral_constant<int, 6>{}); };
+        err = p.w_shares > 1 ? with(std::integral_constant<int, 7>{}) : with(std::integral_constant<int, 6>{});
+        if (err != hipSuccess) return err;
+    } else if (dx && dw && p.both) {
         if ((err = launch_both<DT>(a, op_x, b, op_w)) != hipSuccess) return err;
     } else {
         // (dW first: what it reads of x is near when dx's results are held against it)
@@ -367,13 +463,13 @@ hipError_t linear_grad_f64(const double *x, const float *w, const double *y, con
 size_t linear_grad_scratch(int dtype, int rows, int n, int k, int epilogue)
 {
     if (dtype == kFP32) return f64_blocks(rows, n, k, 32) < 1l << 24 ? 256 : 0;
-    const LinearPlan p = linear_plan(rows, n, k, epilogue);
+    const LinearPlan &p = linear_plan(rows, n, k, epilogue);
     return p.fits ? p.total : 0;
 }
 
 bool linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan)
 {
-    const LinearPlan p = linear_plan(rows, n, k, epilogue);
+    const LinearPlan &p = linear_plan(rows, n, k, epilogue);
     if (!p.fits) return false;
     auto tile = [](Tile t) { return kTileRows[t] << 16 | kTileColumns[t]; };
     plan[0] = tile(p.x_tile);
@@ -384,6 +480,8 @@ bool linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan)
     plan[5] = p.sum_shares;
     plan[6] = p.w_rows.words;
     plan[7] = tile(p.w_rows.rest);
+    plan[8] = p.pair_w ? tile(p.pair_tile) : 0;
+    plan[9] = p.pair_w;
     return true;
 }
 

@@ -17,7 +17,9 @@ DTYPES = [zi.FP32, zi.BF16, zi.FP16]
 # sizes that take every tile of both products, with one share and with several (test_every_tile_is_taken)
 TILES = [(300, 264, 8192, 0), (4100, 72, 2048, 0), (300, 1288, 3000, 0), (2050, 264, 3848, 0), (129, 1536, 3000, 0), (4100, 4096, 264, 0), (129, 2304, 3848, 0),
          (4100, 8192, 264, 0), (129, 1288, 8192, 0), (4100, 1000, 5120, 0), (1000, 8, 8, 0), (515, 264, 3848, 0), (65, 3000, 3000, 0), (4100, 200, 768, 0),
-         (2050, 8192, 8, 0), (2050, 200, 3000, 0), (4100, 4096, 8, 1), (2050, 200, 3848, 0), (1000, 8192, 1288, 0), (1500, 200, 8192, 0), (1048, 8192, 3000, 0), (1, 1288, 8, 0)]
+         (2050, 8192, 8, 0), (2050, 200, 3000, 0), (4100, 4096, 8, 1), (2050, 200, 3848, 0), (1000, 8192, 1288, 0), (1500, 200, 8192, 0), (1048, 8192, 3000, 0), (1, 1288, 8, 0), (2050, 3000, 768, 0), (5000, 1000, 1288, 0), (8200, 1288, 2048, 0), (1000, 8192, 8192, 0)]
+# sizes that have both products in one launch: each of its tiles, dw in one share and in several (test_every_joint_launch_is_taken)
+JOINT = [(200, 200, 8, 0), (300, 264, 8, 1), (700, 520, 8192, 0), (1000, 264, 8, 0), (1500, 200, 520, 2), (6000, 1000, 768, 2), (2000, 2304, 768, 0), (1500, 1536, 1536, 1)]
 SMALL = [(1, 8, 8), (1, 64, 64), (2, 72, 8), (3, 8, 200), (20, 768, 768), (63, 64, 128), (64, 128, 64), (65, 136, 72), (100, 1000, 1048), (257, 512, 256), (513, 2048, 640)]
 
 
@@ -115,6 +117,74 @@ def test_tiles(dtype, rows, n, k, epilogue, relu_x):
     assert l.whole()
     step = lambda m: slice(None, None, max(1, m // 700))  # noqa: E731
     l.check(step(min(rows, n)))
+
+
+def test_every_joint_launch_is_taken():
+    seen = set()
+    for shape in JOINT:
+        p = zo_amd.zo_kernel_linear_grad_plan(*shape)
+        assert p["both"] and 0 < p["both_dw"] < 256 and p["both_dw"] % 8 == 0 and p["dx_shares"] == 1
+        seen.add((p["both"], p["dw_shares"] > 1))
+    assert seen == {(t, several) for t in ((256, 256), (256, 128), (128, 128)) for several in (False, True)}
+
+
+@pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows,n,k,epilogue", JOINT)
+@pytest.mark.parametrize("relu_x", [False, True])
+def test_both_products_in_one_launch(dtype, rows, n, k, epilogue, relu_x):
+    l = Layer(dtype, rows, n, k, epilogue, relu_x)
+    l.run()
+    torch.cuda.synchronize()
+    assert l.whole()
+    l.check(slice(None, None, max(1, min(rows, n) // 500)))
+
+
+@pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows,n,k,epilogue", TILES + JOINT)
+def test_one_product_without_the_other(dtype, rows, n, k, epilogue):
+    """dx alone and dw alone, in launches of their own: the bits of the call for both."""
+    for relu_x in (False, True):
+        l = Layer(dtype, rows, n, k, epilogue, relu_x)
+        l.run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (l.dx.t, l.dw.t)]
+        for dx in (True, False):
+            for t in l.outs():
+                t.fill_(3.0)
+            l.scratch.fill_(0xFF)
+            l.run(dx, not dx, False, w=dx)
+            torch.cuda.synchronize()
+            assert l.whole()
+            assert torch.equal(l.dx.t, want[0]) if dx else torch.equal(l.dw.t, want[1])
+
+
+def test_plans_kept_stay_their_sizes_own():
+    """More sizes than a thread keeps, in turn and over again, from two threads: the same bits as alone."""
+    import threading
+    layers = [Layer(zi.BF16, 40 + 13 * i, 64 + 8 * (i % 7), 72 + 8 * (i % 5), i % 3, False, i) for i in range(48)]
+    want = []
+    for l in layers:
+        l.run()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in l.outs()])
+    for l in layers:
+        for t in l.outs():
+            t.fill_(5.0)
+        l.scratch.fill_(0xFF)
+    torch.cuda.synchronize()
+
+    def work(mine):
+        for _ in range(3):
+            for l in mine:
+                l.run()
+    threads = [threading.Thread(target=work, args=(layers[i::2],)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert all(l.whole() for l in layers)
+    assert all(torch.equal(a, b) for l, w in zip(layers, want) for a, b in zip(l.outs(), w))
 
 
 @pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
