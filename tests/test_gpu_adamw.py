@@ -343,6 +343,21 @@ def test_nothing_to_do():
     zo_amd.zo_kernel_adamw([None], [None], [None], [0], 1, zi.BF16, 8, LR, B1, B2, EPS, WD, 1)
 
 
+@pytest.mark.parametrize("first", [2.0**-40, 2.0**-89, 2.0**116, 2.0**-126])
+def test_roots_of_every_mantissa(first):
+    """v through two powers of two, in each of its fp32 numbers: halved exactly, its root, and a division that shows the root's last bit."""
+    n = 1 << 24
+    v = torch.arange(n, dtype=torch.int32, device=DEV).add_(int(np.float32(2 * first).view(np.int32))).view(torch.float32)
+    state = torch.stack([torch.full((n // 256, 256), 1.0 + 2.0**-20, device=DEV), v.view(-1, 256)], 1).contiguous()
+    param, grad = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    zo_amd.zo_kernel_adamw([param], [grad], [state], [n], 1, zi.FP32, 32, 2.0**-30, 0.5, 0.5, 2.0**-100, 0.0, 1 << 20)
+    half_v = v.cpu().numpy() * F(0.5)
+    step = F(2.0**-30) * F(0.5 * (1.0 + 2.0**-20)) / (np.sqrt(half_v) + F(2.0**-100))
+    assert step.dtype == F
+    assert np.array_equal(param.cpu().numpy().view(np.uint32), (F(0) - step).view(np.uint32))
+    assert np.array_equal(state[:, 1].reshape(-1).cpu().numpy(), half_v)
+
+
 @pytest.mark.parametrize("before", [39, 40, 139, 140, 141, 300])
 def test_a_table_of_empty_tensors_in_front(before):
     """Nothing but empty tensors in a launch's table: no launch, and the numbering goes on."""
