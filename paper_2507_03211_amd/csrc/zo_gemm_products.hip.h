@@ -27,18 +27,20 @@ using ByWords = Product<false, true>;       // G e: contraction over G's columns
 // 20 of 5120 x 8192 70.6 / 67.5.  Long contractions want the deeper ring and stay by themselves: by slabs a
 // share, 1 row of 4096 x 32000 (62) 195.0 / 181.3, 33 of 4096 x 20000 (78) 106.0 / 109.6, 64 of 2048 x 50272 (98) 155.7 / 153.2, 1 of 5120 x 128000
 // (125) 821.9 / 873.4, 20 of 8192 x 50272 (196) 572.7 / 585.7; 4000 rows of 8 x 64, 63 slabs in de, 50.8 / 62.9.
+// EPI: 7 where dx has shares; a linear layer's dx may have one (6, 10): rows x n x k 20 x 768 x 768 14.2 / 11.1, 200 x 768 x 768 13.8 / 11.1, 3 x 576 x 4096 13.4 /
+// 10.6, 100 x 1024 x 1024 13.8 / 12.5.
 constexpr int kBothSlabs = 64, kBothRows = 512;
 struct SmallTiles { const uint16_t *x, *w; void *y; int m, n, k, tiles_m, tiles_n, total; };
 constexpr int kBothStages = 2;
-template <int DT>
+template <int DT, int EPI = 7>
 __global__ __launch_bounds__(256, 2) void head_both_kernel(SmallTiles a, SmallTiles b, ByWords::Arg op_a, ByRows::Arg op_b, int blocks_a)
 {
     if ((int)blockIdx.x < blocks_a)
-        small_tile<DT, 7, 1, false, ByWords, kBothStages>(a.x, a.w, nullptr, nullptr, nullptr, a.y, a.m, a.n, a.k, a.tiles_m, a.tiles_n, a.total, op_a, (int)blockIdx.x);
+        small_tile<DT, EPI, 1, false, ByWords, kBothStages>(a.x, a.w, nullptr, nullptr, nullptr, a.y, a.m, a.n, a.k, a.tiles_m, a.tiles_n, a.total, op_a, (int)blockIdx.x);
     else
         small_tile<DT, 6, 1, false, ByRows, kBothStages>(b.x, b.w, nullptr, nullptr, nullptr, b.y, b.m, b.n, b.k, b.tiles_m, b.tiles_n, b.total, op_b, (int)blockIdx.x - blocks_a);
 }
-template <int DT> hipError_t launch_both(const Args &dx, const ByWords::Arg &op_dx, const Args &de, const ByRows::Arg &op_de)
+template <int DT, int EPI = 7> hipError_t launch_both(const Args &dx, const ByWords::Arg &op_dx, const Args &de, const ByRows::Arg &op_de)
 {
     auto tiles = [](const Args &a) {
         const int tm = (a.m_half + 63) / 64, tn = (a.n + 63) / 64;
@@ -46,7 +48,7 @@ template <int DT> hipError_t launch_both(const Args &dx, const ByWords::Arg &op_
     };
     const SmallTiles a = tiles(dx), b = tiles(de);
     const int blocks_a = (a.total + 7) / 8 * 8, blocks_b = (b.total + 7) / 8 * 8;
-    head_both_kernel<DT><<<dim3(blocks_a + blocks_b), dim3(256), kBothStages * kSmallStageBytes<1>, dx.s>>>(a, b, op_dx, op_de, blocks_a);
+    head_both_kernel<DT, EPI><<<dim3(blocks_a + blocks_b), dim3(256), kBothStages * kSmallStageBytes<1>, dx.s>>>(a, b, op_dx, op_de, blocks_a);
     return hipGetLastError();
 }
 

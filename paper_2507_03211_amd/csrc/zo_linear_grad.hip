@@ -251,7 +251,7 @@ LinearPlan work_out(int rows, int n, int k, int epilogue)
     p.w_share = (r_slabs + p.w_shares - 1) / p.w_shares * BK;
     p.w_rows = p.w_shares == 1 && !p.pair_w ? pick_words(n, k, r_slabs) : Words{p.w_tile, n, p.w_tile};
     p.w_tile = p.w_rows.tile;
-    p.both = !p.pair_w && p.x_tile == T64x64 && p.w_tile == T64x64 && p.w_rows.words == n && p.x_shares > 1 && p.w_shares == 1 && p.x_share <= kBothSlabs * BK && r_slabs * BK <= kBothRows;
+    p.both = !p.pair_w && p.x_tile == T64x64 && p.w_tile == T64x64 && p.w_rows.words == n && p.w_shares == 1 && p.x_share <= kBothSlabs * BK && r_slabs * BK <= kBothRows;
     const int64_t dx = small_blocks(p.x_tile, p.x_shares, rows, k), dw = small_blocks(p.w_tile, p.w_shares, p.w_rows.words, k);
     p.fits = dx <= kMostBlocks && dw <= kMostBlocks && (!p.both || dx + dw <= kMostBlocks);
     const int columns = ((copy ? p.width : n) + 511) / 512, most = kSumBlocks / columns > 1 ? kSumBlocks / columns : 1;
@@ -321,7 +321,8 @@ hipError_t linear_grad(const uint16_t *x, const uint16_t *w, const uint16_t *y, 
         err = p.w_shares > 1 ? with(std::integral_constant<int, 7>{}) : with(std::integral_constant<int, 6>{});
         if (err != hipSuccess) return err;
     } else if (dx && dw && p.both) {
-        if ((err = launch_both<DT>(a, op_x, b, op_w)) != hipSuccess) return err;
+        err = p.x_shares > 1 ? launch_both<DT>(a, op_x, b, op_w) : relu_x ? launch_both<DT, 10>(a, op_x, b, op_w) : launch_both<DT, 6>(a, op_x, b, op_w);
+        if (err != hipSuccess) return err;
     } else {
         // (dW first: what it reads of x is near when dx's results are held against it)
         if (dw) {
@@ -480,8 +481,8 @@ bool linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *plan)
     plan[5] = p.sum_shares;
     plan[6] = p.w_rows.words;
     plan[7] = tile(p.w_rows.rest);
-    plan[8] = p.pair_w ? tile(p.pair_tile) : 0;
-    plan[9] = p.pair_w;
+    plan[8] = p.pair_w ? tile(p.pair_tile) : p.both ? tile(T64x64) : 0;
+    plan[9] = p.pair_w ? p.pair_w : p.both ? (int32_t)small_blocks(T64x64, 1, n, k) : 0;
     return true;
 }
 

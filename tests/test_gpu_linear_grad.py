@@ -158,6 +158,25 @@ def test_one_product_without_the_other(dtype, rows, n, k, epilogue):
             assert torch.equal(l.dx.t, want[0]) if dx else torch.equal(l.dw.t, want[1])
 
 
+@pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
+@pytest.mark.parametrize("rows,n,k", [(1, 768, 768), (3, 576, 4096), (64, 768, 768), (200, 768, 768), (100, 1024, 1024), (20, 8192, 2048)])
+@pytest.mark.parametrize("epilogue", [0, 2, 3])
+@pytest.mark.parametrize("relu_x", [False, True])
+def test_both_products_of_few_rows(dtype, rows, n, k, epilogue, relu_x):
+    p = zo_amd.zo_kernel_linear_grad_plan(rows, n, k, epilogue)
+    assert p["both"] == (64, 64) and (p["dx_shares"] > 1) == (n == 8192)
+    l = Layer(dtype, rows, n, k, epilogue, relu_x)
+    l.run()
+    torch.cuda.synchronize()
+    assert l.whole()
+    l.check(slice(None, None, max(1, min(rows, n) // 50)))
+    want = [t.clone() for t in (l.dx.t, l.dw.t)]
+    l.run(dw=False, db=False)
+    l.run(dx=False, db=False)
+    torch.cuda.synchronize()
+    assert torch.equal(l.dx.t, want[0]) and torch.equal(l.dw.t, want[1])
+
+
 def test_plans_kept_stay_their_sizes_own():
     """More sizes than a thread keeps, in turn and over again, from two threads: the same bits as alone."""
     import threading
