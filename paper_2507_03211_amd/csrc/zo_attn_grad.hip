@@ -210,11 +210,6 @@ __device__ __forceinline__ Item item_of(int block, int pairs)
     return {block % row, block / row};
 }
 
-// Both launches work their rows in units of 32 against 32, software-pipelined, since the one or two wavefronts of a SIMD leave little else to
-// hide an instruction's wait behind: between two multiplies stand a share of the vector arithmetic of a unit whose products are there and the
-// LDS reads of fragments some multiplies ahead (the sched_barriers pin that order).  LDS answers a wavefront in order, so that what is needed soon must
-// not be asked for behind what is not: minus logsumexp and minus D, which S and dP start from, are read a unit ahead, straight into their registers.
-// A barrier for every two units (for each: queries and keys of 4 x 2048, 40 heads of 128 318 and 452 us, without any 260 and 395).
 __device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // word i of two fragments
 {
     uint4 &f = w[i >> 2];
@@ -225,6 +220,9 @@ __device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // wo
 }
 
 // ------------------------------------------------------------------ queries
+// Units of 32 keys, software-pipelined: between two multiplies stand a share of the vector arithmetic of a unit whose products are there and the LDS reads of
+// fragments some multiplies ahead (the sched_barriers pin that order).  LDS answers a wavefront in order, so that what is needed soon must not be
+// asked for behind what is not.  A barrier for every two units (for each: 4 x 2048, 40 heads of 128 318 us, without any 260).
 // Two workgroups to a CU, 232 registers a lane at 128 channels.  4 x 2048, 40 heads of 128, bf16: 290 us, three products of the seven at 0.89 PFLOP/s counting
 // what the mask leaves; 16 x 512, 12 of 64: 26.4; fp16 8 x 131, 32 of 80: 15, where it is loads, D and the units' latency one after another (32 MB
 // are 6.5 us of copying; tiles' loads issued ahead of the queries' own made no difference).
@@ -415,20 +413,21 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 }
 
 // ------------------------------------------------------------------ keys
-// dK and dV take 2 DH / 32 accumulators of 16 registers: one workgroup to a CU from 112 channels on, so that a unit's exponentials, conversions and LDS
-// reads have only its own multiplies to stand behind.  4 x 2048, 40 heads of 128, bf16: 455 us, four products of the seven at 0.76 PFLOP/s; 16 x 512, 12 of 64: 32;
-// fp16 8 x 131, 32 of 80: 15.  P is rounded for dV's product alone: dS from the rounded P has an
-// error against 64 bits of 0.0026 of itself (bf16) where this has 0.0024 and fp32 scores 0.0017.
+// 32 queries at a time: S, dP beside P's exponentials, then dV and dK.  Two wavefronts per SIMD, whose waits each other's multiplies fill, are worth more than
+// one whose own are pipelined: at 128 channels dK, dV, K and V leave 64 of 256 registers for the rest, so that nothing is held ahead but two
+// fragments (pinned: the compiler's own order spills there, 674 us).  Pipelined over two units, one wavefront per SIMD with 386 registers / here, us of the whole
+// call in bf16: 4 x 2048, 40 heads of 128 742 / 657, of 112 720 / 635, of 96 582 / 535, of 64 350 / 345; 16 x 512, 12 of 64 54.1 / 51.7; fp16 8 x 131, 32 of 80
+// 36.3 / 35.3.
 template <int DT, int DH>
-__global__ __launch_bounds__(256, DH <= 96 ? 2 : 1) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
+__global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
                                                                 const float *__restrict__ delta, const float *__restrict__ lse, const RowTops *__restrict__ tops,
                                                                 int seq, int n_heads, int pairs, int tiles)
 {
     using T = TileShape<DH>;
-    constexpr int KS = T::KS, CT = T::CT, R = DH == 80 || DH == 96 ? 2 : 4;
+    constexpr int KS = T::KS, CT = T::CT, R = 2;
     constexpr int kShift = DT == kFP16 ? 14 : 0;               // probabilities carry 2^kShift: down to 2^-28 they are normal numbers
-    __shared__ __attribute__((aligned(256))) u32x4 qs[3][T::PIECES], os[3][T::PIECES];
-    __shared__ float rows[3][2][kTile];                   // logsumexp and D of a tile's queries
+    __shared__ __attribute__((aligned(256))) u32x4 qs[2][T::PIECES], os[2][T::PIECES];
+    __shared__ float rows[2][2][kTile];                         // minus logsumexp and minus D of a tile's queries
     const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
     const int s = item.pair / n_heads, head = item.pair % n_heads, d = n_heads * DH, ld = 3 * d;
@@ -449,126 +448,83 @@ __global__ __launch_bounds__(256, DH <= 96 ? 2 : 1) void attn_grad_keys_kernel(c
     }
     const TileReader<DH> read(lane);
     const TileLoader<DH> load_q(ld, lane, wave), load_o(d, lane, wave);
-    const int t0 = k0 / kTile, n_tiles = (seq + kTile - 1) / kTile, n_units = (seq + 31) / 32, u_first = w0 / 32;
-    auto load = [&](int t, int stage) {
+    const int t0 = k0 / kTile, n_tiles = (seq + kTile - 1) / kTile;
+    auto load = [&](int t) {
         if (t >= n_tiles) return;
-        load_q.load(qs[stage], base, t * kTile, seq);
-        load_o.load(os[stage], obase, t * kTile, seq);
+        load_q.load(qs[t & 1], base, t * kTile, seq);
+        load_o.load(os[t & 1], obase, t * kTile, seq);
         if (wave < 2) {                                          // (queries past the end get zeros: their dO is, too)
             const int left = seq - t * kTile < kTile ? seq - t * kTile : kTile;
             const float *from = (wave ? delta : lse) + (size_t)item.pair * seq + t * kTile;
-            dma4(buffer_of((uint64_t)(uintptr_t)from, (uint32_t)left * 4), 4 * lane, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&rows[stage][wave][0]);
+            dma4(buffer_of((uint64_t)(uintptr_t)from, (uint32_t)left * 4), 4 * lane, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&rows[t & 1][wave][0]);
         }
     };
-    f32x16 dk[CT] = {}, dv[CT] = {}, S[2], dP[2];
-    uint4 qr[R], orow[R], qc[CT], oc[CT], ps[2], ds[2];
-    auto ring = [&](const u32x4 *qt, const u32x4 *ot, int i) {
-        qr[i % R] = read.by_row(qt, i);
-        orow[i % R] = read.by_row(ot, i);
-    };
-    auto multiply = [&](int i, f32x16 &Sn, f32x16 &dPn) {
-        Sn = mfma32<DT>(qr[i % R], kf[i], Sn);
-        dPn = mfma32<DT>(orow[i % R], vf[i], dPn);
-    };
-    // what S and dP of a unit start from: minus logsumexp (over the scaling) and minus D of its queries, four rows at a time
-    auto start = [&](const float (&row)[2][kTile], int half, int g, f32x16 &Sn, f32x16 &dPn) {
-        const float4 l = *(const float4 *)&row[0][32 * half + 8 * g + 4 * fh], v = *(const float4 *)&row[1][32 * half + 8 * g + 4 * fh];
-        Sn[4 * g] = l.x; Sn[4 * g + 1] = l.y; Sn[4 * g + 2] = l.z; Sn[4 * g + 3] = l.w;
-        dPn[4 * g] = v.x; dPn[4 * g + 1] = v.y; dPn[4 * g + 2] = v.z; dPn[4 * g + 3] = v.w;
-    };
-    int tile = t0 - 1, st0 = 2, st1 = 0, st2 = 1;               // as above
-    auto sync = [&] {
-        ++tile;
-        const int left = st0;
-        st0 = st1; st1 = st2; st2 = left;
+    f32x16 dk[CT] = {}, dv[CT] = {};
+    load(t0);
+    for (int t = t0; t < n_tiles; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        load(tile + 2, st2);
-    };
-    // H: the wavefront's j-th unit's lowest bit; which half of its tile unit u is goes by the wavefront
-    auto step = [&](auto hc, int u) {
-        constexpr int H = decltype(hc)::value;
-        f32x16 &Sc = S[H], &dPc = dP[H], &Sn = S[H ^ 1], &dPn = dP[H ^ 1];
-        if (tile < u / 2) sync();
-        const int half = u & 1;
-        const u32x4 *qt = qs[st0] + half * 32 * T::CH, *ot = os[st0] + half * 32 * T::CH;
-        const u32x4 *qt1 = half ? qs[st1] : qs[st0] + 32 * T::CH, *ot1 = half ? os[st1] : os[st0] + 32 * T::CH;
-        const u32x4 *qt2 = qs[st1] + half * 32 * T::CH, *ot2 = os[st1] + half * 32 * T::CH;      // unit u + 2
-        auto pair = [&](int i) {                                // elements i and i + 1
+        load(t + 1);
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int first = t * kTile + 32 * h;
+            if (first < w0) continue;                           // queries that see none of the wavefront's keys
+            const u32x4 *qt = qs[t & 1] + h * 32 * T::CH, *ot = os[t & 1] + h * 32 * T::CH;
+            f32x16 S, dP;                                       // from minus logsumexp (over the scaling) and minus D on
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 l = *(const float4 *)&rows[t & 1][0][32 * h + 8 * g + 4 * fh], v = *(const float4 *)&rows[t & 1][1][32 * h + 8 * g + 4 * fh];
+                S[4 * g] = l.x; S[4 * g + 1] = l.y; S[4 * g + 2] = l.z; S[4 * g + 3] = l.w;
+                dP[4 * g] = v.x; dP[4 * g + 1] = v.y; dP[4 * g + 2] = v.z; dP[4 * g + 3] = v.w;
+            }
+            uint4 ring[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) ring[i] = read.by_row(qt, i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                S = mfma32<DT>(ring[i % R], kf[i], S);
+                __builtin_amdgcn_sched_barrier(0);
+                ring[i % R] = i + R < KS ? read.by_row(qt, i + R) : read.by_row(ot, i + R - KS);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (first == w0) {                                  // queries that do not see the key
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + 4 * fh + (i & 3) < fr) S[i] = -INFINITY;
+            }
+            uint4 ps[2], ds[2];
             auto exponent = [&](float v) { return DT == kFP16 ? __builtin_fmaf(v, sc, (float)kShift) : v * sc; };
-            const float p0 = __builtin_amdgcn_exp2f(exponent(Sc[i])), p1 = __builtin_amdgcn_exp2f(exponent(Sc[i + 1]));
-            auto scaled = [&](float v) { return DT == kFP16 ? v * factor : v; };
-            put(ps, i / 2, pack2<DT>(p0, p1));
-            put(ds, i / 2, pack2<DT>(p0 * scaled(dPc[i]), p1 * scaled(dPc[i + 1])));
-        };
-        // (the last unit's successor is multiplied too, from whatever lies there: nothing reads it)
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            multiply(i, Sn, dPn);
-            __builtin_amdgcn_sched_barrier(0);
-            if (i + R < KS) ring(qt1, ot1, i + R);
-            if (i < CT) {
-                oc[i] = read.by_column(ot, 0, i);
-                qc[i] = read.by_column(qt, 0, i);
-            }
-#pragma unroll
-            for (int p = 4 * i / KS; p < 4 * (i + 1) / KS; ++p) pair(2 * p);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                dv[c] = mfma32<DT>(oc[c], ps[k], dv[c]);
-                dk[c] = mfma32<DT>(qc[c], ds[k], dk[c]);
+            for (int i = 0; i < KS; ++i) {
+                dP = mfma32<DT>(ring[(KS + i) % R], vf[i], dP);
                 __builtin_amdgcn_sched_barrier(0);
-                if (k == 0) {
-                    oc[c] = read.by_column(ot, 16, c);
-                    qc[c] = read.by_column(qt, 16, c);
+                if (i + R < KS) ring[(KS + i) % R] = read.by_row(ot, i + R);
 #pragma unroll
-                    for (int p = 4 + 4 * c / CT; p < 4 + 4 * (c + 1) / CT; ++p) pair(2 * p);
-                } else {                                        // what unit u + 2 starts from, and its first fragments
-#pragma unroll
-                    for (int g = 4 * c / CT; g < 4 * (c + 1) / CT; ++g) start(rows[st1], half, g, Sc, dPc);
-#pragma unroll
-                    for (int i = R * c / CT; i < R * (c + 1) / CT; ++i) ring(qt2, ot2, i);
-                }
+                for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) S[j] = __builtin_amdgcn_exp2f(exponent(S[j]));
                 __builtin_amdgcn_sched_barrier(0);
             }
-    };
-    load(t0, 0);
-    load(t0 + 1, 1);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    {
-        const int stage = u_first / 2 - t0, half = u_first & 1;
+            uint4 oc = read.by_column(ot, 0, 0), qc = read.by_column(qt, 0, 0);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) start(rows[stage], half, g, S[0], dP[0]);
+            for (int j = 0; j < 8; ++j) {
+                auto scaled = [&](float v) { return DT == kFP16 ? v * factor : v; };
+                put(ps, j, pack2<DT>(S[2 * j], S[2 * j + 1]));
+                put(ds, j, pack2<DT>(S[2 * j] * scaled(dP[2 * j]), S[2 * j + 1] * scaled(dP[2 * j + 1])));
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            ring(qs[stage] + half * 32 * T::CH, os[stage] + half * 32 * T::CH, i);
-            multiply(i, S[0], dP[0]);
+            for (int i = 0; i < 2 * CT; ++i) {
+                const int k = i / CT, c = i % CT, n = i + 1;
+                uint4 on{}, qn{};
+                if (n < 2 * CT) { on = read.by_column(ot, 16 * (n / CT), n % CT); qn = read.by_column(qt, 16 * (n / CT), n % CT); }
+                __builtin_amdgcn_sched_barrier(0);
+                dv[c] = mfma32<DT>(oc, ps[k], dv[c]);
+                dk[c] = mfma32<DT>(qc, ds[k], dk[c]);
+                __builtin_amdgcn_sched_barrier(0);
+                oc = on; qc = qn;
+            }
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i)                            // the unit on the diagonal: queries that do not see the key
-            if (8 * (i >> 2) + 4 * fh + (i & 3) < fr) S[0][i] = -INFINITY;
     }
-    while (tile < u_first / 2 && tile + 1 < n_tiles) sync();
-    {
-        const int stage = u_first & 1 ? st1 : st0, half = (u_first & 1) ^ 1;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) start(rows[stage], half, g, S[1], dP[1]);
-#pragma unroll
-        for (int i = 0; i < R; ++i) ring(qs[stage] + half * 32 * T::CH, os[stage] + half * 32 * T::CH, i);
-    }
-    int u = u_first;
-    for (; u + 1 < n_units; u += 2) {
-        step(std::integral_constant<int, 0>{}, u);
-        step(std::integral_constant<int, 1>{}, u + 1);
-    }
-    if (u < n_units) step(std::integral_constant<int, 0>{}, u);
-    while (tile + 1 < n_tiles) sync();                          // for the other wavefronts
     if (key >= seq) return;
     const float k_scale = (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f) / __builtin_sqrtf((float)DH), v_scale = DT == kFP16 ? 0x1p-14f : 1.0f;
     uint16_t *to = dqkv + ((size_t)s * seq + key) * ld + d + head * DH + 4 * fh;
