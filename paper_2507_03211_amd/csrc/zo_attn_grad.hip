@@ -220,23 +220,19 @@ __device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // wo
 }
 
 // ------------------------------------------------------------------ queries
-// Units of 32 keys, software-pipelined: between two multiplies stand a share of the vector arithmetic of a unit whose products are there and the LDS reads of
-// fragments some multiplies ahead (the sched_barriers pin that order).  LDS answers a wavefront in order, so that what is needed soon must not be
-// asked for behind what is not.  A barrier for every two units (for each: 4 x 2048, 40 heads of 128 318 us, without any 260).
-// Two workgroups to a CU, 232 registers a lane at 128 channels.  4 x 2048, 40 heads of 128, bf16: 290 us, three products of the seven at 0.89 PFLOP/s counting
-// what the mask leaves; 16 x 512, 12 of 64: 26.4; fp16 8 x 131, 32 of 80: 15, where it is loads, D and the units' latency one after another (32 MB
-// are 6.5 us of copying; tiles' loads issued ahead of the queries' own made no difference).
+// 32 keys at a time: S, dP beside the exponentials, dQ; two wavefronts per SIMD (211 registers at 128 channels).  Pipelined over two
+// units, with keys in three stages, it is no faster: 4 x 2048, 40 heads of 128 656 us of the whole call in bf16 both ways, of 80 500 / 491, 16 x 512, 12 of 64 52.6 / 51.4,
+// fp16 8 x 131, 32 of 80 35.9 / 35.1; three workgroups to a CU at 96 channels 532 / 546, four at 64 347 / 413 (registers).
 template <int DT, int DH>
 __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ out, const uint16_t *__restrict__ dout,
                                                                    uint16_t *__restrict__ dqkv, float *__restrict__ delta, float *__restrict__ lse, const RowTops *__restrict__ tops,
                                                                    int seq, int n_heads, int pairs, int tiles)
 {
     using T = TileShape<DH>;
-    constexpr int KS = T::KS, CT = T::CT, R = 2;
+    constexpr int KS = T::KS, CT = T::CT, R = 4;
     // the reference is raised when a scaled score passes it by this much: unnormalised probabilities are 2^kRaise at most
     constexpr int kRaise = 4;
-    // keys of tiles T and T + 1 and values of T are read while T + 2's and T + 1's arrive
-    __shared__ __attribute__((aligned(256))) u32x4 ks[3][T::PIECES], vs[2][T::PIECES];
+    __shared__ __attribute__((aligned(256))) u32x4 ks[2][T::PIECES], vs[2][T::PIECES];
     const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
     const int s = item.pair / n_heads, head = item.pair % n_heads, d = n_heads * DH, ld = 3 * d;
@@ -245,8 +241,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     const uint16_t *base = qkv + (size_t)s * seq * ld + head * DH;
     const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
     const int row_tiles = (seq + kTile - 1) / kTile;
-    const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) - kRaise : 0;
-    const float factor = DT == kFP16 ? ldexpf(1.0f, e) : 1.0f;
+    // (fp16: probabilities carry 2^e, and with them dS; so does their sum)
+    const float e = DT == kFP16 ? (float)(scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) - kRaise) : 0.0f;
 
     uint4 qf[KS], of[KS];
     float minus_d = 0.0f;
@@ -273,136 +269,98 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     }
     const TileReader<DH> read(lane);
     const TileLoader<DH> loader(ld, lane, wave);
-    const int last = q0 + kOwn <= seq ? q0 + kOwn : seq, n_tiles = (last + kTile - 1) / kTile, u_last = w0 / 32 < 2 * n_tiles ? w0 / 32 : 2 * n_tiles - 1;
-    auto load_k = [&](int t, int stage) { if (t < n_tiles) loader.load(ks[stage], base + d, t * kTile, seq); };
-    auto load_v = [&](int t) { if (t < n_tiles) loader.load(vs[t & 1], base + 2 * d, t * kTile, seq); };
-    f32x16 acc[CT] = {}, S[2], dP;
-    uint4 kr[R], vr[R], kc[CT], ds[2];
-    float m_run = -INFINITY, moff = 0.0f, thr = -INFINITY, l_lane = 0.0f, top = -INFINITY;
-    // stages of tile T's keys and T + 1's and T + 2's
-    int tile = -1, st0 = 2, st1 = 0, st2 = 1;
-    auto sync = [&] {                                           // on to the next tile
+    const int last = q0 + kOwn <= seq ? q0 + kOwn : seq, n_tiles = (last + kTile - 1) / kTile;
+    auto load = [&](int t) {
+        if (t >= n_tiles) return;
+        loader.load(ks[t & 1], base + d, t * kTile, seq);
+        loader.load(vs[t & 1], base + 2 * d, t * kTile, seq);
+    };
+    f32x16 acc[CT] = {};
+    float m_run = -INFINITY, moff = 0.0f, thr = -INFINITY, l_lane = 0.0f;
+    load(0);
+    for (int t = 0; t < n_tiles; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        ++tile;
-        const int left = st0;
-        st0 = st1; st1 = st2; st2 = left;
-        load_k(tile + 2, st2);
-        load_v(tile + 1);
-    };
-    auto mask = [&](f32x16 &x) {                                // of the unit on the diagonal
+        load(t + 1);
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int first = t * kTile + 32 * h;
+            if (first > w0) break;                              // keys that none of the wavefront's queries sees
+            const u32x4 *kt = ks[t & 1] + h * 32 * T::CH, *vt = vs[t & 1] + h * 32 * T::CH;
+            f32x16 S = {}, dP;
+            uint4 ring[R];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (8 * (i >> 2) + 4 * fh + (i & 3) > fr) x[i] = -INFINITY;
-    };
-    auto maximum = [&](const f32x16 &x) {
-        float t = __builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), x[2]);
-#pragma unroll
-        for (int i = 3; i < 15; i += 2) t = __builtin_fmaxf(__builtin_fmaxf(x[i], x[i + 1]), t);
-        return __builtin_fmaxf(t, x[15]);
-    };
-    auto start = [&] {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) dP[j] = minus_d;
-    };
-    // Step u, with S of unit u there:  dP of unit u | P of unit u;  S of unit u + 1 | dS of unit u;  dQ's products of unit u | the maximum of S
-    auto step = [&](auto hc, int u) {
-        constexpr int H = decltype(hc)::value;                  // u & 1: unit u is half H of its tile
-        f32x16 &Sc = S[H], &Sn = S[H ^ 1];
-        const u32x4 *kt = ks[st0] + H * 32 * T::CH, *vt = vs[tile & 1] + H * 32 * T::CH, *kn = H ? ks[st1] : ks[st0] + 32 * T::CH;
-        if constexpr (H == 0) {                                 // (the other half's were read a unit ago)
-#pragma unroll
-            for (int i = 0; i < R; ++i) vr[i] = read.by_row(vt, i);
-        }
-        if (__builtin_amdgcn_ballot_w64(top > thr) != 0) {
-            float a, b;
-            swap_halves(top, a, b);
-            const float m_new = __builtin_fmaxf(__builtin_fmaxf(a, b), m_run), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
-            l_lane *= alpha;
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
-            m_run = m_new;
-            moff = -m_new * sc;
-            thr = m_new + (float)kRaise / sc;
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-#pragma unroll
-            for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) {
-                Sc[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sc[j], sc, moff));
-                l_lane += Sc[j];
-            }
-            asm volatile("" : "+v"(l_lane));
+            for (int i = 0; i < R; ++i) ring[i] = read.by_row(kt, i);
             __builtin_amdgcn_sched_barrier(0);
-            dP = mfma32<DT>(vr[i % R], of[i], dP);
-            __builtin_amdgcn_sched_barrier(0);
-            if (i + R < KS) vr[i % R] = read.by_row(vt, i + R);
-            // (the last unit's successor is multiplied too, from whatever lies there: nothing reads it)
-            if (i + R >= KS) kr[i + R - KS] = read.by_row(kn, i + R - KS);
-        }
-        const f32x16 zero = {};
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            Sn = mfma32<DT>(kr[i % R], qf[i], i == 0 ? zero : Sn);
-            __builtin_amdgcn_sched_barrier(0);
-            if (i + R < KS) kr[i % R] = read.by_row(kn, i + R);
-            if (i < CT) kc[i] = read.by_column(kt, 0, i);
-#pragma unroll
-            for (int j = 8 * i / KS; j < 8 * (i + 1) / KS; ++j) {
-                auto scaled = [&](float v) { return DT == kFP16 ? v * factor : v; };
-                put(ds, j, pack2<DT>(Sc[2 * j] * scaled(dP[2 * j]), Sc[2 * j + 1] * scaled(dP[2 * j + 1])));
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        start();
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                acc[c] = mfma32<DT>(kc[c], ds[k], acc[c]);
+            for (int i = 0; i < KS; ++i) {
+                S = mfma32<DT>(ring[i % R], qf[i], S);
                 __builtin_amdgcn_sched_barrier(0);
-                if (k == 0) kc[c] = read.by_column(kt, 16, c);
-                if constexpr (H == 0) {
-                    if (k == 1) {
+                ring[i % R] = i + R < KS ? read.by_row(kt, i + R) : read.by_row(vt, i + R - KS);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
-                        for (int i = R * c / CT; i < R * (c + 1) / CT; ++i) vr[i] = read.by_row(vt + 32 * T::CH, i);
-                    }
+            for (int j = 0; j < 16; ++j) dP[j] = minus_d;
+            if (first == w0) {                                  // keys behind the query
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + 4 * fh + (i & 3) > fr) S[i] = -INFINITY;
+            }
+            float top = __builtin_fmaxf(__builtin_fmaxf(S[0], S[1]), S[2]);
+#pragma unroll
+            for (int i = 3; i < 15; i += 2) top = __builtin_fmaxf(__builtin_fmaxf(S[i], S[i + 1]), top);
+            top = __builtin_fmaxf(top, S[15]);
+            if (__builtin_amdgcn_ballot_w64(top > thr) != 0) {
+                float a, b;
+                swap_halves(top, a, b);
+                const float m_new = __builtin_fmaxf(__builtin_fmaxf(a, b), m_run), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
+                l_lane *= alpha;
+#pragma unroll
+                for (int c = 0; c < CT; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
+                m_run = m_new;
+                moff = DT == kFP16 ? __builtin_fmaf(-m_new, sc, e) : -m_new * sc;
+                thr = m_new + (float)kRaise / sc;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                dP = mfma32<DT>(ring[(KS + i) % R], of[i], dP);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i + R < KS) ring[(KS + i) % R] = read.by_row(vt, i + R);
+#pragma unroll
+                for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) {
+                    S[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j], sc, moff));
+                    l_lane += S[j];
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-        if (u + 1 == u_last) mask(Sn);
-        top = maximum(Sn);
-    };
-    load_k(0, 0);
-    load_v(0);
-    load_k(1, 1);
-    sync();
+            uint4 ds[2], kc = read.by_column(kt, 0, 0);
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-        const f32x16 zero = {};
-        S[0] = mfma32<DT>(read.by_row(ks[0], i), qf[i], i == 0 ? zero : S[0]);
+            for (int j = 0; j < 8; ++j) {
+                put(ds, j, pack2<DT>(S[2 * j] * dP[2 * j], S[2 * j + 1] * dP[2 * j + 1]));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 2 * CT; ++i) {
+                const int n = i + 1;
+                uint4 kn{};
+                if (n < 2 * CT) kn = read.by_column(kt, 16 * (n / CT), n % CT);
+                __builtin_amdgcn_sched_barrier(0);
+                acc[i % CT] = mfma32<DT>(kc, ds[i / CT], acc[i % CT]);
+                __builtin_amdgcn_sched_barrier(0);
+                kc = kn;
+            }
+        }
     }
-    start();
-    if (u_last == 0) mask(S[0]);
-    top = maximum(S[0]);
-    int u = 0;
-    for (; u < u_last; u += 2) {
-        step(std::integral_constant<int, 0>{}, u);
-        step(std::integral_constant<int, 1>{}, u + 1);
-        if (tile + 1 < n_tiles) sync();
-    }
-    if (u == u_last) step(std::integral_constant<int, 0>{}, u);
-    while (tile + 1 < n_tiles) sync();                          // for the other wavefronts
     if (q >= seq) return;
     float a, b;
     swap_halves(l_lane, a, b);
     const float l = a + b;
     // as the other launch's scores start from it: minus logsumexp, before the scaling
-    if (fh == 0) lse[(size_t)item.pair * seq + q] = -(m_run + __builtin_amdgcn_logf(l) / sc);
-    const float scale = 1.0f / (l * __builtin_sqrtf((float)DH)) * (DT == kFP16 ? ldexpf(1.0f, -e) : 1.0f);
+    if (fh == 0) lse[(size_t)item.pair * seq + q] = -(m_run + (__builtin_amdgcn_logf(l) - e) / sc);
+    const float scale = 1.0f / (l * __builtin_sqrtf((float)DH));
     uint16_t *dq = dqkv + ((size_t)s * seq + q) * ld + head * DH + 4 * fh;
 #pragma unroll
     for (int c = 0; c < CT; ++c)
