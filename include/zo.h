@@ -451,7 +451,8 @@ int zo_kernel_linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *pl
  * needed.  2-byte dtypes: d_head a multiple of 8, buffers 16-byte aligned (ZO_EINVAL otherwise); heads of 64, 80, 96, 112 and 128 run on the matrix
  * cores, which take P and dS rounded to the type (ZO_FP16: scaled so that no finite P or dS leaves the type's range), others on a slower kernel.  An
  * element of qkv, out or dout that is not finite makes gradients of its sequence and head that are none, those of earlier queries that do not
- * see it among them; other sequences and heads do not see it.  Any length up to 2^20 positions; up to 2^20 channels and 2^30 rows, and no more
+ * see it among them; other sequences and heads do not see it.  On the matrix cores D is summed from P and dout v^T where a sequence has up to 128
+ * positions, and `out` is not read.  Any length up to 2^20 positions; up to 2^20 channels and 2^30 rows, and no more
  * workgroups than a launch holds (2^24 tiles of 64 rows of one head; 2^25 rows on the slower kernel): ZO_EINVAL, and 0 scratch bytes, beyond. */
 size_t zo_kernel_attention_grad_scratch_bytes(int dtype, int n_seq, int seq, int n_heads, int d_head);
 int zo_kernel_attention_grad(const void *qkv, const void *out, const void *dout, void *dqkv, void *scratch, int dtype, int n_seq, int seq,

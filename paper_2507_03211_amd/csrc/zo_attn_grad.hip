@@ -50,6 +50,7 @@ __device__ __forceinline__ void swap_halves(float x, float &a, float &b)
     b = __uint_as_float(r[1]);
 }
 
+constexpr int kShort = 128;                 // positions of a sequence up to which D is summed from P dP (attn_grad_queries_kernel)
 constexpr int kOwn = 128, kTile = 64;      // rows of a workgroup's own (32 a wavefront), rows of a tile that streams through LDS
 
 // fp16: dS = P (dP - D) may lie anywhere: |dP| and |D| are at most A B, with A the largest norm of a row of dO and B of a row of V in the
@@ -223,7 +224,11 @@ __device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // wo
 // 32 keys at a time: S, dP beside the exponentials, dQ; two wavefronts per SIMD (211 registers at 128 channels).  Pipelined over two
 // units, with keys in three stages, it is no faster: 4 x 2048, 40 heads of 128 656 us of the whole call in bf16 both ways, of 80 500 / 491, 16 x 512, 12 of 64 52.6 / 51.4,
 // fp16 8 x 131, 32 of 80 35.9 / 35.1; three workgroups to a CU at 96 channels 532 / 546, four at 64 347 / 413 (registers).
-template <int DT, int DH>
+// D: of sequences up to kShort positions (SHORT) the sum of P dP, by a pass ahead; of longer ones that of dO times `out`, whose rounding to 16 bits then makes the
+// gradients little worse.  Error of all three against 64 bits over that of fp32 arithmetic, both rounded: by `out` 1.67 at 2 positions, 1.57 at 8, 1.51 at 16,
+// 1.48 at 128, 1.46 at 300; by the pass 1.23 - 1.44.  us of the whole call by `out` / by the pass: 8 x 64, 32 heads of 80 fp16 19.4 / 19.2, 8 x 128 bf16 23.3 / 24.9,
+// 16 x 128, 40 of 128 73.2 / 70.9, 256 x 64, 12 of 64 78.4 / 72.7.
+template <int DT, int DH, bool SHORT>
 __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ out, const uint16_t *__restrict__ dout,
                                                                    uint16_t *__restrict__ dqkv, float *__restrict__ delta, float *__restrict__ lse, const RowTops *__restrict__ tops,
                                                                    int seq, int n_heads, int pairs, int tiles)
@@ -245,27 +250,14 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     const float e = DT == kFP16 ? (float)(scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) - kRaise) : 0.0f;
 
     uint4 qf[KS], of[KS];
-    float minus_d = 0.0f;
+    const size_t at = ((size_t)s * seq + (q < seq ? q : 0)) * d + head * DH + 8 * fh;
     {
-        const size_t at = ((size_t)s * seq + (q < seq ? q : 0)) * d + head * DH + 8 * fh;
-        const uint16_t *qp = base + (size_t)(q < seq ? q : 0) * ld + 8 * fh, *gp = dout + at, *op = out + at;
-        uint4 o[KS];
+        const uint16_t *qp = base + (size_t)(q < seq ? q : 0) * ld + 8 * fh, *gp = dout + at;
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
-            o[i] = q < seq ? *(const uint4 *)(op + 16 * i) : uint4{0, 0, 0, 0};
             of[i] = q < seq ? *(const uint4 *)(gp + 16 * i) : uint4{0, 0, 0, 0};
             qf[i] = q < seq ? *(const uint4 *)(qp + 16 * i) : uint4{0, 0, 0, 0};
         }
-        auto two = [&](uint32_t a, uint32_t b) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 16) minus_d = __builtin_fmaf(-Prec<DT>::a2acc((uint16_t)(a >> e)), Prec<DT>::a2acc((uint16_t)(b >> e)), minus_d);
-        };
-#pragma unroll
-        for (int i = 0; i < KS; ++i) { two(o[i].x, of[i].x); two(o[i].y, of[i].y); two(o[i].z, of[i].z); two(o[i].w, of[i].w); }
-        float a, b;
-        swap_halves(minus_d, a, b);
-        minus_d = a + b;
-        if (fh == 0 && q < seq) delta[(size_t)item.pair * seq + q] = minus_d;
     }
     const TileReader<DH> read(lane);
     const TileLoader<DH> loader(ld, lane, wave);
@@ -275,6 +267,68 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
         loader.load(ks[t & 1], base + d, t * kTile, seq);
         loader.load(vs[t & 1], base + 2 * d, t * kTile, seq);
     };
+    auto mask = [&](f32x16 &x) {                                // keys behind the query, of the unit on the diagonal
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (8 * (i >> 2) + 4 * fh + (i & 3) > fr) x[i] = -INFINITY;
+    };
+    auto maximum = [&](const f32x16 &x) {
+        float top = __builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), x[2]);
+#pragma unroll
+        for (int i = 3; i < 15; i += 2) top = __builtin_fmaxf(__builtin_fmaxf(x[i], x[i + 1]), top);
+        return __builtin_fmaxf(top, x[15]);
+    };
+    float minus_d = 0.0f, a, b;
+    if constexpr (SHORT) {
+        float m = -INFINITY, l = 0.0f, sum = 0.0f;
+        load(0);
+        for (int t = 0; t < n_tiles; ++t) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            load(t + 1);
+            for (int h = 0; h < 2; ++h) {
+                const int first = t * kTile + 32 * h;
+                if (first > w0) break;
+                const u32x4 *kt = ks[t & 1] + h * 32 * T::CH, *vt = vs[t & 1] + h * 32 * T::CH;
+                f32x16 S = {}, dP = {};
+#pragma unroll
+                for (int i = 0; i < KS; ++i) S = mfma32<DT>(read.by_row(kt, i), qf[i], S);
+#pragma unroll
+                for (int i = 0; i < KS; ++i) dP = mfma32<DT>(read.by_row(vt, i), of[i], dP);
+                if (first == w0) mask(S);
+                swap_halves(maximum(S), a, b);
+                const float m_new = __builtin_fmaxf(__builtin_fmaxf(a, b), m), alpha = __builtin_amdgcn_exp2f((m - m_new) * sc);
+                l *= alpha;
+                sum *= alpha;
+                m = m_new;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j], sc, -m * sc));
+                    l += p;
+                    sum = __builtin_fmaf(p, dP[j], sum);
+                }
+            }
+        }
+        __syncthreads();                                        // (the tiles are loaded again)
+        swap_halves(l, a, b);
+        l = a + b;
+        swap_halves(sum, a, b);
+        minus_d = -(a + b) / l;
+    } else {
+        const uint16_t *op = out + at;
+        uint4 o[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) o[i] = q < seq ? *(const uint4 *)(op + 16 * i) : uint4{0, 0, 0, 0};
+        auto two = [&](uint32_t a, uint32_t b) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 16) minus_d = __builtin_fmaf(-Prec<DT>::a2acc((uint16_t)(a >> e)), Prec<DT>::a2acc((uint16_t)(b >> e)), minus_d);
+        };
+#pragma unroll
+        for (int i = 0; i < KS; ++i) { two(o[i].x, of[i].x); two(o[i].y, of[i].y); two(o[i].z, of[i].z); two(o[i].w, of[i].w); }
+        swap_halves(minus_d, a, b);
+        minus_d = a + b;
+    }
+    if (fh == 0 && q < seq) delta[(size_t)item.pair * seq + q] = minus_d;
     f32x16 acc[CT] = {};
     float m_run = -INFINITY, moff = 0.0f, thr = -INFINITY, l_lane = 0.0f;
     load(0);
@@ -301,17 +355,9 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
             }
 #pragma unroll
             for (int j = 0; j < 16; ++j) dP[j] = minus_d;
-            if (first == w0) {                                  // keys behind the query
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (8 * (i >> 2) + 4 * fh + (i & 3) > fr) S[i] = -INFINITY;
-            }
-            float top = __builtin_fmaxf(__builtin_fmaxf(S[0], S[1]), S[2]);
-#pragma unroll
-            for (int i = 3; i < 15; i += 2) top = __builtin_fmaxf(__builtin_fmaxf(S[i], S[i + 1]), top);
-            top = __builtin_fmaxf(top, S[15]);
+            if (first == w0) mask(S);
+            const float top = maximum(S);
             if (__builtin_amdgcn_ballot_w64(top > thr) != 0) {
-                float a, b;
                 swap_halves(top, a, b);
                 const float m_new = __builtin_fmaxf(__builtin_fmaxf(a, b), m_run), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
                 l_lane *= alpha;
@@ -355,7 +401,6 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
         }
     }
     if (q >= seq) return;
-    float a, b;
     swap_halves(l_lane, a, b);
     const float l = a + b;
     // as the other launch's scores start from it: minus logsumexp, before the scaling
@@ -510,7 +555,8 @@ hipError_t attn_grad(const uint16_t *qkv, const uint16_t *out, const uint16_t *d
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     const dim3 grid((pairs + 7) / 8 * 8 * tiles);
-    attn_grad_queries_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, out, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
+    auto queries = seq <= kShort ? attn_grad_queries_kernel<DT, DH, true> : attn_grad_queries_kernel<DT, DH, false>;
+    queries<<<grid, dim3(256), 0, s>>>(qkv, out, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
     if ((err = hipGetLastError()) != hipSuccess) return err;
     attn_grad_keys_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
     return hipGetLastError();

@@ -65,6 +65,8 @@ class Attention:
         dp_abs, d_abs = do.abs() @ v.abs().transpose(1, 2), (do.abs() * o.abs()).sum(2, keepdim=True)
         # D: `out` is off by its rounding and by what the forward call's own P was (rounded too, on the matrix cores)
         d_off = (3 * u16 + terms * u) * (do.abs() * (p @ v.abs())).sum(2, keepdim=True) + terms * u * d_abs
+        if matrix and self.seq <= 128:                          # (D is summed from P dP there, P in fp32)
+            d_off = (p * (p_rel + terms * u) * dp_abs).sum(2, keepdim=True)
         ds_off = ds.abs() * (p_rel + (2 * u16 if matrix else 0.0)) + p * (d_off + terms * u * (dp_abs + d_abs))
         p_off = p * (p_rel + (u16 if matrix else 0.0))
         if matrix and self.dtype == zi.FP16:
@@ -96,6 +98,18 @@ def ran(a):
 @pytest.mark.parametrize("seq", [1, 2, 31, 32, 33, 63, 64, 65, 96, 127, 128, 129, 200, 257, 511])
 def test_lengths(dtype, d_head, seq):
     ran(Attention(dtype, 3, seq, 3, d_head)).check()
+
+
+@pytest.mark.parametrize("dtype", [zi.BF16, zi.FP16])
+@pytest.mark.parametrize("d_head", MATRIX)
+@pytest.mark.parametrize("seq", [1, 33, 64, 65, 128, 129])
+def test_short_sequences_do_without_out(dtype, d_head, seq):
+    a = ran(Attention(dtype, 3, seq, 2, d_head, size=2.0))
+    a.check()
+    want = a.dqkv.t.clone()
+    a.out.fill_(math.nan)
+    ran(a)
+    assert torch.equal(a.dqkv.t, want) if seq <= 128 else bool(torch.isnan(a.dqkv.t).any())
 
 
 @pytest.mark.parametrize("dtype,d_head", [(zi.FP32, c) for c in (1, 4, 16, 33, 64, 128)] + [(t, c) for t in (zi.BF16, zi.FP16) for c in (8, 40, 72, 120)])
