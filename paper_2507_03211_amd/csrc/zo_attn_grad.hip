@@ -5,7 +5,7 @@
 //
 // Matrix path (16-bit types, heads of 64, 80, 96, 112, 128), two launches, and in fp16 one before them that finds what bounds dS (below):
 //   queries  a wavefront's 32 queries against the keys they see: D, S, dP, dQ.  The softmax runs along (one pass, a reference that is raised
-//            as scores pass it), so that logsumexp comes out at the end, for the other launch
+//            as scores pass it), so that the reference and the sum come out at the end, for the other launch
 //   keys     a wavefront's 32 keys against the queries that see them: S, dP, dV, dK
 // Seven products instead of five: with dQ from the launch over the keys it would take sums of other workgroups', in memory and in an order
 // that changes.  Both are computed so that a lane owns a column of the scores (a query there, a key here), and the contraction of the second
@@ -56,6 +56,8 @@ constexpr int kOwn = 128, kTile = 64;      // rows of a workgroup's own (32 a wa
 // fp16: dS = P (dP - D) may lie anywhere: |dP| and |D| are at most A B, with A the largest norm of a row of dO and B of a row of V in the
 // sequence and head, so 2^e dS with 2^e = 2^14 / (2 A B) rounded down is within the type whatever P is, and numbers 2^28 below that bound are still
 // normal ones.  2^-e is taken out of the fp32 sums.  bf16 has fp32's range: e = 0.
+// What the keys' launch's probabilities carry: 2^kShift, with which they are normal numbers of fp16 down to 2^-28.
+template <int DT> constexpr int kShift = DT == kFP16 ? 14 : 0;
 struct RowTops { float out2, value2; };                         // of 64 rows: the largest |dO|^2 and |V|^2
 __device__ __forceinline__ int scale_exponent(const RowTops *tops, int tiles)
 {
@@ -176,16 +178,18 @@ __device__ __forceinline__ u32x4 buffer_of(uint64_t first, uint32_t bytes)
     return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)first), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(first >> 32)),
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
-template <int DH> struct TileLoader : TileShape<DH> {
+// LEAN (rows of 16 pieces): a register instead of one a load.  A load's rows lie four behind the last one's, and its swizzle differs in the two lowest bits.
+template <int DH, bool LEAN = false> struct TileLoader : TileShape<DH> {
     using T = TileShape<DH>;
     static constexpr int LOADS = T::PIECES / 256;               // of a wavefront
-    uint32_t off[LOADS];
+    static_assert(!LEAN || (T::CHD == 16 && LOADS == 4), "rows of 256 bytes, at multiples of these from one another");
+    uint32_t off[LEAN ? 1 : LOADS];
     uint32_t ld;
     int wave;
     __device__ __forceinline__ TileLoader(int ld_, int lane, int wave_) : ld((uint32_t)ld_ * 2u), wave(wave_)
     {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
+        for (int i = 0; i < (LEAN ? 1 : LOADS); ++i) {
             const int p = 64 * (LOADS * wave + i) + lane, r = p / T::CH;
             off[i] = (uint32_t)r * ld + (uint32_t)T::in_row((p % T::CH) ^ T::swizzle(r)) * 16u;
         }
@@ -196,8 +200,10 @@ template <int DH> struct TileLoader : TileShape<DH> {
         const int left = seq - row0 < kTile ? seq - row0 : kTile;
         const u32x4 rows = buffer_of((uint64_t)(uintptr_t)first + (uint64_t)row0 * ld, (uint32_t)(left - 1) * ld + DH * 2);
         const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4 *)tile;
+        uint32_t at = off[0];
+        if constexpr (LEAN) asm volatile("" : "+v"(at));         // (or the others are worked out ahead of the loop, and kept)
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) dma16(rows, off[i], lds + (uint32_t)(LOADS * wave + i) * 1024u);
+        for (int i = 0; i < LOADS; ++i) dma16(rows, LEAN ? (at ^ (uint32_t)(16 * i)) + (uint32_t)(4 * i) * ld : off[i], lds + (uint32_t)(LOADS * wave + i) * 1024u);
     }
 };
 
@@ -230,13 +236,14 @@ __device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // wo
 // 16 x 128, 40 of 128 73.2 / 70.9, 256 x 64, 12 of 64 78.4 / 72.7.
 template <int DT, int DH, bool SHORT>
 __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ out, const uint16_t *__restrict__ dout,
-                                                                   uint16_t *__restrict__ dqkv, float *__restrict__ delta, float *__restrict__ lse, const RowTops *__restrict__ tops,
+                                                                   uint16_t *__restrict__ dqkv, float *__restrict__ rows, const RowTops *__restrict__ tops,
                                                                    int seq, int n_heads, int pairs, int tiles)
 {
     using T = TileShape<DH>;
     constexpr int KS = T::KS, CT = T::CT, R = 4;
     // the reference is raised when a scaled score passes it by this much: unnormalised probabilities are 2^kRaise at most
     constexpr int kRaise = 4;
+    const float lazy = (float)kRaise * __builtin_sqrtf((float)DH) / 1.4426950408889634f;
     __shared__ __attribute__((aligned(256))) u32x4 ks[2][T::PIECES], vs[2][T::PIECES];
     const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
@@ -247,7 +254,10 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
     const int row_tiles = (seq + kTile - 1) / kTile;
     // (fp16: probabilities carry 2^e, and with them dS; so does their sum)
-    const float e = DT == kFP16 ? (float)(scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) - kRaise) : 0.0f;
+    const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * row_tiles, row_tiles) - kRaise : 0;
+    // A score against the reference, as an exponent of two.  The difference first: it is exact where it counts.  A product of the reference and sc would be
+    // off by its last place, which for large scores is all of P
+    auto exponent = [&](float s, float m) { return DT == kFP16 ? __builtin_fmaf(s - m, sc, (float)e) : (s - m) * sc; };
 
     uint4 qf[KS], of[KS];
     const size_t at = ((size_t)s * seq + (q < seq ? q : 0)) * d + head * DH + 8 * fh;
@@ -303,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
                 m = m_new;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j], sc, -m * sc));
+                    const float p = __builtin_amdgcn_exp2f((S[j] - m) * sc);
                     l += p;
                     sum = __builtin_fmaf(p, dP[j], sum);
                 }
@@ -328,9 +338,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
         swap_halves(minus_d, a, b);
         minus_d = a + b;
     }
-    if (fh == 0 && q < seq) delta[(size_t)item.pair * seq + q] = minus_d;
     f32x16 acc[CT] = {};
-    float m_run = -INFINITY, moff = 0.0f, thr = -INFINITY, l_lane = 0.0f;
+    float m_run = -INFINITY, l_lane = 0.0f;
     load(0);
     for (int t = 0; t < n_tiles; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -356,9 +365,9 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 #pragma unroll
             for (int j = 0; j < 16; ++j) dP[j] = minus_d;
             if (first == w0) mask(S);
-            const float top = maximum(S);
-            if (__builtin_amdgcn_ballot_w64(top > thr) != 0) {
-                swap_halves(top, a, b);
+            const float most = maximum(S);
+            if (__builtin_amdgcn_ballot_w64(most - m_run > lazy) != 0) {
+                swap_halves(most, a, b);
                 const float m_new = __builtin_fmaxf(__builtin_fmaxf(a, b), m_run), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
                 l_lane *= alpha;
 #pragma unroll
@@ -366,8 +375,6 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
                 m_run = m_new;
-                moff = DT == kFP16 ? __builtin_fmaf(-m_new, sc, e) : -m_new * sc;
-                thr = m_new + (float)kRaise / sc;
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -377,7 +384,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
                 if (i + R < KS) ring[(KS + i) % R] = read.by_row(vt, i + R);
 #pragma unroll
                 for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) {
-                    S[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j], sc, moff));
+                    S[j] = __builtin_amdgcn_exp2f(exponent(S[j], m_run));
                     l_lane += S[j];
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -403,8 +410,12 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
     if (q >= seq) return;
     swap_halves(l_lane, a, b);
     const float l = a + b;
-    // as the other launch's scores start from it: minus logsumexp, before the scaling
-    if (fh == 0) lse[(size_t)item.pair * seq + q] = -(m_run + (__builtin_amdgcn_logf(l) - e) / sc);
+    // for the other launch, in two numbers: in one, as a logsumexp, the sum would be rounded to the scores' last place
+    if (fh == 0) {
+        const size_t row = (size_t)item.pair * seq + q;
+        *(f32x2 *)(rows + 2 * row) = f32x2{m_run, (float)kShift<DT> - __builtin_amdgcn_logf(ldexpf(l, -e))};
+        rows[2 * (size_t)pairs * seq + row] = minus_d;
+    }
     const float scale = 1.0f / (l * __builtin_sqrtf((float)DH));
     uint16_t *dq = dqkv + ((size_t)s * seq + q) * ld + head * DH + 4 * fh;
 #pragma unroll
@@ -424,14 +435,13 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 // 36.3 / 35.3.
 template <int DT, int DH>
 __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
-                                                                const float *__restrict__ delta, const float *__restrict__ lse, const RowTops *__restrict__ tops,
+                                                                const float *__restrict__ rows, const RowTops *__restrict__ tops,
                                                                 int seq, int n_heads, int pairs, int tiles)
 {
     using T = TileShape<DH>;
-    constexpr int KS = T::KS, CT = T::CT, R = 2;
-    constexpr int kShift = DT == kFP16 ? 14 : 0;               // probabilities carry 2^kShift: down to 2^-28 they are normal numbers
+    constexpr int KS = T::KS, CT = T::CT, R = 2, AHEAD = KS < 7 ? 2 : 1;
     __shared__ __attribute__((aligned(256))) u32x4 qs[2][T::PIECES], os[2][T::PIECES];
-    __shared__ float rows[2][2][kTile];                         // minus logsumexp and minus D of a tile's queries
+    __shared__ __attribute__((aligned(16))) float refs[2][kTile][2], minus_d[2][kTile];   // of a tile's queries: reference and kShift - logarithm of the sum, minus D
     const Item item = item_of((int)blockIdx.x, pairs);
     if (item.pair >= pairs) return;
     const int s = item.pair / n_heads, head = item.pair % n_heads, d = n_heads * DH, ld = 3 * d;
@@ -440,7 +450,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *
     const uint16_t *base = qkv + (size_t)s * seq * ld + head * DH, *obase = dout + (size_t)s * seq * d + head * DH;
     const float sc = 1.4426950408889634f / __builtin_sqrtf((float)DH);
     const int e = DT == kFP16 ? scale_exponent(tops + (size_t)item.pair * ((seq + kTile - 1) / kTile), (seq + kTile - 1) / kTile) : 0;
-    const float factor = DT == kFP16 ? ldexpf(1.0f, e - kShift) : 1.0f;
+    const float factor = DT == kFP16 ? ldexpf(1.0f, e - kShift<DT>) : 1.0f;
     uint4 kf[KS], vf[KS];
     {
         const uint16_t *kp = base + d + (size_t)(key < seq ? key : 0) * ld + 8 * fh;
@@ -451,16 +461,18 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *
         }
     }
     const TileReader<DH> read(lane);
-    const TileLoader<DH> load_q(ld, lane, wave), load_o(d, lane, wave);
+    const TileLoader<DH, DH == 128> load_q(ld, lane, wave), load_o(d, lane, wave);
     const int t0 = k0 / kTile, n_tiles = (seq + kTile - 1) / kTile;
     auto load = [&](int t) {
         if (t >= n_tiles) return;
         load_q.load(qs[t & 1], base, t * kTile, seq);
         load_o.load(os[t & 1], obase, t * kTile, seq);
-        if (wave < 2) {                                          // (queries past the end get zeros: their dO is, too)
+        if (wave < 3) {                                          // (queries past the end get zeros: their dO is, too)
             const int left = seq - t * kTile < kTile ? seq - t * kTile : kTile;
-            const float *from = (wave ? delta : lse) + (size_t)item.pair * seq + t * kTile;
-            dma4(buffer_of((uint64_t)(uintptr_t)from, (uint32_t)left * 4), 4 * lane, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&rows[t & 1][wave][0]);
+            const size_t row = (size_t)item.pair * seq + t * kTile;
+            auto lds = [](float *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)p; };
+            if (wave < 2) dma4(buffer_of((uint64_t)(uintptr_t)(rows + 2 * row), (uint32_t)left * 8), 4 * lane + 256 * wave, lds(&refs[t & 1][32 * wave][0]));
+            else dma4(buffer_of((uint64_t)(uintptr_t)(rows + 2 * (size_t)pairs * seq + row), (uint32_t)left * 4), 4 * lane, lds(&minus_d[t & 1][0]));
         }
     };
     f32x16 dk[CT] = {}, dv[CT] = {};
@@ -474,13 +486,18 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *
             const int first = t * kTile + 32 * h;
             if (first < w0) continue;                           // queries that see none of the wavefront's keys
             const u32x4 *qt = qs[t & 1] + h * 32 * T::CH, *ot = os[t & 1] + h * 32 * T::CH;
-            f32x16 S, dP;                                       // from minus logsumexp (over the scaling) and minus D on
+            // S from zero on, by the same products in the same order as in the queries' launch: the same bits, of which the reference is one
+            f32x16 S = {}, dP;                                  // (from minus D on)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float4 l = *(const float4 *)&rows[t & 1][0][32 * h + 8 * g + 4 * fh], v = *(const float4 *)&rows[t & 1][1][32 * h + 8 * g + 4 * fh];
-                S[4 * g] = l.x; S[4 * g + 1] = l.y; S[4 * g + 2] = l.z; S[4 * g + 3] = l.w;
-                dP[4 * g] = v.x; dP[4 * g + 1] = v.y; dP[4 * g + 2] = v.z; dP[4 * g + 3] = v.w;
+                const f32x4 v = *(const f32x4 *)&minus_d[t & 1][32 * h + 8 * g + 4 * fh];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dP[4 * g + j] = v[j];
             }
+            auto two_refs = [&](int j) { return *(const f32x4 *)&refs[t & 1][32 * h + 8 * (j >> 2) + 4 * fh + (j & 3)][0]; };
+            f32x4 ref[AHEAD];                                   // of rows 2 i, 2 i + 1
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) ref[i] = two_refs(2 * i);
             uint4 ring[R];
 #pragma unroll
             for (int i = 0; i < R; ++i) ring[i] = read.by_row(qt, i);
@@ -498,14 +515,17 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *
                     if (8 * (i >> 2) + 4 * fh + (i & 3) < fr) S[i] = -INFINITY;
             }
             uint4 ps[2], ds[2];
-            auto exponent = [&](float v) { return DT == kFP16 ? __builtin_fmaf(v, sc, (float)kShift) : v * sc; };
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 dP = mfma32<DT>(ring[(KS + i) % R], vf[i], dP);
                 __builtin_amdgcn_sched_barrier(0);
                 if (i + R < KS) ring[(KS + i) % R] = read.by_row(ot, i + R);
 #pragma unroll
-                for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) S[j] = __builtin_amdgcn_exp2f(exponent(S[j]));
+                for (int j = 16 * i / KS; j < 16 * (i + 1) / KS; ++j) {
+                    const f32x4 &r = ref[j / 2 % AHEAD];
+                    S[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[j] - r[2 * (j & 1)], sc, r[2 * (j & 1) + 1]));
+                    if ((j & 1) && j + 2 * AHEAD - 1 < 16) ref[j / 2 % AHEAD] = two_refs(j + 2 * AHEAD - 1);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             uint4 oc = read.by_column(ot, 0, 0), qc = read.by_column(qt, 0, 0);
@@ -547,8 +567,8 @@ template <int DT, int DH>
 hipError_t attn_grad(const uint16_t *qkv, const uint16_t *out, const uint16_t *dout, uint16_t *dqkv, char *ws, int n_seq, int seq, int n_heads, hipStream_t s)
 {
     const int pairs = n_seq * n_heads, row_tiles = (seq + kTile - 1) / kTile, tiles = (seq + kOwn - 1) / kOwn;
-    float *delta = (float *)ws, *lse = delta + (size_t)pairs * seq;
-    RowTops *tops = (RowTops *)(lse + (size_t)pairs * seq);
+    float *rows = (float *)ws;                                  // of each query two numbers, then, of each, minus D
+    RowTops *tops = (RowTops *)(rows + 3 * (size_t)pairs * seq);
     hipError_t err = hipSuccess;
     if constexpr (DT == kFP16) {
         attn_grad_tops_kernel<DH><<<dim3(pairs * row_tiles), dim3(256), 0, s>>>(qkv, dout, tops, seq, n_heads, row_tiles);
@@ -556,14 +576,14 @@ hipError_t attn_grad(const uint16_t *qkv, const uint16_t *out, const uint16_t *d
     }
     const dim3 grid((pairs + 7) / 8 * 8 * tiles);
     auto queries = seq <= kShort ? attn_grad_queries_kernel<DT, DH, true> : attn_grad_queries_kernel<DT, DH, false>;
-    queries<<<grid, dim3(256), 0, s>>>(qkv, out, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
+    queries<<<grid, dim3(256), 0, s>>>(qkv, out, dout, dqkv, rows, tops, seq, n_heads, pairs, tiles);
     if ((err = hipGetLastError()) != hipSuccess) return err;
-    attn_grad_keys_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, dout, dqkv, delta, lse, tops, seq, n_heads, pairs, tiles);
+    attn_grad_keys_kernel<DT, DH><<<grid, dim3(256), 0, s>>>(qkv, dout, dqkv, rows, tops, seq, n_heads, pairs, tiles);
     return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ other heads and precisions
-// A workgroup per query of a head: logsumexp over the keys it sees, D, dQ.  128 threads have a key each, then a channel each.
+// A workgroup per query of a head: maximum and sum of the softmax over the keys it sees, D, dQ.  128 threads have a key each, then a channel each.
 template <int DT>
 __global__ __launch_bounds__(128) void attn_grad_query_kernel(const void *__restrict__ qkv_, const void *__restrict__ out_, const void *__restrict__ dout_, void *__restrict__ dqkv_,
                                                               void *__restrict__ rows_, int seq, int n_heads, int d_head, size_t n_rows)
@@ -594,12 +614,12 @@ __global__ __launch_bounds__(128) void attn_grad_query_kernel(const void *__rest
         top = m;
     }
     const Acc most = block_max(top, red);
-    const Acc l = block_sum(sum != (Acc)0 ? sum * (Acc)exp(top - most) : (Acc)0, red), lse = most + (Acc)log(l);
+    const Acc one_over = (Acc)1 / block_sum(sum != (Acc)0 ? sum * (Acc)exp(top - most) : (Acc)0, red);
     Acc dq = 0;
     for (int k0 = 0; k0 <= q; k0 += 128) {
         const int k = k0 + tid;
         __syncthreads();
-        ds[tid] = k <= q ? (Acc)exp(dot(0, k, 1) * scale - lse) * (dot(1, k, 2) - delta) : (Acc)0;
+        ds[tid] = k <= q ? (Acc)exp(dot(0, k, 1) * scale - most) * one_over * (dot(1, k, 2) - delta) : (Acc)0;
         __syncthreads();
         const int n = q - k0 + 1 < 128 ? q - k0 + 1 : 128;
         if (mine)
@@ -609,7 +629,8 @@ __global__ __launch_bounds__(128) void attn_grad_query_kernel(const void *__rest
     if (tid == 0) {
         Acc *rows = (Acc *)rows_ + (size_t)head * n_rows + row;
         rows[0] = delta;
-        rows[(size_t)n_heads * n_rows] = lse;
+        rows[(size_t)n_heads * n_rows] = most;                 // (and the sum by itself: logsumexp would round it to the scores' last place)
+        rows[2 * (size_t)n_heads * n_rows] = one_over;
     }
 }
 // A workgroup per key of a head: dK and dV over the queries that see it.
@@ -625,7 +646,7 @@ __global__ __launch_bounds__(128) void attn_grad_key_kernel(const void *__restri
     const size_t row = blockIdx.x, first = row / seq * seq, ld = 3 * (size_t)d;
     const int key = (int)(row - first);
     const A *qkv = (const A *)qkv_ + head * d_head, *dout = (const A *)dout_ + head * d_head;
-    const Acc *delta = (const Acc *)rows_ + (size_t)head * n_rows + first, *lse = delta + (size_t)n_heads * n_rows;
+    const Acc *delta = (const Acc *)rows_ + (size_t)head * n_rows + first, *most = delta + (size_t)n_heads * n_rows, *one_over = most + (size_t)n_heads * n_rows;
     const Acc scale = (Acc)1 / (Acc)__builtin_sqrt((double)d_head);
     const bool mine = tid < d_head;
     own[0][tid] = mine ? P::a2acc(qkv[row * ld + d + tid]) : (Acc)0;
@@ -639,7 +660,7 @@ __global__ __launch_bounds__(128) void attn_grad_key_kernel(const void *__restri
     for (int q0 = key; q0 < seq; q0 += 128) {
         const int q = q0 + tid;
         __syncthreads();
-        ps[tid] = q < seq ? (Acc)exp(dot(0, qkv + (first + q) * ld) * scale - lse[q]) : (Acc)0;
+        ps[tid] = q < seq ? (Acc)exp(dot(0, qkv + (first + q) * ld) * scale - most[q]) * one_over[q] : (Acc)0;
         ds[tid] = q < seq ? ps[tid] * (dot(1, dout + (first + q) * d) - delta[q]) : (Acc)0;
         __syncthreads();
         const int n = seq - q0 < 128 ? seq - q0 : 128;
@@ -676,10 +697,10 @@ size_t attention_grad_scratch(int dtype, int n_seq, int seq, int n_heads, int d_
     // a launch's size is counted in threads, by 32 bits, and in workgroups of the second dimension by 16
     if (on_matrix_cores(dtype, d_head)) {
         if ((pairs + 7) / 8 * 8 * row_tiles >= (size_t)1 << 24) return 0;
-        return 2 * 4 * pairs * seq + pairs * row_tiles * sizeof(RowTops);
+        return 3 * 4 * pairs * seq + pairs * row_tiles * sizeof(RowTops);
     }
     if ((size_t)n_seq * seq >= (size_t)1 << 25 || n_heads > 65535) return 0;
-    return 2 * acc_bytes(dtype) * pairs * seq;
+    return 3 * acc_bytes(dtype) * pairs * seq;
 }
 
 hipError_t launch_attention_grad(const void *qkv, const void *out, const void *dout, void *dqkv, void *scratch, int dtype, int n_seq, int seq, int n_heads,
