@@ -19,10 +19,6 @@ SOURCES = ["zo_api.hip", "zo_stream_kernels.hip", "zo_forward_kernels.hip", "zo_
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 
-# Matrix instructions write to ordinary registers where these suffice: scores and their gradients are worked on right after, and a result in an
-# accumulation register takes a move more each (attention's gradient, keys of 128 channels: 2517 -> 2258 instructions, 240 -> 62 moves).
-EXTRA = {"zo_attn_grad.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
-
 
 def _hipcc():
     for cand in (os.environ.get("HIPCC"), "/opt/rocm/bin/hipcc", "hipcc"):
@@ -38,7 +34,7 @@ def build(verbose=False):
 
     def compile_one(src):
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
-        cmd = [hipcc] + FLAGS + EXTRA.get(src, []) + ["-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc] + FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         proc = subprocess.run(cmd, capture_output=True, text=True)
