@@ -478,7 +478,9 @@ int zo_kernel_attention_grad(const void *qkv, const void *out, const void *dout,
  *                    has clipped them gives max_norm infinity.  A norm that is not finite: the call writes nothing.
  *   rounding, seed   ZO_ROUND_NEAREST, or ZO_ROUND_STOCHASTIC for the parameters (16-bit types; see zo_set_update_rounding) with words of
  *                    stream 3 for (seed, the tensor's place in the list, element): a seed of its own for each call
- * lr, weight_decay >= 0, beta1 and beta2 in [0, 1), eps > 0. */
+ * lr, weight_decay >= 0, beta1 and beta2 in [0, 1), eps > 0.
+ * A captured graph holds these numbers, and the rates and words worked from them: every replay is the same step number, with the same words for rounding, and
+ * rounds each element up or down by the same threshold.  A loop of steps makes this call beside its graphs, or captures it anew for each step. */
 size_t zo_kernel_adamw_state_bytes(uint64_t numel, int state_bits);
 int zo_kernel_adamw(void *const *param, const void *const *grad, void *const *state, const uint64_t *numel, int n_tensors, int dtype,
                     int state_bits, double lr, double beta1, double beta2, double eps, double weight_decay, uint64_t step,
