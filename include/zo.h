@@ -471,7 +471,7 @@ int zo_kernel_attention_grad(const void *qkv, const void *out, const void *dout,
  *                    state_bits 8: 256 e4m3 numbers, 256 more and two fp32 scales, 520 bytes: m = number x scale[0], sqrt(v) = number
  *                    x scale[1], each scale its block's largest magnitude / 448, nearest even; a v above zero is never held as zero.  A
  *                    moment of three bits behind the first moves once a step changes it by 1/32 to 1/16 of itself beside its block's largest.
- *                    A block with a new moment that is not finite gets a scale that is not a number.
+ *                    A block with a new moment that is not finite gets a scale that is not a number; one of m below 448 x 2^-126 throughout is zeros.
  *   step             counts from 1
  *   norm, max_norm   NULL: c = 1.  Else device: the gradients' global norm (norm[0] of zo_kernel_grad_clip), and c = max_norm / norm[0] where
  *                    norm[0] > max_norm, else 1: a program that has the norm alone need not have the clipped gradients written; one that

@@ -52,7 +52,7 @@ __device__ __forceinline__ void from_e4m3(uint32_t w, float scale, float (&x)[4]
 
 // A block's new numbers as e4m3 and a scale, the largest magnitude / 448.  LOW (no number is negative): what is above zero stays above it,
 // so that a root that is small beside its block's largest never makes a division by eps alone.  A block that holds anything not finite
-// gets a scale that is not a number; one below 2^-126 / 448 in all its magnitudes is zeros.
+// gets a scale that is not a number; one below 448 x 2^-126 in all its magnitudes is zeros.
 template <bool LOW> __device__ __forceinline__ uint32_t hold8(const float (&x)[4], float &scale)
 {
     uint32_t top = 0;
