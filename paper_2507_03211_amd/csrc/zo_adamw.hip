@@ -223,7 +223,7 @@ template <int DT, int BITS, bool SR, bool WHOLE> __device__ __forceinline__ void
 
 // One launch for up to N tensors; a chunk of 4096 elements is a workgroup's at a time, four blocks of 256 a wavefront's, whose loads are all under way
 // before the first is worked (8-bit moments, below: 332 us, two blocks 336, one 345; no difference with 32 bits).  Bound by memory with 32-bit moments: 43 M bf16 weights, 22 bytes each, 187 us (5.1 TB/s; a copy runs
-// at 5.0).  With 8-bit moments and words for rounding by its instructions: 10.06 bytes an element, 137 M bf16 weights 326 us (4.2 TB/s, 276 at the copy
+// at 5.0).  With 8-bit moments and words for rounding by its instructions: 10.06 bytes an element, 137 M bf16 weights 324 - 335 us (4.1 - 4.2 TB/s, 276 at the copy
 // rate): some 350 a block, of which Philox's 19 multiplies take four times as long as others and division, two scales and their maxima the most of the rest.
 template <int DT, int BITS, bool SR, int N>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamBatchOf<N> b, AdamScalars k)

@@ -209,7 +209,7 @@ template <int DH, bool LEAN = false> struct TileLoader : TileShape<DH> {
 
 // Which workgroup has which rows of which (sequence, head): the longest tiles of all pairs first, so that what is left at a launch's end is
 // short; consecutive workgroups go round-robin to the 8 XCDs, all tiles of a pair to one of them.  All tiles of a pair, then the next one's:
-// queries and keys of 4 x 2048, 40 heads of 128 441 and 553 us, here 318 and 452; 16 x 512, 12 of 64 29.0 and 42.0, here 22.8 and 34.7.
+// 4 x 2048, 40 heads of 128 744 us of the whole call, here 693; of 64 410 / 367; 16 x 512, 12 of 64 58.8 / 53.5; 8 x 131, 32 of 80 fp16 40.7 / 35.7.
 struct Item { int pair, tile; };
 __device__ __forceinline__ Item item_of(int block, int pairs)
 {
@@ -227,13 +227,13 @@ __device__ __forceinline__ void put(uint4 (&w)[2], int i, uint32_t v)      // wo
 }
 
 // ------------------------------------------------------------------ queries
-// 32 keys at a time: S, dP beside the exponentials, dQ; two wavefronts per SIMD (211 registers at 128 channels).  Pipelined over two
-// units, with keys in three stages, it is no faster: 4 x 2048, 40 heads of 128 656 us of the whole call in bf16 both ways, of 80 500 / 491, 16 x 512, 12 of 64 52.6 / 51.4,
-// fp16 8 x 131, 32 of 80 35.9 / 35.1; three workgroups to a CU at 96 channels 532 / 546, four at 64 347 / 413 (registers).
+// 32 keys at a time: S, dP beside the exponentials, dQ; two wavefronts per SIMD (210 registers at 128 channels).  Pipelined over two
+// units, with keys in three stages, it was no faster (4 x 2048, 40 heads of 128 656 us of the whole call in bf16 both ways, of 80 500 / 491, 16 x 512, 12 of 64 52.6 / 51.4).
+// Three workgroups to a CU at 96 channels 610 us, four at 64 454 (registers), where this has 554 and 367.
 // D: of sequences up to kShort positions (SHORT) the sum of P dP, by a pass ahead; of longer ones that of dO times `out`, whose rounding to 16 bits then makes the
 // gradients little worse.  Error of all three against 64 bits over that of fp32 arithmetic, both rounded: by `out` 1.67 at 2 positions, 1.57 at 8, 1.51 at 16,
-// 1.48 at 128, 1.46 at 300; by the pass 1.23 - 1.44.  us of the whole call by `out` / by the pass: 8 x 64, 32 heads of 80 fp16 19.4 / 19.2, 8 x 128 bf16 23.3 / 24.9,
-// 16 x 128, 40 of 128 73.2 / 70.9, 256 x 64, 12 of 64 78.4 / 72.7.
+// 1.48 at 128, 1.46 at 300; by the pass 1.23 - 1.44.  us of the whole call by `out` / by the pass: 8 x 64, 32 heads of 80 fp16 18.3 / 18.5, 8 x 128 bf16 23.8 / 25.0,
+// 16 x 128, 40 of 128 73.7 / 72.3, 256 x 64, 12 of 64 76.3 / 72.2.
 template <int DT, int DH, bool SHORT>
 __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ out, const uint16_t *__restrict__ dout,
                                                                    uint16_t *__restrict__ dqkv, float *__restrict__ rows, const RowTops *__restrict__ tops,
@@ -428,11 +428,11 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 
 // ------------------------------------------------------------------ keys
 // 32 queries at a time: S, dP beside P's exponentials, then dV and dK.  Two wavefronts per SIMD, whose waits each other's multiplies fill, are worth more than
-// one whose own are pipelined: at 128 channels dK, dV, K and V leave 64 of 256 registers for the rest, so that nothing is held ahead but two
-// fragments (pinned: the compiler's own order spills there, 674 us).  4 x 2048, 40 heads of 128: 350 - 380 us, matrix cores busy 46 % of the cycles, vector units 29,
-// LDS 29, at 1.97 GHz; the queries' launch 285 - 304, 43, 38 and 22 %.  Pipelined over two units, one wavefront per SIMD with 386 registers / here, us of the whole
-// call in bf16: 4 x 2048, 40 heads of 128 742 / 657, of 112 720 / 635, of 96 582 / 535, of 64 350 / 345; 16 x 512, 12 of 64 54.1 / 51.7; fp16 8 x 131, 32 of 80
-// 36.3 / 35.3.
+// one whose own are pipelined (386 registers; 4 x 2048, 40 heads of 128 742 us of the whole call / 657, of 112 720 / 635, of 96 582 / 535, of 64 350 / 345, 16 x 512, 12 of 64 54.1 /
+// 51.7, when a row had one number, its logsumexp, which is wrong for large scores).  A row's reference and sum apart cost a subtraction and a read more a score: 663 / 681, 638 / 654,
+// 541 / 554, 348 / 367, 50.5 / 53.5.  At 128 channels dK, dV, K and V leave 64 of 256 registers for the rest, so that nothing is held ahead but two fragments and two rows' numbers,
+// and a load's addresses are worked out as it goes out (four rows' numbers and addresses kept: spills, 793).  4 x 2048, 40 heads of 128: 372 - 377 us, matrix cores busy 46 % of the
+// cycles, vector units 32, LDS 31 without conflicts; the queries' launch 294 - 299, 43, 42 and 22 %.
 template <int DT, int DH>
 __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
                                                                 const float *__restrict__ rows, const RowTops *__restrict__ tops,
@@ -471,6 +471,10 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *
             const int left = seq - t * kTile < kTile ? seq - t * kTile : kTile;
             const size_t row = (size_t)item.pair * seq + t * kTile;
             auto lds = [](float *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)p; };
+            // (the lane's number anew: kept, it is spilled at 128 channels, and its reload waits for the tiles: 693 us for 681)
+            int all = -1;
+            asm volatile("" : "+s"(all));
+            const int lane = __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
             if (wave < 2) dma4(buffer_of((uint64_t)(uintptr_t)(rows + 2 * row), (uint32_t)left * 8), 4 * lane + 256 * wave, lds(&refs[t & 1][32 * wave][0]));
             else dma4(buffer_of((uint64_t)(uintptr_t)(rows + 2 * (size_t)pairs * seq + row), (uint32_t)left * 4), 4 * lane, lds(&minus_d[t & 1][0]));
         }
