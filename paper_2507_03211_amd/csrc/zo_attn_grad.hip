@@ -431,8 +431,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_queries_kernel(const uint16_
 // one whose own are pipelined (386 registers; 4 x 2048, 40 heads of 128 742 us of the whole call / 657, of 112 720 / 635, of 96 582 / 535, of 64 350 / 345, 16 x 512, 12 of 64 54.1 /
 // 51.7, when a row had one number, its logsumexp, which is wrong for large scores).  A row's reference and sum apart cost a subtraction and a read more a score: 663 / 681, 638 / 654,
 // 541 / 554, 348 / 367, 50.5 / 53.5.  At 128 channels dK, dV, K and V leave 64 of 256 registers for the rest, so that nothing is held ahead but two fragments and two rows' numbers,
-// and a load's addresses are worked out as it goes out (four rows' numbers and addresses kept: spills, 793).  4 x 2048, 40 heads of 128: 372 - 377 us, matrix cores busy 46 % of the
-// cycles, vector units 32, LDS 31 without conflicts; the queries' launch 294 - 299, 43, 42 and 22 %.
+// and a load's addresses are worked out as it goes out (four rows' numbers and addresses kept: spills, 793).  4 x 2048, 40 heads of 128: 372 - 383 us, matrix cores busy 46 % of the
+// cycles, vector units 32, LDS 31 without conflicts; the queries' launch 294 - 302, 43, 42 and 22 %.
 template <int DT, int DH>
 __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(const uint16_t *__restrict__ qkv, const uint16_t *__restrict__ dout, uint16_t *__restrict__ dqkv,
                                                                 const float *__restrict__ rows, const RowTops *__restrict__ tops,
