@@ -450,7 +450,7 @@ int zo_kernel_linear_grad_plan(int rows, int n, int k, int epilogue, int32_t *pl
  * dqkv overlaps no input (ZO_EINVAL if it does).  Probabilities are worked again from q and k, nothing of the forward call's but `out` is
  * needed.  2-byte dtypes: d_head a multiple of 8, buffers 16-byte aligned (ZO_EINVAL otherwise); heads of 64, 80, 96, 112 and 128 run on the matrix
  * cores, which take P and dS rounded to the type (ZO_FP16: scaled so that no finite P or dS leaves the type's range), others on a slower kernel.  Scores
- * of any size do whose q k stays within fp32 (ZO_FP32: fp64): a score is off by the rounding of that sum alone, and equal keys have equal P.  An
+ * may be of any size as long as q k stays within fp32 (ZO_FP32: fp64): they are off by the rounding of that sum alone, and equal keys have equal P.  An
  * element of qkv, out or dout that is not finite makes gradients of its sequence and head that are none, those of earlier queries that do not
  * see it among them; other sequences and heads do not see it.  On the matrix cores D is summed from P and dout v^T where a sequence has up to 128
  * positions, and `out` is not read.  Any length up to 2^20 positions; up to 2^20 channels and 2^30 rows, and no more
